@@ -6,7 +6,7 @@ import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRCS = [os.path.join(HERE, "csrc", n) for n in ("pgxgo.hip", "pgxhex.hip", "pgxpolicy.hip")]
+SRCS = [os.path.join(HERE, "csrc", n) for n in ("pgxgo.hip", "pgxhex.hip", "pgxpolicy.hip", "pgxcache.hip")]
 LIB = os.path.join(HERE, "libpgxgo.so")
 FAST = os.path.join(HERE, "_fastcall.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,854 @@
+// pgxcache.hip -- a paged cache of keys and values whose slots follow the environments' (include/pgxcache.h), gfx950.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <new>
+
+#include "pgxcache.h"
+
+struct pgxcache_ctx {
+  pgxcache_opts o;
+  void* kv;
+  int32_t *table, *lengths, *refs;
+  uint64_t* free_bits;     // a bit per page: free; 0 behind the last page
+  int32_t* grown;          // [slots] tokens that the slot's last advance made room for
+  int32_t* plan;           // [slots] fork: the page for the copy of the last page, kNoTail or kSkip
+  int32_t* moved_to;       // [pages] compact: where a page at or above `used` goes
+  int2* moves;             // [pages] compact: (from, to)
+  int32_t* counts;         // compact: used, number of moves
+  uint32_t* arrived;       // [kSplitBlocks] attend: blocks of a row that are done, 0 between calls
+  float* partial;          // attend: what they found
+};
+
+namespace {
+
+thread_local int g_last_hip = 0;
+
+#define HIPCHK(expr)                                   \
+  do {                                                 \
+    hipError_t e_ = (expr);                            \
+    if (e_ != hipSuccess) {                            \
+      g_last_hip = (int)e_;                            \
+      return PGXCACHE_EHIP;                            \
+    }                                                  \
+  } while (0)
+
+constexpr int kOneBlock = 1024;      // threads of the kernels that give out pages
+constexpr int kNoTail = -1, kSkip = -2;
+constexpr int kSplitBlocks = 1024;   // most blocks of an attend call that splits sequences
+constexpr int kHeads = 16;           // query heads of a matrix tile
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_2 __attribute__((aligned(2)));
+
+// what every kernel knows of the cache
+struct Cache {
+  char* kv;
+  int32_t *table, *lengths, *refs;
+  uint64_t* free_bits;
+  int32_t* grown;
+  int32_t slots, pages, width, page_shift, layers, kv_heads, head_dim;
+
+  __device__ __forceinline__ int pages_of(int tokens) const { return (int)(((int64_t)tokens + (1 << page_shift) - 1) >> page_shift); }
+  __device__ __forceinline__ int capacity() const { return (int)min((int64_t)width << page_shift, (int64_t)0x7FFFFFFF); }
+  __device__ __forceinline__ int length(int slot) const { return min(max(lengths[slot], 0), capacity()); }
+  __device__ __forceinline__ int32_t* row(int slot) const { return table + (int64_t)slot * width; }
+  __device__ __forceinline__ bool is_page(int p) const { return (uint32_t)p < (uint32_t)pages; }
+  __device__ __forceinline__ int64_t head_bytes() const { return ((int64_t)head_dim << page_shift) * 2; }      // one head's keys or values of a page
+  __device__ __forceinline__ int64_t page_bytes() const { return head_bytes() * kv_heads * 2 * layers; }
+  __device__ __forceinline__ void release(int p) const {   // one table entry less names the page
+    if (is_page(p) && atomicSub(&refs[p], 1) == 1) atomicOr((unsigned long long*)&free_bits[p >> 6], 1ull << (p & 63));
+  }
+};
+
+__global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arrived) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t free = __ballot(i < c.pages && c.refs[min(i, (int64_t)c.pages - 1)] == 0);
+  if ((threadIdx.x & 63) == 0 && i < ((int64_t)c.pages + 63) / 64 * 64) c.free_bits[i >> 6] = free;
+  if (i < c.slots) c.grown[i] = 0;
+  if (i < kSplitBlocks) arrived[i] = 0;
+}
+
+// ---- giving out pages: one block sees all of it ----------------------------------------------------------------------------------
+// sum over the threads before this one; *total: over all
+__device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* shared /* 17 words */, uint32_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t s = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t up = __shfl_up(s, d);
+    if (lane >= d) s += up;
+  }
+  __syncthreads();
+  if (lane == 63) shared[wave] = s;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kOneBlock / 64; ++w) {
+    const uint32_t v = shared[w];
+    before += w < wave ? v : 0;
+    all += v;
+  }
+  *total = all;
+  return before + s - x;
+}
+
+// The free pages in ascending order.  Thread t has counted those in its stretch of the bits; at[t]: how many lie before it.
+struct FreePages {
+  const uint64_t* bits;
+  int words, stretch;
+  uint32_t* at;          // LDS, kOneBlock
+  uint32_t count;
+
+  __device__ __forceinline__ FreePages(const Cache& c, uint32_t* at_, uint32_t* shared) : bits(c.free_bits), words((c.pages + 63) / 64), at(at_) {
+    stretch = (words + kOneBlock - 1) / kOneBlock;
+    uint32_t n = 0;
+    for (int w = (int)threadIdx.x * stretch; w < min(words, ((int)threadIdx.x + 1) * stretch); ++w) n += (uint32_t)__popcll(bits[w]);
+    at[threadIdx.x] = exclusive_sum(n, shared, &count);
+    __syncthreads();
+  }
+  // the page with `rank` free ones below it (rank < count)
+  __device__ __forceinline__ int select(uint32_t rank) const {
+    int t = 0;
+#pragma unroll
+    for (int d = kOneBlock / 2; d > 0; d >>= 1)
+      if (at[t + d] <= rank) t += d;
+    uint32_t left = rank - at[t];
+    int w = t * stretch;
+    uint64_t b = bits[w];
+    while (left >= (uint32_t)__popcll(b)) {
+      left -= (uint32_t)__popcll(b);
+      b = bits[++w];
+    }
+    int bit = 0;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      const uint32_t low = (uint32_t)__popcll(b >> bit & ((1ull << d) - 1));
+      if (left >= low) { left -= low; bit += d; }
+    }
+    return w * 64 + bit;
+  }
+  // the next one above p (there has to be one)
+  __device__ __forceinline__ int next(int p) const {
+    int w = p >> 6;
+    uint64_t b = (p & 63) == 63 ? 0 : bits[w] & ~0ull << ((p & 63) + 1);
+    while (b == 0) b = bits[++w];
+    return w * 64 + (int)__builtin_ctzll(b);
+  }
+};
+
+__global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, int32_t* plan, uint8_t* status) {
+  __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64];
+  const FreePages free(c, at, shared);
+  uint32_t given = 0;
+  for (int first = 0; first < n; first += kOneBlock) {
+    const int i = first + (int)threadIdx.x;
+    const bool entry = i < n;
+    const int slot = !entry ? -1 : slots ? slots[i] : i;
+    const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
+    const int more = !entry ? 0 : counts ? counts[i] : count;
+    uint8_t said = !entry || slot == -1 ? 0 : !is_slot || more < 0 ? PGXCACHE_BAD_ENTRY : 0;
+    int length = 0;
+    uint32_t need = 0, all;
+    if (is_slot && said == 0) {
+      length = c.length(slot);
+      if ((int64_t)length + more > c.capacity()) said = PGXCACHE_FULL;
+      else need = (uint32_t)(c.pages_of(length + more) - c.pages_of(length));
+    }
+    const uint32_t rank = given + exclusive_sum(need, shared, &all);
+    if (need > 0 && (rank > free.count || need > free.count - rank)) { said = PGXCACHE_NO_PAGES; }
+    given = min(given + min(all, 0x40000000u), 0x40000000u);
+    const bool done = is_slot && said == 0;
+    if (done && need > 0) {
+      int32_t* row = c.row(slot) + c.pages_of(length);
+      int p = free.select(rank);
+      for (uint32_t k = 0;;) {
+        row[k] = p;
+        c.refs[p] = 1;
+        if (++k == need) break;
+        p = free.next(p);
+      }
+    }
+    if (is_slot) c.grown[slot] = done ? more : 0;
+    if (done && more > 0) c.lengths[slot] = length + more;
+    if (entry) {
+      plan[i] = done ? (int32_t)need : 0;
+      if (status) status[i] = said;
+    }
+  }
+  __syncthreads();   // no one looks at the bits any more
+  for (int i = (int)threadIdx.x; i < n; i += kOneBlock) {
+    const int need = plan[i];
+    if (need == 0) continue;
+    const int slot = slots ? slots[i] : i, have = c.pages_of(c.length(slot));
+    for (int k = have - need; k < have; ++k) {
+      const int p = c.row(slot)[k];
+      atomicAnd((unsigned long long*)&c.free_bits[p >> 6], ~(1ull << (p & 63)));
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, int32_t* plan, uint8_t* status) {
+  __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64];
+  const FreePages free(c, at, shared);
+  uint32_t given = 0;
+  for (int first = 0; first < n; first += kOneBlock) {
+    const int i = first + (int)threadIdx.x;
+    const bool entry = i < n;
+    const int s = entry ? src[i] : -1, d = entry ? dst[i] : -1;
+    const bool out = s == -1 || d == -1, slots = (uint32_t)s < (uint32_t)c.slots && (uint32_t)d < (uint32_t)c.slots;
+    uint8_t said = out || slots ? 0 : PGXCACHE_BAD_ENTRY;
+    const uint32_t need = slots && s != d && (c.length(s) & ((1 << c.page_shift) - 1)) != 0;
+    uint32_t all;
+    const uint32_t rank = given + exclusive_sum(need, shared, &all);
+    given += all;
+    int tail = !slots || s == d ? kSkip : kNoTail;
+    if (need) {
+      if (rank < free.count) tail = free.select(rank);
+      else { tail = kSkip; said = PGXCACHE_NO_PAGES; }
+    }
+    if (entry) {
+      plan[i] = tail;
+      if (status) status[i] = said;
+    }
+  }
+  __syncthreads();
+  for (int i = (int)threadIdx.x; i < n; i += kOneBlock) {
+    const int p = plan[i];
+    if (p < 0) continue;
+    c.refs[p] = 1;
+    atomicAnd((unsigned long long*)&c.free_bits[p >> 6], ~(1ull << (p & 63)));
+  }
+}
+
+// a block per entry.  A page that both slots name keeps the source's reference throughout, so none comes free in between.
+__global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, const int32_t* plan) {
+  const int i = (int)blockIdx.x, tail = plan[i];
+  if (tail == kSkip) return;
+  const int s = src[i], d = dst[i], length = c.length(s), full = length >> c.page_shift;
+  const int old = c.pages_of(c.length(d)), most = max(old, full + (tail >= 0));
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    c.lengths[d] = length;
+    c.grown[d] = 0;
+  }
+  const int32_t* from = c.row(s);
+  int32_t* to = c.row(d);
+  for (int k = (int)threadIdx.x; k < most; k += 256) {
+    const int now = k < full ? from[k] : k == full && tail >= 0 ? tail : -1;
+    if (k < full && c.is_page(now)) atomicAdd(&c.refs[now], 1);
+    if (k < old) c.release(to[k]);
+    to[k] = now;
+  }
+  if (tail < 0 || !c.is_page(from[full])) return;
+  // the filled beginning of every head's keys and values
+  const int64_t head = c.head_bytes();
+  const int units = (length & ((1 << c.page_shift) - 1)) * c.head_dim / 8, lane = (int)threadIdx.x & 63;
+  const char* a = c.kv + from[full] * c.page_bytes();
+  char* b = c.kv + tail * c.page_bytes();
+  for (int h = (int)threadIdx.x >> 6; h < c.layers * 2 * c.kv_heads; h += 4)
+    for (int u = lane; u < units; u += 64) ((u32x4*)(b + h * head))[u] = ((const u32x4*)(a + h * head))[u];
+}
+
+__global__ void __launch_bounds__(256) free_kernel(Cache c, int n, const int32_t* slots) {
+  const int i = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+  if (i >= n) return;
+  const int slot = slots ? slots[i] : i;
+  if ((uint32_t)slot >= (uint32_t)c.slots) return;
+  int32_t* row = c.row(slot);
+  for (int k = lane, old = c.pages_of(c.length(slot)); k < old; k += 64) c.release(atomicExch(&row[k], -1));
+  if (lane == 0) {
+    c.lengths[slot] = 0;
+    c.grown[slot] = 0;
+  }
+}
+
+__global__ void __launch_bounds__(kOneBlock) compact_plan_kernel(Cache c, int2* moves, int32_t* moved_to, int32_t* counts, int32_t* used_out) {
+  __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64];
+  __shared__ int holes;
+  const FreePages free(c, at, shared);
+  const int used = c.pages - (int)free.count, t = (int)threadIdx.x;
+  const int first = t * free.stretch, last = min(free.words, first + free.stretch);
+  // the free pages below `used`
+  if (threadIdx.x == 0 && used == c.pages) holes = 0;
+  if (used < c.pages && first <= used >> 6 && used >> 6 < last) {
+    uint32_t below = at[t];
+    for (int w = first; w < used >> 6; ++w) below += (uint32_t)__popcll(free.bits[w]);
+    holes = (int)(below + (uint32_t)__popcll(free.bits[used >> 6] & ((1ull << (used & 63)) - 1)));
+  }
+  __syncthreads();
+  const int n = holes;
+  if (t == 0) {
+    counts[0] = used;
+    counts[1] = n;
+    if (used_out) *used_out = used;
+  }
+  // pages in use at and above `used`, in order: the r-th of them goes to the r-th free page
+  uint32_t taken = at[t];          // free pages before the word
+  int to = -1;
+  for (int w = first; w < last; ++w) {
+    const uint64_t b = free.bits[w];
+    const int page = w * 64, inside = min(64, c.pages - page);
+    uint64_t in_use = ~b & (inside == 64 ? ~0ull : (1ull << inside) - 1);
+    if (page < used) in_use &= used - page >= 64 ? 0ull : ~0ull << (used - page);
+    while (in_use) {
+      const int bit = (int)__builtin_ctzll(in_use), p = page + bit;
+      in_use &= in_use - 1;
+      const int below = p - (int)(taken + (uint32_t)__popcll(b & ((1ull << bit) - 1)));   // pages in use below p
+      const int r = below - (used - n);
+      to = to < 0 ? free.select((uint32_t)r) : free.next(to);
+      moves[r] = make_int2(p, to);
+      moved_to[p] = to;
+    }
+    taken += (uint32_t)__popcll(b);
+  }
+  __syncthreads();
+  for (int w = t; w < free.words; w += kOneBlock) {
+    const int page = w * 64, inside = min(64, c.pages - page);
+    const uint64_t there = inside == 64 ? ~0ull : (1ull << inside) - 1;
+    c.free_bits[w] = page + 64 <= used ? 0ull : page >= used ? there : there & ~0ull << (used - page);
+  }
+}
+
+__global__ void __launch_bounds__(256) compact_move_kernel(Cache c, const int2* moves, const int32_t* moved_to, const int32_t* counts) {
+  const int used = counts[0], n = counts[1], lane = (int)threadIdx.x & 63;
+  for (int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); slot < c.slots; slot += (int64_t)gridDim.x * 4) {
+    int32_t* row = c.row((int)slot);
+    for (int k = lane, have = c.pages_of(c.length((int)slot)); k < have; k += 64) {
+      const int p = row[k];
+      if (p >= used && p < c.pages) row[k] = moved_to[p];
+    }
+  }
+  const int64_t units = c.page_bytes() / 16;
+  for (int m = (int)blockIdx.x; m < n; m += (int)gridDim.x) {
+    const int2 move = moves[m];
+    if (threadIdx.x == 0) {
+      c.refs[move.y] = c.refs[move.x];
+      c.refs[move.x] = 0;
+    }
+    const u32x4* a = (const u32x4*)(c.kv + move.x * c.page_bytes());
+    u32x4* b = (u32x4*)(c.kv + move.y * c.page_bytes());
+    for (int64_t u = threadIdx.x; u < units; u += 256) b[u] = a[u];
+  }
+}
+
+struct Tokens {   // keys or values of new tokens
+  const char* p;
+  int64_t entry, token, head;   // strides in bytes
+};
+
+// keys and values of one token: [kv_heads][head_dim] each, by 16 bytes
+__device__ __forceinline__ void write_token(const Cache& c, int layer, int page, int inside, const char* k, int64_t k_head, const char* v, int64_t v_head, int from, int step) {
+  const int units = c.head_dim / 8, per = c.kv_heads * units;
+  char* to = c.kv + page * c.page_bytes() + (int64_t)layer * 2 * c.kv_heads * c.head_bytes() + (int64_t)inside * c.head_dim * 2;
+  for (int u = from; u < 2 * per; u += step) {
+    const int value = u >= per, r = value ? u - per : u, head = r / units, at = r % units * 16;
+    const char* x = (value ? v + head * v_head : k + head * k_head) + at;
+    *(u32x4*)(to + (int64_t)(value * c.kv_heads + head) * c.head_bytes() + at) = *(const u32x4_2*)x;
+  }
+}
+
+// a wavefront per token
+__global__ void __launch_bounds__(256) write_kernel(Cache c, int layer, int n, const int32_t* slots, int tokens, Tokens k, Tokens v) {
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (unit >= (int64_t)n * tokens) return;
+  const int i = (int)(unit / tokens), t = (int)(unit % tokens), slot = slots ? slots[i] : i;
+  if ((uint32_t)slot >= (uint32_t)c.slots) return;
+  const int grown = c.grown[slot], at = c.length(slot) - grown + t;
+  if (t >= grown || at < 0) return;
+  const int page = c.row(slot)[at >> c.page_shift];
+  if (!c.is_page(page)) return;
+  write_token(c, layer, page, at & ((1 << c.page_shift) - 1), k.p + i * k.entry + t * k.token, k.head, v.p + i * v.entry + t * v.token, v.head,
+              (int)threadIdx.x & 63, 64);
+}
+
+// ---- attention of one token per entry ------------------------------------------------------------------------------------------------
+// Bound by the keys and values, which are read once: 2 head_dim elements per token and key head against 4 head_dim multiplications
+// per query head.  The 16 columns of a matrix tile are the query heads that share a key head (those beyond the group are zero), its
+// rows are tokens, 32 at a time:
+//     S^T [32 tokens][16 heads] = K [32][D] * Q^T [D][16],    O^T [D][16] += V^T [D][32] * P^T [32][16]
+// A wavefront keeps everything in registers.  Lane 16 g + c of v_mfma_f32_16x16x32 has row (column) c of its left (right) operand
+// for the 8 contraction indices of group g, and column c, rows 4 g + r of the result.  So a lane that has scored tokens 4 g + r
+// (and 16 + 4 g + r from the second half) holds its probabilities just where the second product wants them, if contraction
+// index 8 g + j there means token 4 g + j for j < 4 and 16 + 4 g + j - 4 above.  V is read along its rows, the lane taking elements
+// c D/16 ... of its 8 tokens; a byte permutation per two values turns them into left operands, the m-th of which has row c stand for
+// element c D/16 + m.  The result then has elements (4 g + r) D/16 + m in the lane: D/4 neighbouring ones per lane.
+struct AttendArgs {
+  const char *q, *k, *v;
+  char* out;
+  float* lse;
+  int64_t q_entry, q_head, k_entry, k_head, v_entry, v_head, out_entry, out_head;   // bytes
+  const int32_t* slots;
+  float* partial;
+  uint32_t* arrived;
+  int32_t n, layer, heads, group, head_tiles, splits;
+  float scale;   // times log2 e
+};
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef f32x4 f32x4_4 __attribute__((aligned(4)));
+
+struct F16 {
+  typedef _Float16 elem;
+  typedef elem x8 __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+struct BF16 {
+  typedef __bf16 elem;
+  typedef elem x8 __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+
+constexpr float kLn2 = 0.69314718055994530942f;
+// The running maximum is raised only when a score passes it by 2^8: probabilities up to that are exact enough in either type (they are
+// held as two numbers), and the tiles' maxima need no exchange between lanes.
+constexpr float kSlack = 8.0f;
+
+__device__ __forceinline__ float across_groups_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float across_groups_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+template <int NT>
+struct Tile {   // 32 tokens: keys [half][32-element part], values [token][dword]
+  u32x4 k[2][NT];
+  uint32_t v[8][NT];
+};
+
+// W wavefronts share a row (an entry and a key head); with W = 4 a row may also be split over blocks
+template <class T, int NT, int W>
+__global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
+  typedef typename T::x8 x8;
+  constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
+  __shared__ float joined_m[4][kHeads], joined_l[4][kHeads];
+  extern __shared__ float joined_o[];   // W = 4: [3][kHeads][D]
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const int64_t unit = W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x / a.splits;
+  const int split = W == 1 ? 0 : (int)(blockIdx.x % a.splits);
+  if (W == 1 && unit >= (int64_t)a.n * c.kv_heads * a.head_tiles) return;
+  const int head_tile = (int)(unit % a.head_tiles), kv_head = (int)(unit / a.head_tiles % c.kv_heads), i = (int)(unit / a.head_tiles / c.kv_heads);
+  const int slot = a.slots ? a.slots[i] : i;
+  const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
+  const int length = is_slot ? c.length(slot) : 0;
+  const int first_head = head_tile * kHeads, heads_here = min(kHeads, a.group - first_head), head0 = kv_head * a.group + first_head;
+
+  if (length == 0) {   // nothing to attend to
+    if (split == 0 && (W == 1 || wave == 0) && col < heads_here) {
+      char* out = a.out + i * a.out_entry + (head0 + col) * a.out_head + g * kOut * 2;
+#pragma unroll
+      for (int u = 0; u < NT; ++u) *(u32x4_2*)(out + u * 16) = u32x4{0, 0, 0, 0};
+      if (a.lse && g == 0) a.lse[(int64_t)i * a.heads + head0 + col] = -INFINITY;
+    }
+    return;
+  }
+  const int tiles = (int)(((int64_t)length + 31) >> 5);
+  const int chunk = ((tiles + a.splits - 1) / a.splits + W - 1) / W * W, active = (tiles + chunk - 1) / chunk;
+  if (split >= active) return;
+  const int begin = split * chunk, end = min(tiles, begin + chunk);
+
+  const int32_t* row = c.row(slot);
+  const int64_t page_bytes = c.page_bytes(), head_bytes = c.head_bytes();
+  const char* keys = c.kv + ((int64_t)a.layer * 2 * c.kv_heads + kv_head) * head_bytes;
+  const char* values = keys + c.kv_heads * head_bytes;
+  const int in_page = (1 << c.page_shift) - 1;
+
+  // the new token's key and value go into the cache first, by the block that reads the last tile
+  if (a.k && end == tiles && c.grown[slot] > 0) {
+    const int at = length - 1, page = row[at >> c.page_shift];
+    if ((W == 1 || wave == 0) && c.is_page(page) && lane < 2 * D / 8) {
+      const int u = lane % (D / 8) * 16;
+      const char* x = lane < D / 8 ? a.k + i * a.k_entry + kv_head * a.k_head : a.v + i * a.v_entry + kv_head * a.v_head;
+      *(u32x4*)((char*)(lane < D / 8 ? keys : values) + page * page_bytes + (int64_t)(at & in_page) * D * 2 + u) = *(const u32x4_2*)(x + u);
+    }
+    // (a wavefront's own memory operations are in order; other wavefronts wait)
+    if (W > 1) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+
+  x8 q[NT];
+  {
+    const char* p = a.q + i * a.q_entry + (head0 + min(col, heads_here - 1)) * a.q_head + g * 16;
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {
+      u32x4 x = *(const u32x4_2*)(p + m * 64);
+      if (col >= heads_here) x = u32x4{0, 0, 0, 0};
+      q[m] = __builtin_bit_cast(x8, x);
+    }
+  }
+
+  float top = -INFINITY, sum = 0.0f;   // of the lane's head: the maximum that all four groups use, and this group's sum
+  f32x4 acc[2 * NT];
+#pragma unroll
+  for (int m = 0; m < 2 * NT; ++m) acc[m] = f32x4{0, 0, 0, 0};
+
+  int ids = 0;   // page of half-tile lane & 1 of the wavefront's tile number (a multiple of 32) + lane / 2
+  const int last_half = (length - 1) >> 4;
+  auto load = [&](Tile<NT>& t, int number) {   // the wavefront's tile of that number
+    const int tile = begin + wave % W + number * W;
+    if ((number & 31) == 0) {
+      const int half = min((tile + (lane >> 1) * W) * 2 + (lane & 1), last_half);
+      const int p = row[(half << 4) >> c.page_shift];
+      ids = c.is_page(p) ? p : 0;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t page = (int64_t)__builtin_amdgcn_readlane(ids, (number & 31) * 2 + h) * page_bytes + (int64_t)((tile * 32 + h * 16) & in_page) * (D * 2);
+      const char* k = keys + page + (col * D * 2 + g * 16);
+#pragma unroll
+      for (int m = 0; m < NT; ++m) t.k[h][m] = *(const u32x4*)(k + m * 64);
+      const char* v = values + page + (g * 4 * D * 2 + col * NT * 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int w = 0; w < NT; ++w) t.v[h * 4 + j][w] = ((const uint32_t*)(v + j * D * 2))[w];
+    }
+  };
+  auto compute = [&](Tile<NT>& t, int number) {
+    const int tile = begin + wave % W + number * W;
+    f32x4 s[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      s[h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int m = 0; m < NT; ++m) s[h] = T::mfma(__builtin_bit_cast(x8, t.k[h][m]), q[m], s[h]);
+      s[h] *= a.scale;
+    }
+    if (tile * 32 + 32 > length) {   // tokens behind the last: no score, and their values may hold anything
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (tile * 32 + h * 16 + g * 4 + r >= length) {
+            s[h][r] = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < NT; ++w) t.v[h * 4 + r][w] = 0;
+          }
+    }
+    float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    if (__any(most > top + kSlack)) {
+      const float now = across_groups_max(fmaxf(most, top));
+      const float factor = now > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 1.0f;
+      top = now;
+      sum *= factor;
+#pragma unroll
+      for (int m = 0; m < 2 * NT; ++m) acc[m] *= factor;
+    }
+    const float from = top > -INFINITY ? top : 0.0f;
+    x8 high, low;   // p = high + low, to 2^-17 (bf16) or 2^-22 (f16) of p: one number would round the output a second time
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float p = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - from);
+      sum += p;
+      high[j] = (typename T::elem)p;
+      low[j] = (typename T::elem)(p - (float)high[j]);
+    }
+#pragma unroll
+    for (int m = 0; m < 2 * NT; ++m) {
+      u32x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_perm(t.v[2 * j + 1][m / 2], t.v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
+      acc[m] = T::mfma(__builtin_bit_cast(x8, x), high, acc[m]);
+      acc[m] = T::mfma(__builtin_bit_cast(x8, x), low, acc[m]);
+    }
+  };
+  const int mine = (end - begin - wave % W + W - 1) / W;   // this wavefront's tiles
+  if (mine > 0) {
+    Tile<NT> t0, t1;
+    load(t0, 0);
+    for (int number = 0; number < mine; number += 2) {   // the next tile is under way while this one is computed
+      if (number + 1 < mine) load(t1, number + 1);
+      compute(t0, number);
+      if (number + 1 >= mine) break;
+      if (number + 2 < mine) load(t0, number + 2);
+      compute(t1, number + 1);
+    }
+  }
+  sum = across_groups_sum(sum);
+
+  if (W > 1) {   // the four wavefronts' parts, into the first's registers
+    if (g == 0) { joined_m[wave][col] = top; joined_l[wave][col] = sum; }
+    __syncthreads();
+    float now = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) now = fmaxf(now, joined_m[w][col]);
+    const float from = now > -INFINITY ? now : 0.0f, factor = __builtin_amdgcn_exp2f(top - from);
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) sum += joined_l[w][col] * __builtin_amdgcn_exp2f(joined_m[w][col] - from);
+    top = now;
+#pragma unroll
+    for (int m = 0; m < 2 * NT; ++m) acc[m] *= factor;
+    if (wave > 0) {
+#pragma unroll
+      for (int m = 0; m < 2 * NT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) joined_o[((wave - 1) * 8 * NT + m * 4 + r) * 64 + lane] = acc[m][r];
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 0; w < W - 1; ++w)
+#pragma unroll
+        for (int m = 0; m < 2 * NT; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[m][r] += joined_o[(w * 8 * NT + m * 4 + r) * 64 + lane];
+    }
+  }
+
+  if (W == 1 || active == 1) {
+    if (W > 1 && wave > 0) return;
+    if (col >= heads_here) return;
+    const float inverse = 1.0f / sum;
+    char* out = a.out + i * a.out_entry + (head0 + col) * a.out_head + g * kOut * 2;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      x8 x;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (typename T::elem)(acc[(u * 8 + e) % (2 * NT)][(u * 8 + e) / (2 * NT)] * inverse);
+      *(u32x4_2*)(out + u * 16) = __builtin_bit_cast(u32x4, x);
+    }
+    if (a.lse && g == 0) a.lse[(int64_t)i * a.heads + head0 + col] = (top + __log2f(sum)) * kLn2;
+    return;
+  }
+
+  // The row is split over `active` blocks: each leaves its part in memory, and the one that comes last joins them, in their order.
+  constexpr int kPart = kHeads * (D + 2);
+  float* parts = a.partial + unit * a.splits * kPart;
+  if (wave == 0 && col < heads_here) {
+    float* p = parts + (int64_t)split * kPart;
+    if (g == 0) { p[col] = top; p[kHeads + col] = sum; }
+    float* o = p + 2 * kHeads + col * D + g * kOut;
+#pragma unroll
+    for (int u = 0; u < kOut / 4; ++u) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = acc[(u * 4 + e) % (2 * NT)][(u * 4 + e) / (2 * NT)];
+      *(f32x4_4*)(o + u * 4) = x;
+    }
+    __threadfence();
+  }
+  __shared__ int is_last;
+  __syncthreads();
+  if (threadIdx.x == 0) is_last = atomicAdd(&a.arrived[unit], 1u) == (uint32_t)active - 1u;
+  __syncthreads();
+  if (!is_last) return;
+  __threadfence();
+  if (threadIdx.x == 0) a.arrived[unit] = 0;
+  float* weights = joined_o;   // [active][kHeads], active <= 256
+  for (int h = wave; h < heads_here; h += 4) {
+    float m = -INFINITY;
+    for (int s = lane; s < active; s += 64) m = fmaxf(m, parts[(int64_t)s * kPart + h]);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    const float from = m > -INFINITY ? m : 0.0f;
+    float l = 0.0f;
+    for (int s = lane; s < active; s += 64) l += parts[(int64_t)s * kPart + kHeads + h] * __builtin_amdgcn_exp2f(parts[(int64_t)s * kPart + h] - from);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+    const float inverse = 1.0f / l;
+    for (int s = lane; s < active; s += 64) weights[s * kHeads + h] = __builtin_amdgcn_exp2f(parts[(int64_t)s * kPart + h] - from) * inverse;
+    if (a.lse && lane == 0) a.lse[(int64_t)i * a.heads + head0 + h] = (m + __log2f(l)) * kLn2;
+  }
+  __syncthreads();
+  for (int e = (int)threadIdx.x; e < heads_here * D; e += 256) {
+    const int h = e / D, d = e % D;
+    const float* o = parts + 2 * kHeads + e;
+    float x = 0.0f;
+#pragma unroll 8
+    for (int s = 0; s < active; ++s) x += weights[s * kHeads + h] * o[(int64_t)s * kPart];
+    ((typename T::elem*)(a.out + i * a.out_entry + (head0 + h) * a.out_head))[d] = (typename T::elem)x;
+  }
+}
+
+template <class T, int NT>
+hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles;
+  // enough rows to give every wavefront slot of the machine one: a wavefront each; else four, and long rows are split over blocks
+  if (rows >= 4096) {
+    a.splits = 1;
+    hipLaunchKernelGGL((attend_kernel<T, NT, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, c, a);
+  } else {
+    const int64_t most_tiles = ((int64_t)c.width << c.page_shift) / 32 + 1, spread = kSplitBlocks / rows;
+    int64_t splits = spread < (most_tiles + 3) / 4 ? spread : (most_tiles + 3) / 4;
+    a.splits = (int32_t)(splits < 1 ? 1 : splits > 256 ? 256 : splits);
+    const size_t join = (size_t)3 * kHeads * NT * 32 * 4, weights = (size_t)a.splits * kHeads * 4;
+    hipLaunchKernelGGL((attend_kernel<T, NT, 4>), dim3((unsigned)(rows * a.splits)), dim3(256), join > weights ? join : weights, stream, c, a);
+  }
+  return hipGetLastError();
+}
+template <class T>
+hipError_t launch_attend_for(const Cache& c, const AttendArgs& a, hipStream_t stream) {
+  switch (c.head_dim) {
+    case 32: return launch_attend<T, 1>(c, a, stream);
+    case 64: return launch_attend<T, 2>(c, a, stream);
+    case 96: return launch_attend<T, 3>(c, a, stream);
+    case 128: return launch_attend<T, 4>(c, a, stream);
+    default: return launch_attend<T, 8>(c, a, stream);
+  }
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------------------------
+bool opts_ok(const pgxcache_opts* o) {
+  if (!o || o->slots < 1 || o->pages < 1 || o->width < 1 || o->layers < 1 || o->kv_heads < 1) return false;
+  if (o->width > (1 << 20) || o->layers > 4096 || o->kv_heads > 4096 || o->pages > 0x7FFFFFC0) return false;
+  if (o->page_size < 16 || o->page_size > 1024 || (o->page_size & (o->page_size - 1)) != 0) return false;
+  if (o->head_dim != 32 && o->head_dim != 64 && o->head_dim != 96 && o->head_dim != 128 && o->head_dim != 256) return false;
+  return o->type == PGXCACHE_F16 || o->type == PGXCACHE_BF16;
+}
+
+struct Layout {
+  size_t free_bits, grown, plan, moved_to, moves, counts, arrived, partial, total;
+};
+Layout layout(const pgxcache_opts& o) {
+  Layout l;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  l.free_bits = take(((size_t)o.pages + 63) / 64 * 8);
+  l.grown = take((size_t)o.slots * 4);
+  l.plan = take((size_t)o.slots * 4);
+  l.moved_to = take((size_t)o.pages * 4);
+  l.moves = take((size_t)o.pages * 8);
+  l.counts = take(8);
+  l.arrived = take(kSplitBlocks * 4);
+  l.partial = take((size_t)kSplitBlocks * kHeads * ((size_t)o.head_dim + 2) * 4);
+  l.total = at;
+  return l;
+}
+
+Cache cache_of(pgxcache_t h) {
+  Cache c;
+  c.kv = (char*)h->kv; c.table = h->table; c.lengths = h->lengths; c.refs = h->refs; c.free_bits = h->free_bits; c.grown = h->grown;
+  c.slots = h->o.slots; c.pages = h->o.pages; c.width = h->o.width; c.page_shift = __builtin_ctz((unsigned)h->o.page_size);
+  c.layers = h->o.layers; c.kv_heads = h->o.kv_heads; c.head_dim = h->o.head_dim;
+  return c;
+}
+bool list_ok(pgxcache_t h, int32_t n) { return h && n >= 0 && n <= h->o.slots; }
+
+}  // namespace
+
+extern "C" {
+
+size_t pgxcache_work_bytes(const pgxcache_opts* opts) { return opts_ok(opts) ? layout(*opts).total : 0; }
+
+int pgxcache_rescan(pgxcache_t h) {
+  if (!h) return PGXCACHE_EINVAL;
+  const int64_t most = h->o.pages > h->o.slots ? h->o.pages : h->o.slots, threads = most > kSplitBlocks ? most : kSplitBlocks;
+  hipLaunchKernelGGL(scan_refs_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), h->arrived);
+  HIPCHK(hipGetLastError());
+  return PGXCACHE_OK;
+}
+
+int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
+                  void* work_dev, size_t work_bytes) {
+  if (!out || !opts_ok(opts) || !kv_dev || !table_dev || !lengths_dev || !refs_dev || !work_dev) return PGXCACHE_EINVAL;
+  if (((uintptr_t)kv_dev & 15u) != 0 || ((uintptr_t)work_dev & 255u) != 0) return PGXCACHE_EINVAL;
+  if ((((uintptr_t)table_dev | (uintptr_t)lengths_dev | (uintptr_t)refs_dev) & 3u) != 0) return PGXCACHE_EINVAL;
+  const Layout l = layout(*opts);
+  if (work_bytes < l.total) return PGXCACHE_EINVAL;
+  pgxcache_t h = new (std::nothrow) pgxcache_ctx;
+  if (!h) return PGXCACHE_ENOMEM;
+  char* w = (char*)work_dev;
+  h->o = *opts;
+  h->kv = kv_dev; h->table = table_dev; h->lengths = lengths_dev; h->refs = refs_dev;
+  h->free_bits = (uint64_t*)(w + l.free_bits); h->grown = (int32_t*)(w + l.grown); h->plan = (int32_t*)(w + l.plan);
+  h->moved_to = (int32_t*)(w + l.moved_to); h->moves = (int2*)(w + l.moves); h->counts = (int32_t*)(w + l.counts);
+  h->arrived = (uint32_t*)(w + l.arrived); h->partial = (float*)(w + l.partial);
+  const int rc = pgxcache_rescan(h);
+  if (rc != PGXCACHE_OK) { delete h; return rc; }
+  *out = h;
+  return PGXCACHE_OK;
+}
+
+int pgxcache_destroy(pgxcache_t h) {
+  if (!h) return PGXCACHE_EINVAL;
+  delete h;
+  return PGXCACHE_OK;
+}
+
+int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const int32_t* counts_dev, int32_t count, uint8_t* status_dev) {
+  if (!list_ok(h, n) || (!counts_dev && count < 0)) return PGXCACHE_EINVAL;
+  if (n == 0) return PGXCACHE_OK;
+  hipLaunchKernelGGL(advance_kernel, dim3(1), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, slots_dev, counts_dev, count, h->plan, status_dev);
+  HIPCHK(hipGetLastError());
+  return PGXCACHE_OK;
+}
+
+int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t tokens, const void* k_dev, int64_t k_entry_stride,
+                   int64_t k_token_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride, int64_t v_token_stride, int64_t v_head_stride) {
+  if (!list_ok(h, n) || layer < 0 || layer >= h->o.layers || tokens < 0) return PGXCACHE_EINVAL;
+  if (n == 0 || tokens == 0) return PGXCACHE_OK;
+  if (!k_dev || !v_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 1u) != 0) return PGXCACHE_EINVAL;
+  const int64_t blocks = ((int64_t)n * tokens + 3) / 4;
+  if (blocks > 0x7FFFFFFF) return PGXCACHE_EINVAL;
+  const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};
+  hipLaunchKernelGGL(write_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), layer, n, slots_dev, tokens, k, v);
+  HIPCHK(hipGetLastError());
+  return PGXCACHE_OK;
+}
+
+int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t heads, const void* q_dev, int64_t q_entry_stride,
+                    int64_t q_head_stride, const void* k_dev, int64_t k_entry_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride,
+                    int64_t v_head_stride, float scale, void* out_dev, int64_t out_entry_stride, int64_t out_head_stride, float* lse_dev) {
+  if (!list_ok(h, n) || layer < 0 || layer >= h->o.layers || heads < 1 || heads > 65536 || heads % h->o.kv_heads != 0) return PGXCACHE_EINVAL;
+  if (!(scale - scale == 0.0f) || (k_dev != nullptr) != (v_dev != nullptr)) return PGXCACHE_EINVAL;
+  if (n == 0) return PGXCACHE_OK;
+  if (!q_dev || !out_dev || (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)out_dev) & 1u) != 0) return PGXCACHE_EINVAL;
+  AttendArgs a;
+  a.q = (const char*)q_dev; a.k = (const char*)k_dev; a.v = (const char*)v_dev; a.out = (char*)out_dev; a.lse = lse_dev;
+  a.q_entry = q_entry_stride * 2; a.q_head = q_head_stride * 2; a.k_entry = k_entry_stride * 2; a.k_head = k_head_stride * 2;
+  a.v_entry = v_entry_stride * 2; a.v_head = v_head_stride * 2; a.out_entry = out_entry_stride * 2; a.out_head = out_head_stride * 2;
+  a.slots = slots_dev; a.partial = h->partial; a.arrived = h->arrived;
+  a.n = n; a.layer = layer; a.heads = heads; a.group = heads / h->o.kv_heads; a.head_tiles = (a.group + kHeads - 1) / kHeads;
+  a.scale = scale * 1.44269504088896340736f;
+  if ((int64_t)n * h->o.kv_heads * a.head_tiles > 0x7FFFFFFF) return PGXCACHE_EINVAL;
+  const Cache c = cache_of(h);
+  HIPCHK(h->o.type == PGXCACHE_F16 ? launch_attend_for<F16>(c, a, (hipStream_t)h->o.stream) : launch_attend_for<BF16>(c, a, (hipStream_t)h->o.stream));
+  return PGXCACHE_OK;
+}
+
+int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const int32_t* dst_slots_dev, uint8_t* status_dev) {
+  if (!list_ok(h, n)) return PGXCACHE_EINVAL;
+  if (n == 0) return PGXCACHE_OK;
+  if (!src_slots_dev || !dst_slots_dev) return PGXCACHE_EINVAL;
+  hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan, status_dev);
+  HIPCHK(hipGetLastError());
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan);
+  HIPCHK(hipGetLastError());
+  return PGXCACHE_OK;
+}
+
+int pgxcache_free(pgxcache_t h, int32_t n, const int32_t* slots_dev) {
+  if (!list_ok(h, n)) return PGXCACHE_EINVAL;
+  if (n == 0) return PGXCACHE_OK;
+  hipLaunchKernelGGL(free_kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, slots_dev);
+  HIPCHK(hipGetLastError());
+  return PGXCACHE_OK;
+}
+
+int pgxcache_compact(pgxcache_t h, int32_t* used_dev) {
+  if (!h) return PGXCACHE_EINVAL;
+  hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), h->moves, h->moved_to, h->counts, used_dev);
+  HIPCHK(hipGetLastError());
+  hipLaunchKernelGGL(compact_move_kernel, dim3(2048), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), h->moves, h->moved_to, h->counts);
+  HIPCHK(hipGetLastError());
+  return PGXCACHE_OK;
+}
+
+const char* pgxcache_strerror(int code) {
+  switch (code) {
+    case PGXCACHE_OK: return "ok";
+    case PGXCACHE_EINVAL: return "invalid argument";
+    case PGXCACHE_EHIP: return "HIP runtime error";
+    case PGXCACHE_ENOMEM: return "out of host memory";
+    default: return "unknown error";
+  }
+}
+
+int pgxcache_last_hip_error(void) { return g_last_hip; }
+
+}  // extern "C"
