@@ -45,7 +45,7 @@ def build_fastcall(verbose: bool = False) -> str:
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = [
         "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-        *[f"-I{p}" for p in cpp_extension.include_paths()], "-I" + sysconfig.get_paths()["include"],
+        *[f"-I{p}" for p in cpp_extension.include_paths()], "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"],
         "-o", FAST, os.path.join(HERE, "csrc", "fastcall.cpp"), f"-L{libs}", "-lc10", "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{libs}",
     ]
     if verbose:

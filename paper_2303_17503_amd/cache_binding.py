@@ -3,12 +3,14 @@ import ctypes as C
 
 import torch
 
-from .binding import PgxGoError, _need, _ptr, lib as _golib
+from . import binding
+from .binding import PgxGoError, _address, _need, _ptr, lib as _golib
 
 TYPES = {torch.float16: 1, torch.bfloat16: 2}
 HEAD_DIMS = (32, 64, 96, 128, 256)
 NO_PAGES, FULL, BAD_ENTRY = 1, 2, 255
 _ready = False
+_fast = None   # as in binding.py
 
 
 class _Opts(C.Structure):
@@ -17,7 +19,7 @@ class _Opts(C.Structure):
 
 def lib():
     """The shared library with the pgxcache_* prototypes declared; raises if it has not been built (no fallback)."""
-    global _ready
+    global _ready, _fast
     L = _golib()
     if not _ready:
         vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
@@ -35,6 +37,7 @@ def lib():
         L.pgxcache_strerror.restype = C.c_char_p
         L.pgxcache_strerror.argtypes = [C.c_int]
         L.pgxcache_last_hip_error.restype = C.c_int
+        _fast = binding._fast
         _ready = True
     return L
 
@@ -78,6 +81,10 @@ class PagedCache:
             h = C.c_void_p()
             _check(L.pgxcache_init(C.byref(h), C.byref(opts), _ptr(kv), _ptr(table), _ptr(lengths), _ptr(refs), _ptr(self._work), nbytes), "pgxcache_init")
         self._h = h
+        if _fast is not None:
+            self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "attend", "fork")}
+            self._shape = (self.slots, self.kv_heads, self.head_dim, TYPES[self.dtype], self.device.index)
+        self._scale = self.head_dim ** -0.5
 
     @classmethod
     def empty(cls, slots, pages, max_length, layers, kv_heads, head_dim, page_size=16, dtype=torch.bfloat16, device="cuda:0"):
@@ -120,6 +127,10 @@ class PagedCache:
 
     def advance(self, slots=None, counts=1, status=None):
         """Room for counts (a number, or int32 [n]) more tokens in each of the slots (int32 [n], pairwise distinct; None: all)."""
+        if _fast is not None:
+            rc = _fast.cache_advance(self._calls["advance"], self._h.value, self._shape, slots, counts, status)
+            if rc == 0: return
+            if rc is not None: _check(rc, "pgxcache_advance")
         n, p = self._list(slots)
         each = isinstance(counts, torch.Tensor)
         if each: _need(counts, torch.int32, (n,), "counts")
@@ -129,6 +140,10 @@ class PagedCache:
     def write(self, layer, k, v, slots=None):
         """Keys and values of the tokens that the slots' last advance made room for: [n][kv_heads][head_dim], or [n][tokens][kv_heads][head_dim]
         of which a slot takes as many as it has room for."""
+        if _fast is not None:   # (one token per slot)
+            rc = _fast.cache_write(self._calls["write"], self._h.value, self._shape, layer, k, v, slots)
+            if rc == 0: return
+            if rc is not None: _check(rc, "pgxcache_write")
         n, p = self._list(slots)
         many = getattr(k, "ndim", 0) == 4
         tokens = k.shape[1] if many else 1
@@ -141,6 +156,11 @@ class PagedCache:
         """Attention of one token per slot, q [n][heads][head_dim], over the slot's tokens; heads a multiple of kv_heads; scale: head_dim ** -0.5.
         k and v [n][kv_heads][head_dim] (both or neither): the newest token's, written to the cache on the way.  Returns out, or with
         lse (True, or a float32 [n][heads] tensor) out and the logarithms of the sums of exponentials."""
+        scale = self._scale if scale is None else scale
+        if _fast is not None:
+            got = _fast.cache_attend(self._calls["attend"], self._h.value, self._shape, layer, q, slots, k, v, scale, out, lse)
+            if type(got) is tuple: return got[0] if lse is False else got
+            if got is not None: _check(got, "pgxcache_attend")
         n, p = self._list(slots)
         if getattr(q, "ndim", 0) != 3:
             raise PgxGoError("q: expected [n][heads][head_dim]")
@@ -160,14 +180,17 @@ class PagedCache:
         op = self._heads(out, (n, heads, self.head_dim), "out")
         if lse is True: lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
         elif lse is not False: _need(lse, torch.float32, (n, heads), "lse")
-        scale = self.head_dim ** -0.5 if scale is None else float(scale)
-        _check(lib().pgxcache_attend(self._h, int(layer), n, p, heads, qp, *q.stride()[:2], kp, *ks, vp, *vs, scale, op, *out.stride()[:2],
+        _check(lib().pgxcache_attend(self._h, int(layer), n, p, heads, qp, *q.stride()[:2], kp, *ks, vp, *vs, float(scale), op, *out.stride()[:2],
                                      None if lse is False else lse.data_ptr()), "pgxcache_attend")
         return out if lse is False else (out, lse)
 
     def fork(self, src, dst, status=None):
         """slot[dst[i]] = slot[src[i]]: full pages are shared, a partly filled last one is copied.  As for GoEnv.copy_slots, destinations are
         pairwise distinct and none is the source of another entry."""
+        if _fast is not None:
+            rc = _fast.cache_fork(self._calls["fork"], self._h.value, self._shape, src, dst, status)
+            if rc == 0: return
+            if rc is not None: _check(rc, "pgxcache_fork")
         n, s = self._list(src, "src")
         _need(dst, torch.int32, (n,), "dst")
         _check(lib().pgxcache_fork(self._h, n, s, _ptr(dst), self._status(status, n)), "pgxcache_fork")

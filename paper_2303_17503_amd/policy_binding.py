@@ -8,11 +8,14 @@ import ctypes as C
 
 import torch
 
-from .binding import PgxGoError, _ptr, lib as _golib
+from . import binding
+from .binding import PgxGoError, _address, _ptr, lib as _golib
 
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 MAX_ACTIONS, MAX_RECORD = 8192, 65535
 _ready = False
+_fast = None   # as in binding.py: checks the arguments, makes the outputs and calls, or leaves the call to the Python lines
+_calls = {}
 
 
 class _Adjust(C.Structure):
@@ -24,7 +27,7 @@ class _Adjust(C.Structure):
 
 def lib():
     """The shared library with the pgxpolicy_* prototypes declared; raises if it has not been built (no fallback)."""
-    global _ready
+    global _ready, _fast
     L = _golib()
     if not _ready:
         vp, i32, i64, f32, adj = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.POINTER(_Adjust)
@@ -34,6 +37,10 @@ def lib():
         L.pgxpolicy_strerror.restype = C.c_char_p
         L.pgxpolicy_strerror.argtypes = [C.c_int]
         L.pgxpolicy_last_hip_error.restype = C.c_int
+        _calls.update({n: _address(getattr(L, "pgxpolicy_" + n)) for n in ("logits", "sample", "loss")})
+        _fast = binding._fast
+        if _fast is not None:
+            _fast.set_raw_stream(torch._C._cuda_getCurrentRawStream)
         _ready = True
     return L
 
@@ -114,6 +121,11 @@ def adjust_logits(logits, mask=None, bias=None, record=None, begin=None, end=Non
     logits float32, float16 or bfloat16 [rows][actions]; mask uint8 or bool [rows][>= actions], as GoEnv.new_mask; bias float32 [actions] or
     [rows][actions]; record int32 [rows][plies] of any strides, of which plies begin[b] <= t < end[b] count (int32 [rows]);
     repetition above 1, frequency and presence above 0 make repeated moves less likely; temperature a number or float32 [rows]."""
+    if not _ready: lib()
+    if _fast is not None:
+        got = _fast.policy_logits(_calls["logits"], logits, mask, bias, record, begin, end, repetition, frequency, presence, temperature, normalize, out)
+        if type(got) is tuple: return got[0]
+        if got is not None: _check(got, "pgxpolicy_logits")
     rows, actions = _logits(logits)
     a = _adjust(logits, rows, actions, mask, bias, record, begin, end, repetition, frequency, presence, temperature)
     if out is None:
@@ -130,6 +142,11 @@ def sample_actions(logits, noise=None, mask=None, bias=None, record=None, begin=
     """(int32 [rows] actions, float32 [rows] their log-probabilities): the possible action with the largest adjusted logit plus noise.
     With Gumbel noise (float32 [rows][actions]) a draw from the adjusted distribution, without it the most likely action; rows
     of temperature 0 are greedy.  -1 and 0 where nothing is possible.  Other arguments as for adjust_logits."""
+    if not _ready: lib()
+    if _fast is not None:
+        got = _fast.policy_sample(_calls["sample"], logits, noise, mask, bias, record, begin, end, repetition, frequency, presence, temperature, out, logp)
+        if type(got) is tuple: return got
+        if got is not None: _check(got, "pgxpolicy_sample")
     rows, actions = _logits(logits)
     a = _adjust(logits, rows, actions, mask, bias, record, begin, end, repetition, frequency, presence, temperature)
     dev = logits.device
@@ -148,6 +165,12 @@ def policy_loss(logits, target, weight=None, entropy=0.0, grad_scale=1.0, mask=N
     weight (float32 [rows]), less `entropy` times its entropy; the gradient of grad_scale times the sum of the losses for the logits,
     in their type, comes with it (logits.backward(gradient) goes on from there).  target: float32 [rows][actions], a search's visit
     shares, or int32 [rows], a move each (-1: none).  Other arguments as for adjust_logits."""
+    if not _ready: lib()
+    if _fast is not None:
+        got = _fast.policy_loss(_calls["loss"], logits, target, weight, entropy, grad_scale, mask, bias, record, begin, end, repetition, frequency, presence,
+                                temperature, grad)
+        if type(got) is tuple: return got
+        if got is not None: _check(got, "pgxpolicy_loss")
     rows, actions = _logits(logits)
     a = _adjust(logits, rows, actions, mask, bias, record, begin, end, repetition, frequency, presence, temperature)
     dev = logits.device

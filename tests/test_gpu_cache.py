@@ -374,3 +374,31 @@ REFUSED = [
 def test_refusals(what):
     with pytest.raises(pg.PgxGoError):
         dict(REFUSED)[what](*cache_and_more())
+
+
+@pytest.mark.parametrize("what", [n for n, _ in REFUSED])
+def test_refusals_without_the_native_checks(what, monkeypatch):
+    monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    test_refusals(what)
+
+
+def test_native_and_python_checks_make_the_same_calls(monkeypatch):
+    def history():
+        g = torch.Generator("cuda").manual_seed(1)
+        new = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+        cache = filled([20, 5, 0, 33], 2, 2, 64, 16, torch.bfloat16, width=6, spare=20, junk=0.0)
+        out, status = [], torch.zeros(3, dtype=torch.uint8, device="cuda")
+        cache.advance()
+        cache.write(0, new(4, 2, 64), new(4, 2, 64))
+        cache.advance(ints([3, -1, 9]), ints([2, 1, 1]), status)
+        cache.write(1, new(3, 2, 64), new(3, 2, 64), ints([3, -1, 9]))
+        out += [status.clone(), cache.attend(0, new(4, 6, 64)), *cache.attend(1, new(2, 2, 64), ints([3, 0]), k=new(2, 2, 64), v=new(2, 2, 64), scale=1, lse=True)]
+        out += [*cache.attend(1, new(4, 2, 64), out=torch.empty(4, 2, 64, dtype=torch.bfloat16, device="cuda"), lse=torch.empty(4, 2, device="cuda"))]
+        cache.fork(ints([3, 0, -1]), ints([1, 2, 0]), status)
+        return out + [status, cache.kv, cache.table, cache.lengths, cache.refs]
+
+    assert pg.cache_binding._fast is not None
+    native = history()
+    monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    for a, b in zip(native, history()):
+        assert torch.equal(a, b)

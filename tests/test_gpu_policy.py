@@ -323,3 +323,43 @@ def test_refusals(what):
     k = {"mask": torch.ones(8, 82, dtype=torch.uint8, device="cuda"), "bias": torch.zeros(82, device="cuda")}
     with pytest.raises(pg.PgxGoError):
         dict(REFUSED)[what](x, k)
+
+
+@pytest.mark.parametrize("what", [n for n, _ in REFUSED])
+def test_refusals_without_the_native_checks(what, monkeypatch):
+    monkeypatch.setattr(pg.policy_binding, "_fast", None)
+    test_refusals(what)
+
+
+@pytest.mark.parametrize("actions", [5, 82, 362])
+def test_native_and_python_checks_make_the_same_calls(actions, monkeypatch):
+    x, how, g = inputs(12, actions, "bf16", 4, padded=True, record=9, time_major=True)
+    noise, y, w = torch.randn(12, actions, generator=g).cuda(), torch.rand(12, actions, generator=g).cuda(), torch.randn(12, generator=g).cuda()
+    moves = torch.randint(-1, actions, (12,), generator=g, dtype=torch.int32).cuda()
+    plain = {k: v for k, v in how.items() if k == "mask"}
+
+    def every():
+        out = []
+        for h in (how, plain, {**plain, "temperature": 2}, {**plain, "bias": noise}):
+            out += [pg.adjust_logits(x, **h), pg.adjust_logits(x, normalize=True, **h), *pg.sample_actions(x, noise=noise, **h), *pg.sample_actions(x, **h),
+                    *pg.policy_loss(x, y, weight=w, entropy=0.1, grad_scale=0.5, **h), *pg.policy_loss(x, moves, **h)]
+        return out
+
+    calls = []
+    real = pg.policy_binding._fast
+
+    class Counting:
+        def __getattr__(self, name):
+            def call(*a):
+                got = getattr(real, name)(*a)
+                calls.append(got)
+                return got
+            return call
+
+    assert real is not None
+    monkeypatch.setattr(pg.policy_binding, "_fast", Counting())
+    native = every()
+    assert len(calls) == 24 and all(type(c) is tuple for c in calls)   # none was left to Python
+    monkeypatch.setattr(pg.policy_binding, "_fast", None)
+    for a, b in zip(native, every()):
+        assert a.dtype == b.dtype and torch.equal(a.view(torch.int16 if a.dtype == torch.bfloat16 else torch.int32), b.view(torch.int16 if b.dtype == torch.bfloat16 else torch.int32))
