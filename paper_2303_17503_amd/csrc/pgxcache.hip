@@ -70,9 +70,16 @@ __global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arriv
   if (i < kSplitBlocks) arrived[i] = 0;
 }
 
-// ---- giving out pages: one block sees all of it ----------------------------------------------------------------------------------
+// ---- giving out pages ----------------------------------------------------------------------------------------------------------------
+// A call takes the lowest free pages, its entries in their order.  Which entry gets which follows from the free pages' bits and the
+// needs of the entries before it, and every block of a planning kernel works both out for itself from memory that no one writes
+// meanwhile; a second kernel then takes the pages out of the bits.  Bound by the round trips to memory that depend on each other (the list, the
+// lengths it names; the bits beside them), so the bits are kept in LDS.  4096 entries of a pool of 143000 pages: one block that took the
+// entries 1024 at a time and looked the bits up in memory took 40 us; blocks of 1024 entries side by side take <<FORK_PLAN_4096>>.
+constexpr int kBitsInLds = 4096;   // words: pools of up to 262144 pages; beyond, the bits are looked up in memory
+
 // sum over the threads before this one; *total: over all
-__device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* shared /* 17 words */, uint32_t* total) {
+__device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* shared /* kOneBlock / 64 words */, uint32_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t s = x;
 #pragma unroll
@@ -97,18 +104,51 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* shared /
 // The free pages in ascending order.  Thread t has counted those in its stretch of the bits; at[t]: how many lie before it.
 struct FreePages {
   const uint64_t* bits;
+  uint64_t own[kBitsInLds / kOneBlock];   // this thread's words, while they are on their way to LDS
   int words, stretch;
   uint32_t* at;          // LDS, kOneBlock
   uint32_t count;
 
-  __device__ __forceinline__ FreePages(const Cache& c, uint32_t* at_, uint32_t* shared) : bits(c.free_bits), words((c.pages + 63) / 64), at(at_) {
+  // load() begins, ready() ends: what is done between the two waits for memory at the same time
+  __device__ __forceinline__ void load(const Cache& c) {
+    bits = c.free_bits;
+    words = (c.pages + 63) / 64;
     stretch = (words + kOneBlock - 1) / kOneBlock;
+    if (words <= kBitsInLds) {
+#pragma unroll
+      for (int k = 0; k < kBitsInLds / kOneBlock; ++k) {
+        const int w = (int)threadIdx.x * stretch + k;
+        own[k] = k < stretch && w < words ? bits[w] : 0;
+      }
+    }
+  }
+  __device__ __forceinline__ void ready(uint64_t* lds /* kBitsInLds */, uint32_t* at_, uint32_t* shared) {
+    at = at_;
     uint32_t n = 0;
-    for (int w = (int)threadIdx.x * stretch; w < min(words, ((int)threadIdx.x + 1) * stretch); ++w) n += (uint32_t)__popcll(bits[w]);
+    if (words <= kBitsInLds) {
+#pragma unroll
+      for (int k = 0; k < kBitsInLds / kOneBlock; ++k) {
+        if (k < stretch) lds[(int)threadIdx.x * stretch + k] = own[k];
+        n += (uint32_t)__popcll(own[k]);
+      }
+      bits = lds;
+    } else {
+      for (int w = (int)threadIdx.x * stretch; w < min(words, ((int)threadIdx.x + 1) * stretch); ++w) n += (uint32_t)__popcll(bits[w]);
+    }
     at[threadIdx.x] = exclusive_sum(n, shared, &count);
     __syncthreads();
   }
-  // the page with `rank` free ones below it (rank < count)
+  // the place in `b` of its set bit with `left` set ones below it
+  static __device__ __forceinline__ int place(uint64_t b, uint32_t left) {
+    int bit = 0;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      const uint32_t low = (uint32_t)__popcll(b >> bit & ((1ull << d) - 1));
+      if (left >= low) { left -= low; bit += d; }
+    }
+    return bit;
+  }
+  // the free page with `rank` free ones below it (rank < count)
   __device__ __forceinline__ int select(uint32_t rank) const {
     int t = 0;
 #pragma unroll
@@ -121,134 +161,210 @@ struct FreePages {
       left -= (uint32_t)__popcll(b);
       b = bits[++w];
     }
-    int bit = 0;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-      const uint32_t low = (uint32_t)__popcll(b >> bit & ((1ull << d) - 1));
-      if (left >= low) { left -= low; bit += d; }
-    }
-    return w * 64 + bit;
+    return w * 64 + place(b, left);
   }
-  // the next one above p (there has to be one)
-  __device__ __forceinline__ int next(int p) const {
-    int w = p >> 6;
-    uint64_t b = (p & 63) == 63 ? 0 : bits[w] & ~0ull << ((p & 63) + 1);
-    while (b == 0) b = bits[++w];
-    return w * 64 + (int)__builtin_ctzll(b);
+  // the page in use with `rank` ones in use below it (there has to be one)
+  __device__ __forceinline__ int select_used(uint32_t rank) const {
+    int t = 0;
+#pragma unroll
+    for (int d = kOneBlock / 2; d > 0; d >>= 1)
+      if ((t + d) * stretch < words && (uint32_t)((t + d) * stretch * 64) - at[t + d] <= rank) t += d;
+    int w = t * stretch;
+    uint32_t left = rank - ((uint32_t)(w * 64) - at[t]);
+    uint64_t b = ~bits[w];
+    while (left >= (uint32_t)__popcll(b)) {
+      left -= (uint32_t)__popcll(b);
+      b = ~bits[++w];
+    }
+    return w * 64 + place(b, left);
+  }
+  // free pages below page p
+  __device__ __forceinline__ uint32_t below(int p) const {
+    const int t = (p >> 6) / stretch;
+    if (p >> 6 >= words) return count;
+    uint32_t n = at[t];
+    for (int w = t * stretch; w < p >> 6; ++w) n += (uint32_t)__popcll(bits[w]);
+    return n + (uint32_t)__popcll(bits[p >> 6] & ((1ull << (p & 63)) - 1));
   }
 };
 
+struct Advance {   // what an entry of an advance call asks for
+  int slot, more, length;
+  uint32_t need;
+  uint8_t said;
+  bool is_slot;
+};
+__device__ __forceinline__ Advance asked(const Cache& c, int n, const int32_t* slots, const int32_t* counts, int count, int i) {
+  Advance e;
+  const bool entry = i < n;
+  e.slot = !entry ? -1 : slots ? slots[i] : i;
+  e.more = !entry ? 0 : counts ? counts[i] : count;
+  e.is_slot = (uint32_t)e.slot < (uint32_t)c.slots;
+  e.length = e.is_slot ? c.length(e.slot) : 0;
+  e.need = 0;
+  e.said = e.slot == -1 || (e.is_slot && e.more >= 0) ? 0 : PGXCACHE_BAD_ENTRY;
+  if (e.is_slot && e.said == 0) {
+    if ((int64_t)e.length + e.more > c.capacity()) e.said = PGXCACHE_FULL;
+    else e.need = (uint32_t)(c.pages_of(e.length + e.more) - c.pages_of(e.length));
+  }
+  return e;
+}
+__device__ __forceinline__ void finish(const Cache& c, const Advance& e, bool done) {
+  if (e.is_slot) c.grown[e.slot] = done ? e.more : 0;
+  if (done && e.more > 0) c.lengths[e.slot] = e.length + e.more;
+}
+__device__ __forceinline__ void take(const Cache& c, int p) {
+  if (c.is_page(p)) atomicAnd((unsigned long long*)&c.free_bits[p >> 6], ~(1ull << (p & 63)));
+}
+
+// Entries kOneBlock * blockIdx.x and on.  ALONE: there are no other blocks, and the call ends here; else advance_apply_kernel follows.
+template <bool ALONE>
 __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, int32_t* plan, uint8_t* status) {
-  __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64];
-  const FreePages free(c, at, shared);
-  uint32_t given = 0;
-  for (int first = 0; first < n; first += kOneBlock) {
-    const int i = first + (int)threadIdx.x;
-    const bool entry = i < n;
-    const int slot = !entry ? -1 : slots ? slots[i] : i;
-    const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
-    const int more = !entry ? 0 : counts ? counts[i] : count;
-    uint8_t said = !entry || slot == -1 ? 0 : !is_slot || more < 0 ? PGXCACHE_BAD_ENTRY : 0;
-    int length = 0;
-    uint32_t need = 0, all;
-    if (is_slot && said == 0) {
-      length = c.length(slot);
-      if ((int64_t)length + more > c.capacity()) said = PGXCACHE_FULL;
-      else need = (uint32_t)(c.pages_of(length + more) - c.pages_of(length));
+  __shared__ uint64_t lds_bits[kBitsInLds];
+  __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64], ends[kOneBlock];
+  __shared__ int32_t row_of[kOneBlock], have_of[kOneBlock];
+  const int tid = (int)threadIdx.x, first = (int)blockIdx.x * kOneBlock, i = first + tid;
+  FreePages free;
+  free.load(c);
+  const Advance e = asked(c, n, slots, counts, count, i);
+  uint32_t before = 0, all;   // needs of the blocks before this one (sums beyond 2^30 are as good as 2^30: no pool has so many pages left)
+  if (!ALONE) {
+    uint64_t sum = 0;
+    for (int k = 0; k < (int)blockIdx.x; ++k) sum += asked(c, n, slots, counts, count, k * kOneBlock + tid).need;
+    exclusive_sum((uint32_t)min(sum, (uint64_t)(1u << 20)), shared, &before);
+  }
+  const uint32_t inside = exclusive_sum(e.need, shared, &all);
+  free.ready(lds_bits, at, shared);
+  const uint32_t rank = before + inside;
+  const uint8_t said = e.need > 0 && (rank > free.count || e.need > free.count - rank) ? PGXCACHE_NO_PAGES : e.said;
+  const bool done = e.is_slot && said == 0;
+  if (status && i < n) status[i] = said;
+  ends[tid] = inside + e.need;
+  row_of[tid] = done ? e.slot : -1;
+  have_of[tid] = c.pages_of(e.length);
+  __syncthreads();
+  // a thread per page, whichever entry it is for
+  int mine = -1;
+  const uint32_t there = before < free.count ? min(all, free.count - before) : 0;
+  for (uint32_t r = (uint32_t)tid; r < there; r += kOneBlock) {
+    int t = 0;   // the entry: the first whose pages end above r
+#pragma unroll
+    for (int d = kOneBlock / 2; d > 0; d >>= 1)
+      if (ends[t + d - 1] <= r) t += d;
+    const int slot = row_of[t];
+    if (slot < 0) continue;
+    const int k = (int)(r - (t > 0 ? ends[t - 1] : 0)), p = free.select(before + r);
+    c.row(slot)[have_of[t] + k] = p;
+    c.refs[p] = 1;
+    if (ALONE) {
+      if (free.bits == lds_bits) take(c, p);   // nobody looks at those in memory any more
+      else mine = p;
     }
-    const uint32_t rank = given + exclusive_sum(need, shared, &all);
-    if (need > 0 && (rank > free.count || need > free.count - rank)) { said = PGXCACHE_NO_PAGES; }
-    given = min(given + min(all, 0x40000000u), 0x40000000u);
-    const bool done = is_slot && said == 0;
-    if (done && need > 0) {
-      int32_t* row = c.row(slot) + c.pages_of(length);
-      int p = free.select(rank);
-      for (uint32_t k = 0;;) {
-        row[k] = p;
-        c.refs[p] = 1;
-        if (++k == need) break;
-        p = free.next(p);
+  }
+  if (ALONE) {
+    finish(c, e, done);
+    if (free.bits != lds_bits) {
+      __syncthreads();
+      if (all <= kOneBlock) {
+        if (mine >= 0) take(c, mine);
+      } else if (done) {
+        for (uint32_t k = 0; k < e.need; ++k) take(c, c.row(e.slot)[c.pages_of(e.length) + (int)k]);
       }
     }
-    if (is_slot) c.grown[slot] = done ? more : 0;
-    if (done && more > 0) c.lengths[slot] = length + more;
-    if (entry) {
-      plan[i] = done ? (int32_t)need : 0;
-      if (status) status[i] = said;
-    }
+  } else if (i < n) {
+    plan[i] = done ? 1 : 0;
   }
-  __syncthreads();   // no one looks at the bits any more
-  for (int i = (int)threadIdx.x; i < n; i += kOneBlock) {
-    const int need = plan[i];
-    if (need == 0) continue;
-    const int slot = slots ? slots[i] : i, have = c.pages_of(c.length(slot));
-    for (int k = have - need; k < have; ++k) {
-      const int p = c.row(slot)[k];
-      atomicAnd((unsigned long long*)&c.free_bits[p >> 6], ~(1ull << (p & 63)));
-    }
-  }
+}
+__global__ void __launch_bounds__(256) advance_apply_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, const int32_t* plan) {
+  const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
+  if (i >= n) return;
+  const Advance e = asked(c, n, slots, counts, count, i);
+  const bool done = plan[i] != 0;
+  if (done)
+    for (uint32_t k = 0; k < e.need; ++k) take(c, c.row(e.slot)[c.pages_of(e.length) + (int)k]);
+  finish(c, e, done);
 }
 
 __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, int32_t* plan, uint8_t* status) {
+  __shared__ uint64_t lds_bits[kBitsInLds];
   __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64];
-  const FreePages free(c, at, shared);
-  uint32_t given = 0;
-  for (int first = 0; first < n; first += kOneBlock) {
-    const int i = first + (int)threadIdx.x;
-    const bool entry = i < n;
-    const int s = entry ? src[i] : -1, d = entry ? dst[i] : -1;
-    const bool out = s == -1 || d == -1, slots = (uint32_t)s < (uint32_t)c.slots && (uint32_t)d < (uint32_t)c.slots;
-    uint8_t said = out || slots ? 0 : PGXCACHE_BAD_ENTRY;
-    const uint32_t need = slots && s != d && (c.length(s) & ((1 << c.page_shift) - 1)) != 0;
-    uint32_t all;
-    const uint32_t rank = given + exclusive_sum(need, shared, &all);
-    given += all;
-    int tail = !slots || s == d ? kSkip : kNoTail;
-    if (need) {
-      if (rank < free.count) tail = free.select(rank);
-      else { tail = kSkip; said = PGXCACHE_NO_PAGES; }
-    }
-    if (entry) {
-      plan[i] = tail;
-      if (status) status[i] = said;
-    }
+  FreePages free;
+  free.load(c);
+  auto look = [&](int i, bool* slots, bool* same) {   // whether the entry needs a page
+    const int s = i < n ? src[i] : -1, d = i < n ? dst[i] : -1;
+    *slots = (uint32_t)s < (uint32_t)c.slots && (uint32_t)d < (uint32_t)c.slots;
+    *same = s == d || s == -1 || d == -1;
+    return *slots && s != d && (c.length(s) & ((1 << c.page_shift) - 1)) != 0;
+  };
+  const int i = (int)blockIdx.x * kOneBlock + (int)threadIdx.x;
+  bool slots, nothing, unused1, unused2;
+  const bool need = look(i, &slots, &nothing);
+  uint32_t before = 0, all;
+  if (blockIdx.x > 0) {
+    uint32_t sum = 0;
+#pragma unroll 4
+    for (int k = 0; k < (int)blockIdx.x; ++k) sum += look(k * kOneBlock + (int)threadIdx.x, &unused1, &unused2);
+    exclusive_sum(sum, shared, &before);
   }
-  __syncthreads();
-  for (int i = (int)threadIdx.x; i < n; i += kOneBlock) {
-    const int p = plan[i];
-    if (p < 0) continue;
-    c.refs[p] = 1;
-    atomicAnd((unsigned long long*)&c.free_bits[p >> 6], ~(1ull << (p & 63)));
+  const uint32_t rank = before + exclusive_sum(need, shared, &all);
+  free.ready(lds_bits, at, shared);
+  uint8_t said = slots || nothing ? 0 : PGXCACHE_BAD_ENTRY;
+  int tail = !slots || nothing ? kSkip : kNoTail;
+  if (need) {
+    if (rank < free.count) tail = free.select(rank);
+    else { tail = kSkip; said = PGXCACHE_NO_PAGES; }
+  }
+  if (i < n) {
+    plan[i] = tail;
+    if (status) status[i] = said;
   }
 }
 
-// a block per entry.  A page that both slots name keeps the source's reference throughout, so none comes free in between.
+// A block per entry, of one wavefront for pages of up to 16 KB (4096 entries whose tails are 8 KB on average: 20.3 us with four wavefronts
+// each, <<FORK_4096>> with one, all of which the machine holds at once) and more for larger ones.  A page that both slots name keeps the
+// source's reference throughout, so none comes free in between.
 __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, const int32_t* plan) {
-  const int i = (int)blockIdx.x, tail = plan[i];
+  const int i = (int)blockIdx.x, tail = plan[i], s = src[i], d = dst[i], tid = (int)threadIdx.x, threads = (int)blockDim.x;
   if (tail == kSkip) return;
-  const int s = src[i], d = dst[i], length = c.length(s), full = length >> c.page_shift;
+  const int length = c.length(s), full = length >> c.page_shift, filled = length & ((1 << c.page_shift) - 1);
   const int old = c.pages_of(c.length(d)), most = max(old, full + (tail >= 0));
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    c.lengths[d] = length;
-    c.grown[d] = 0;
-  }
   const int32_t* from = c.row(s);
   int32_t* to = c.row(d);
-  for (int k = (int)threadIdx.x; k < most; k += 256) {
+  if (tail >= 0 && c.is_page(from[full])) {   // the filled beginning of every head's keys and values
+    const uint32_t units = (uint32_t)(filled * c.head_dim / 8), all = (uint32_t)(c.layers * 2 * c.kv_heads) * units;
+    const uint32_t head = (uint32_t)(c.head_bytes() / 16);
+    const u32x4* a = (const u32x4*)(c.kv + from[full] * c.page_bytes());
+    u32x4* b = (u32x4*)(c.kv + tail * c.page_bytes());
+    constexpr int kAhead = 8;
+    for (uint32_t u = (uint32_t)tid; u < all; u += (uint32_t)threads * kAhead) {
+      u32x4 x[kAhead];
+      uint32_t at[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const uint32_t v = min(u + (uint32_t)(k * threads), all - 1), h = v / units;
+        at[k] = h * head + (v - h * units);
+        x[k] = a[at[k]];
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (u + (uint32_t)(k * threads) < all) b[at[k]] = x[k];
+    }
+  }
+  for (int k = tid; k < most; k += threads) {
     const int now = k < full ? from[k] : k == full && tail >= 0 ? tail : -1;
     if (k < full && c.is_page(now)) atomicAdd(&c.refs[now], 1);
     if (k < old) c.release(to[k]);
     to[k] = now;
   }
-  if (tail < 0 || !c.is_page(from[full])) return;
-  // the filled beginning of every head's keys and values
-  const int64_t head = c.head_bytes();
-  const int units = (length & ((1 << c.page_shift) - 1)) * c.head_dim / 8, lane = (int)threadIdx.x & 63;
-  const char* a = c.kv + from[full] * c.page_bytes();
-  char* b = c.kv + tail * c.page_bytes();
-  for (int h = (int)threadIdx.x >> 6; h < c.layers * 2 * c.kv_heads; h += 4)
-    for (int u = lane; u < units; u += 64) ((u32x4*)(b + h * head))[u] = ((const u32x4*)(a + h * head))[u];
+  __syncthreads();   // everyone has read the old length
+  if (tid == 0) {
+    c.lengths[d] = length;
+    c.grown[d] = 0;
+    if (tail >= 0) {
+      c.refs[tail] = 1;
+      take(c, tail);
+    }
+  }
 }
 
 __global__ void __launch_bounds__(256) free_kernel(Cache c, int n, const int32_t* slots) {
@@ -264,55 +380,35 @@ __global__ void __launch_bounds__(256) free_kernel(Cache c, int n, const int32_t
   }
 }
 
+// a thread per page that moves: the r-th of those in use at and above `used` goes to the r-th free one
 __global__ void __launch_bounds__(kOneBlock) compact_plan_kernel(Cache c, int2* moves, int32_t* moved_to, int32_t* counts, int32_t* used_out) {
+  __shared__ uint64_t lds_bits[kBitsInLds];
   __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64];
-  __shared__ int holes;
-  const FreePages free(c, at, shared);
-  const int used = c.pages - (int)free.count, t = (int)threadIdx.x;
-  const int first = t * free.stretch, last = min(free.words, first + free.stretch);
-  // the free pages below `used`
-  if (threadIdx.x == 0 && used == c.pages) holes = 0;
-  if (used < c.pages && first <= used >> 6 && used >> 6 < last) {
-    uint32_t below = at[t];
-    for (int w = first; w < used >> 6; ++w) below += (uint32_t)__popcll(free.bits[w]);
-    holes = (int)(below + (uint32_t)__popcll(free.bits[used >> 6] & ((1ull << (used & 63)) - 1)));
-  }
-  __syncthreads();
-  const int n = holes;
-  if (t == 0) {
+  FreePages free;
+  free.load(c);
+  free.ready(lds_bits, at, shared);
+  const int used = c.pages - (int)free.count, n = (int)free.below(used);   // as many free pages lie below `used` as pages in use above
+  const int i = (int)blockIdx.x * kOneBlock + (int)threadIdx.x;
+  if (i == 0) {
     counts[0] = used;
     counts[1] = n;
     if (used_out) *used_out = used;
   }
-  // pages in use at and above `used`, in order: the r-th of them goes to the r-th free page
-  uint32_t taken = at[t];          // free pages before the word
-  int to = -1;
-  for (int w = first; w < last; ++w) {
-    const uint64_t b = free.bits[w];
-    const int page = w * 64, inside = min(64, c.pages - page);
-    uint64_t in_use = ~b & (inside == 64 ? ~0ull : (1ull << inside) - 1);
-    if (page < used) in_use &= used - page >= 64 ? 0ull : ~0ull << (used - page);
-    while (in_use) {
-      const int bit = (int)__builtin_ctzll(in_use), p = page + bit;
-      in_use &= in_use - 1;
-      const int below = p - (int)(taken + (uint32_t)__popcll(b & ((1ull << bit) - 1)));   // pages in use below p
-      const int r = below - (used - n);
-      to = to < 0 ? free.select((uint32_t)r) : free.next(to);
-      moves[r] = make_int2(p, to);
-      moved_to[p] = to;
-    }
-    taken += (uint32_t)__popcll(b);
-  }
-  __syncthreads();
-  for (int w = t; w < free.words; w += kOneBlock) {
-    const int page = w * 64, inside = min(64, c.pages - page);
-    const uint64_t there = inside == 64 ? ~0ull : (1ull << inside) - 1;
-    c.free_bits[w] = page + 64 <= used ? 0ull : page >= used ? there : there & ~0ull << (used - page);
+  for (int r = i; r < n; r += (int)gridDim.x * kOneBlock) {
+    const int from = free.select_used((uint32_t)(used - n + r)), to = free.select((uint32_t)r);
+    moves[r] = make_int2(from, to);
+    moved_to[from] = to;
   }
 }
 
 __global__ void __launch_bounds__(256) compact_move_kernel(Cache c, const int2* moves, const int32_t* moved_to, const int32_t* counts) {
   const int used = counts[0], n = counts[1], lane = (int)threadIdx.x & 63;
+  if (n == 0) return;
+  for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < (c.pages + 63) / 64; w += (int64_t)gridDim.x * 256) {
+    const int64_t page = w * 64, inside = min((int64_t)64, c.pages - page);
+    const uint64_t there = inside == 64 ? ~0ull : (1ull << inside) - 1;
+    c.free_bits[w] = page + 64 <= used ? 0ull : page >= used ? there : there & ~0ull << (used - page);
+  }
   for (int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); slot < c.slots; slot += (int64_t)gridDim.x * 4) {
     int32_t* row = c.row((int)slot);
     for (int k = lane, have = c.pages_of(c.length((int)slot)); k < have; k += 64) {
@@ -338,29 +434,39 @@ struct Tokens {   // keys or values of new tokens
   int64_t entry, token, head;   // strides in bytes
 };
 
-// keys and values of one token: [kv_heads][head_dim] each, by 16 bytes
-__device__ __forceinline__ void write_token(const Cache& c, int layer, int page, int inside, const char* k, int64_t k_head, const char* v, int64_t v_head, int from, int step) {
-  const int units = c.head_dim / 8, per = c.kv_heads * units;
-  char* to = c.kv + page * c.page_bytes() + (int64_t)layer * 2 * c.kv_heads * c.head_bytes() + (int64_t)inside * c.head_dim * 2;
-  for (int u = from; u < 2 * per; u += step) {
-    const int value = u >= per, r = value ? u - per : u, head = r / units, at = r % units * 16;
-    const char* x = (value ? v + head * v_head : k + head * k_head) + at;
-    *(u32x4*)(to + (int64_t)(value * c.kv_heads + head) * c.head_bytes() + at) = *(const u32x4_2*)x;
-  }
-}
-
-// a wavefront per token
+// A thread per 16 bytes of a head's key or value and four tokens.
+constexpr int kTokensPerThread = 4;
 __global__ void __launch_bounds__(256) write_kernel(Cache c, int layer, int n, const int32_t* slots, int tokens, Tokens k, Tokens v) {
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (unit >= (int64_t)n * tokens) return;
-  const int i = (int)(unit / tokens), t = (int)(unit % tokens), slot = slots ? slots[i] : i;
+  const uint32_t units = (uint32_t)c.head_dim / 8, per_entry = 2u * (uint32_t)c.kv_heads * units;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t runs = (uint32_t)(tokens + kTokensPerThread - 1) / kTokensPerThread;
+  const int64_t token_run = x / per_entry;
+  const uint32_t u = (uint32_t)(x - token_run * per_entry);
+  if (token_run >= (int64_t)n * runs) return;
+  const int i = (int)(token_run / runs), t0 = (int)(token_run - (int64_t)i * runs) * kTokensPerThread;
+  const int slot = slots ? slots[i] : i;
   if ((uint32_t)slot >= (uint32_t)c.slots) return;
-  const int grown = c.grown[slot], at = c.length(slot) - grown + t;
-  if (t >= grown || at < 0) return;
-  const int page = c.row(slot)[at >> c.page_shift];
-  if (!c.is_page(page)) return;
-  write_token(c, layer, page, at & ((1 << c.page_shift) - 1), k.p + i * k.entry + t * k.token, k.head, v.p + i * v.entry + t * v.token, v.head,
-              (int)threadIdx.x & 63, 64);
+  const int grown = min(c.grown[slot], tokens), first = c.length(slot) - c.grown[slot];
+  if (t0 >= grown || first < 0) return;
+  const uint32_t which = u / units, at = u % units * 16;   // which: keys of all heads, then values
+  const bool value = which >= (uint32_t)c.kv_heads;
+  const uint32_t head = value ? which - (uint32_t)c.kv_heads : which;
+  const Tokens& from = value ? v : k;
+  const char* p = from.p + i * from.entry + head * from.head + at;
+  char* to = c.kv + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes() + at;
+  const int32_t* row = c.row(slot);
+  u32x4 data[kTokensPerThread];
+  int page[kTokensPerThread];
+#pragma unroll
+  for (int j = 0; j < kTokensPerThread; ++j) {
+    const int t = min(t0 + j, grown - 1);
+    data[j] = *(const u32x4_2*)(p + t * from.token);
+    page[j] = row[(first + t) >> c.page_shift];
+  }
+#pragma unroll
+  for (int j = 0; j < kTokensPerThread; ++j)
+    if (t0 + j < grown && c.is_page(page[j]))
+      *(u32x4*)(to + page[j] * c.page_bytes() + (int64_t)((first + t0 + j) & ((1 << c.page_shift) - 1)) * c.head_dim * 2) = data[j];
 }
 
 // ---- attention of one token per entry ------------------------------------------------------------------------------------------------
@@ -773,7 +879,16 @@ int pgxcache_destroy(pgxcache_t h) {
 int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const int32_t* counts_dev, int32_t count, uint8_t* status_dev) {
   if (!list_ok(h, n) || (!counts_dev && count < 0)) return PGXCACHE_EINVAL;
   if (n == 0) return PGXCACHE_OK;
-  hipLaunchKernelGGL(advance_kernel, dim3(1), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, slots_dev, counts_dev, count, h->plan, status_dev);
+  const hipStream_t stream = (hipStream_t)h->o.stream;
+  const Cache c = cache_of(h);
+  if (n <= kOneBlock) {   // one launch
+    hipLaunchKernelGGL((advance_kernel<true>), dim3(1), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
+    HIPCHK(hipGetLastError());
+    return PGXCACHE_OK;
+  }
+  hipLaunchKernelGGL((advance_kernel<false>), dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
+  HIPCHK(hipGetLastError());
+  hipLaunchKernelGGL(advance_apply_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, c, n, slots_dev, counts_dev, count, h->plan);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
@@ -783,7 +898,8 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
   if (!list_ok(h, n) || layer < 0 || layer >= h->o.layers || tokens < 0) return PGXCACHE_EINVAL;
   if (n == 0 || tokens == 0) return PGXCACHE_OK;
   if (!k_dev || !v_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 1u) != 0) return PGXCACHE_EINVAL;
-  const int64_t blocks = ((int64_t)n * tokens + 3) / 4;
+  const int64_t runs = ((int64_t)tokens + kTokensPerThread - 1) / kTokensPerThread;
+  const int64_t blocks = ((int64_t)n * runs * 2 * h->o.kv_heads * (h->o.head_dim / 8) + 255) / 256;
   if (blocks > 0x7FFFFFFF) return PGXCACHE_EINVAL;
   const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};
   hipLaunchKernelGGL(write_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), layer, n, slots_dev, tokens, k, v);
@@ -815,9 +931,10 @@ int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const i
   if (!list_ok(h, n)) return PGXCACHE_EINVAL;
   if (n == 0) return PGXCACHE_OK;
   if (!src_slots_dev || !dst_slots_dev) return PGXCACHE_EINVAL;
-  hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan, status_dev);
+  hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan, status_dev);
   HIPCHK(hipGetLastError());
-  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan);
+  const size_t page = (size_t)h->o.layers * 2 * h->o.kv_heads * h->o.page_size * h->o.head_dim * 2;
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n), dim3(page <= 16384 ? 64 : page <= 32768 ? 128 : 256), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
@@ -832,7 +949,7 @@ int pgxcache_free(pgxcache_t h, int32_t n, const int32_t* slots_dev) {
 
 int pgxcache_compact(pgxcache_t h, int32_t* used_dev) {
   if (!h) return PGXCACHE_EINVAL;
-  hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), h->moves, h->moved_to, h->counts, used_dev);
+  hipLaunchKernelGGL(compact_plan_kernel, dim3(16), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), h->moves, h->moved_to, h->counts, used_dev);
   HIPCHK(hipGetLastError());
   hipLaunchKernelGGL(compact_move_kernel, dim3(2048), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), h->moves, h->moved_to, h->counts);
   HIPCHK(hipGetLastError());
