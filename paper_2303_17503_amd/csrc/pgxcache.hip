@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <new>
+#include <type_traits>
 
 #include "pgxcache.h"
 
@@ -12,6 +13,7 @@ struct pgxcache_ctx {
   void* kv;
   int32_t *table, *lengths, *refs;
   uint64_t* free_bits;     // a bit per page: free; 0 behind the last page
+  uint64_t* taken;         // the same shape: pages given out by a plan and still marked free; 0 between calls
   int32_t* grown;          // [slots] tokens that the slot's last advance made room for
   int32_t* plan;           // [slots] fork: the page for the copy of the last page, kNoTail or kSkip
   int32_t* moved_to;       // [pages] compact: where a page at or above `used` goes
@@ -36,7 +38,8 @@ thread_local int g_last_hip = 0;
 
 constexpr int kOneBlock = 1024;      // threads of the kernels that give out pages
 constexpr int kNoTail = -1, kSkip = -2;
-constexpr int kSplitBlocks = 1024;   // most blocks of an attend call that splits sequences
+constexpr int kSplitBlocks = 512;    // most blocks of an attend call that splits rows
+constexpr int kMostSplits = 128;     // most blocks of one row
 constexpr int kHeads = 16;           // query heads of a matrix tile
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -46,7 +49,7 @@ typedef u32x4 u32x4_2 __attribute__((aligned(2)));
 struct Cache {
   char* kv;
   int32_t *table, *lengths, *refs;
-  uint64_t* free_bits;
+  uint64_t *free_bits, *taken;
   int32_t* grown;
   int32_t slots, pages, width, page_shift, layers, kv_heads, head_dim;
 
@@ -65,7 +68,10 @@ struct Cache {
 __global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arrived) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t free = __ballot(i < c.pages && c.refs[min(i, (int64_t)c.pages - 1)] == 0);
-  if ((threadIdx.x & 63) == 0 && i < ((int64_t)c.pages + 63) / 64 * 64) c.free_bits[i >> 6] = free;
+  if ((threadIdx.x & 63) == 0 && i < ((int64_t)c.pages + 63) / 64 * 64) {
+    c.free_bits[i >> 6] = free;
+    c.taken[i >> 6] = 0;
+  }
   if (i < c.slots) c.grown[i] = 0;
   if (i < kSplitBlocks) arrived[i] = 0;
 }
@@ -75,7 +81,7 @@ __global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arriv
 // needs of the entries before it, and every block of a planning kernel works both out for itself from memory that no one writes
 // meanwhile; a second kernel then takes the pages out of the bits.  Bound by the round trips to memory that depend on each other (the list, the
 // lengths it names; the bits beside them), so the bits are kept in LDS.  4096 entries of a pool of 143000 pages: one block that took the
-// entries 1024 at a time and looked the bits up in memory took 40 us; blocks of 1024 entries side by side take <<FORK_PLAN_4096>>.
+// entries 1024 at a time and looked the bits up in memory took 40 us; blocks of 1024 entries side by side take 7.1 us.
 constexpr int kBitsInLds = 4096;   // words: pools of up to 262144 pages; beyond, the bits are looked up in memory
 
 // sum over the threads before this one; *total: over all
@@ -178,6 +184,22 @@ struct FreePages {
     }
     return w * 64 + place(b, left);
   }
+  // f(word, its bits, those of them with ranks from lo to hi - 1) for the words of this thread's stretch that have such
+  template <class F>
+  __device__ __forceinline__ void ranks(uint32_t lo, uint32_t hi, F&& f) const {
+    uint32_t before = at[threadIdx.x];
+    for (int w = (int)threadIdx.x * stretch; w < min(words, ((int)threadIdx.x + 1) * stretch) && before < hi; ++w) {
+      const uint64_t b = bits[w];
+      const uint32_t n = (uint32_t)__popcll(b);
+      if (before + n > lo) {
+        uint64_t mask = b;
+        if (before < lo) mask &= ~0ull << place(b, lo - before);
+        if (before + n > hi) mask &= (1ull << place(b, hi - before)) - 1;
+        if (mask) f(w, b, mask);
+      }
+      before += n;
+    }
+  }
   // free pages below page p
   __device__ __forceinline__ uint32_t below(int p) const {
     const int t = (p >> 6) / stretch;
@@ -213,17 +235,16 @@ __device__ __forceinline__ void finish(const Cache& c, const Advance& e, bool do
   if (e.is_slot) c.grown[e.slot] = done ? e.more : 0;
   if (done && e.more > 0) c.lengths[e.slot] = e.length + e.more;
 }
-__device__ __forceinline__ void take(const Cache& c, int p) {
-  if (c.is_page(p)) atomicAnd((unsigned long long*)&c.free_bits[p >> 6], ~(1ull << (p & 63)));
-}
-
 // Entries kOneBlock * blockIdx.x and on.  ALONE: there are no other blocks, and the call ends here; else advance_apply_kernel follows.
+// The pages that the entries get are the free ones of consecutive ranks (an entry that cannot have its pages is followed by others that cannot),
+// so they leave the bits a word at a time (4600 pages, taken out one by one: 52 us, now <<ADVANCE_BULK>>).
 template <bool ALONE>
 __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, int32_t* plan, uint8_t* status) {
   __shared__ uint64_t lds_bits[kBitsInLds];
-  __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64], ends[kOneBlock];
+  __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64], ends[kOneBlock], taken_end;
   __shared__ int32_t row_of[kOneBlock], have_of[kOneBlock];
   const int tid = (int)threadIdx.x, first = (int)blockIdx.x * kOneBlock, i = first + tid;
+  if (tid == 0) taken_end = 0;
   FreePages free;
   free.load(c);
   const Advance e = asked(c, n, slots, counts, count, i);
@@ -242,47 +263,39 @@ __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, cons
   ends[tid] = inside + e.need;
   row_of[tid] = done ? e.slot : -1;
   have_of[tid] = c.pages_of(e.length);
+  if (done && e.need > 0) atomicMax(&taken_end, rank + e.need);
   __syncthreads();
   // a thread per page, whichever entry it is for
-  int mine = -1;
-  const uint32_t there = before < free.count ? min(all, free.count - before) : 0;
+  const uint32_t there = taken_end > before ? taken_end - before : 0;
   for (uint32_t r = (uint32_t)tid; r < there; r += kOneBlock) {
     int t = 0;   // the entry: the first whose pages end above r
 #pragma unroll
     for (int d = kOneBlock / 2; d > 0; d >>= 1)
       if (ends[t + d - 1] <= r) t += d;
     const int slot = row_of[t];
-    if (slot < 0) continue;
     const int k = (int)(r - (t > 0 ? ends[t - 1] : 0)), p = free.select(before + r);
     c.row(slot)[have_of[t] + k] = p;
     c.refs[p] = 1;
-    if (ALONE) {
-      if (free.bits == lds_bits) take(c, p);   // nobody looks at those in memory any more
-      else mine = p;
-    }
   }
   if (ALONE) {
     finish(c, e, done);
-    if (free.bits != lds_bits) {
-      __syncthreads();
-      if (all <= kOneBlock) {
-        if (mine >= 0) take(c, mine);
-      } else if (done) {
-        for (uint32_t k = 0; k < e.need; ++k) take(c, c.row(e.slot)[c.pages_of(e.length) + (int)k]);
-      }
-    }
-  } else if (i < n) {
-    plan[i] = done ? 1 : 0;
+    __syncthreads();   // nobody looks at the bits any more
+    free.ranks(before, before + there, [&](int w, uint64_t b, uint64_t mask) { c.free_bits[w] = b & ~mask; });
+  } else {
+    if (i < n) plan[i] = done ? 1 : 0;
+    free.ranks(before, before + there, [&](int w, uint64_t, uint64_t mask) { atomicOr((unsigned long long*)&c.taken[w], mask); });
   }
 }
 __global__ void __launch_bounds__(256) advance_apply_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, const int32_t* plan) {
   const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
-  if (i >= n) return;
-  const Advance e = asked(c, n, slots, counts, count, i);
-  const bool done = plan[i] != 0;
-  if (done)
-    for (uint32_t k = 0; k < e.need; ++k) take(c, c.row(e.slot)[c.pages_of(e.length) + (int)k]);
-  finish(c, e, done);
+  if (i < (c.pages + 63) / 64) {
+    const uint64_t taken = c.taken[i];
+    if (taken) {
+      c.free_bits[i] &= ~taken;
+      c.taken[i] = 0;
+    }
+  }
+  if (i < n) finish(c, asked(c, n, slots, counts, count, i), plan[i] != 0);
 }
 
 __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, int32_t* plan, uint8_t* status) {
@@ -318,13 +331,25 @@ __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, co
     plan[i] = tail;
     if (status) status[i] = said;
   }
+  free.ranks(before, min(before + all, free.count), [&](int w, uint64_t, uint64_t mask) { atomicOr((unsigned long long*)&c.taken[w], mask); });
 }
 
 // A block per entry, of one wavefront for pages of up to 16 KB (4096 entries whose tails are 8 KB on average: 20.3 us with four wavefronts
-// each, <<FORK_4096>> with one, all of which the machine holds at once) and more for larger ones.  A page that both slots name keeps the
+// each, 17.9 us with one, all of which the machine holds at once) and more for larger ones.  A page that both slots name keeps the
 // source's reference throughout, so none comes free in between.
 __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, const int32_t* plan) {
-  const int i = (int)blockIdx.x, tail = plan[i], s = src[i], d = dst[i], tid = (int)threadIdx.x, threads = (int)blockDim.x;
+  const int tid = (int)threadIdx.x, threads = (int)blockDim.x;
+  if ((int)blockIdx.x >= n) {   // the blocks behind the entries' take the plan's pages out of the bits
+    const int w = ((int)blockIdx.x - n) * threads + tid;
+    if (w >= (c.pages + 63) / 64) return;
+    const uint64_t taken = c.taken[w];
+    if (taken) {
+      atomicAnd((unsigned long long*)&c.free_bits[w], ~taken);
+      c.taken[w] = 0;
+    }
+    return;
+  }
+  const int i = (int)blockIdx.x, tail = plan[i], s = src[i], d = dst[i];
   if (tail == kSkip) return;
   const int length = c.length(s), full = length >> c.page_shift, filled = length & ((1 << c.page_shift) - 1);
   const int old = c.pages_of(c.length(d)), most = max(old, full + (tail >= 0));
@@ -360,10 +385,7 @@ __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const int32_t
   if (tid == 0) {
     c.lengths[d] = length;
     c.grown[d] = 0;
-    if (tail >= 0) {
-      c.refs[tail] = 1;
-      take(c, tail);
-    }
+    if (tail >= 0) c.refs[tail] = 1;
   }
 }
 
@@ -520,31 +542,39 @@ __device__ __forceinline__ float across_groups_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// What one block leaves for another of the same launch goes through the dies' L2 caches, which do not know of each other, without
+// writing back or dropping anything else in them: a device-wide fence per block instead cost 20 us each (3 sequences of 110000
+// tokens: 282 -> 250 us).
+constexpr int kAcrossDies = 16;             // cache policy of a buffer instruction: as an atomic access of the whole device (sc1)
+constexpr int kBufferFlags = 0x00027000;    // raw buffer of 32-bit words
+
 template <int NT>
 struct Tile {   // 32 tokens: keys [half][32-element part], values [token][dword]
   u32x4 k[2][NT];
   uint32_t v[8][NT];
 };
 
-// W wavefronts share a row (an entry and a key head); with W = 4 a row may also be split over blocks
+// W wavefronts share a row (an entry and a key head); with four a row may also be split over blocks
 template <class T, int NT, int W>
-__global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
+__global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c, AttendArgs a) {
   typedef typename T::x8 x8;
   constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
-  __shared__ float joined_m[4][kHeads], joined_l[4][kHeads];
-  extern __shared__ float joined_o[];   // W = 4: [3][kHeads][D]
+  __shared__ float joined_m[W][kHeads], joined_l[W][kHeads];
+  extern __shared__ float joined_o[];   // [W - 1][kHeads][D]
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const int64_t unit = W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x / a.splits;
-  const int split = W == 1 ? 0 : (int)(blockIdx.x % a.splits);
-  if (W == 1 && unit >= (int64_t)a.n * c.kv_heads * a.head_tiles) return;
-  const int head_tile = (int)(unit % a.head_tiles), kv_head = (int)(unit / a.head_tiles % c.kv_heads), i = (int)(unit / a.head_tiles / c.kv_heads);
+  // head tiles and key heads are next to each other in the launch, then the parts of a sequence: what runs together reads neighbouring memory
+  const uint32_t place = blockIdx.x, per_part = (uint32_t)(c.kv_heads * a.head_tiles);
+  const uint32_t part = place / per_part, in_part = place - part * per_part;
+  const int i = (int)(part / (uint32_t)a.splits), split = (int)(part - (uint32_t)i * (uint32_t)a.splits);
+  const int kv_head = (int)(in_part / (uint32_t)a.head_tiles), head_tile = (int)(in_part - (uint32_t)(kv_head * a.head_tiles));
+  const uint32_t unit = (uint32_t)i * per_part + in_part;
   const int slot = a.slots ? a.slots[i] : i;
   const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
   const int length = is_slot ? c.length(slot) : 0;
   const int first_head = head_tile * kHeads, heads_here = min(kHeads, a.group - first_head), head0 = kv_head * a.group + first_head;
 
   if (length == 0) {   // nothing to attend to
-    if (split == 0 && (W == 1 || wave == 0) && col < heads_here) {
+    if (split == 0 && wave == 0 && col < heads_here) {
       char* out = a.out + i * a.out_entry + (head0 + col) * a.out_head + g * kOut * 2;
 #pragma unroll
       for (int u = 0; u < NT; ++u) *(u32x4_2*)(out + u * 16) = u32x4{0, 0, 0, 0};
@@ -563,16 +593,19 @@ __global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
   const char* values = keys + c.kv_heads * head_bytes;
   const int in_page = (1 << c.page_shift) - 1;
 
+  const bool alone = W > 1 && tiles <= 1;   // nothing to share: the first wavefront goes on by itself
+  if (alone && wave > 0) return;
+
   // the new token's key and value go into the cache first, by the block that reads the last tile
   if (a.k && end == tiles && c.grown[slot] > 0) {
     const int at = length - 1, page = row[at >> c.page_shift];
-    if ((W == 1 || wave == 0) && c.is_page(page) && lane < 2 * D / 8) {
+    if (wave == 0 && c.is_page(page) && lane < 2 * D / 8) {
       const int u = lane % (D / 8) * 16;
       const char* x = lane < D / 8 ? a.k + i * a.k_entry + kv_head * a.k_head : a.v + i * a.v_entry + kv_head * a.v_head;
       *(u32x4*)((char*)(lane < D / 8 ? keys : values) + page * page_bytes + (int64_t)(at & in_page) * D * 2 + u) = *(const u32x4_2*)(x + u);
     }
     // (a wavefront's own memory operations are in order; other wavefronts wait)
-    if (W > 1) __syncthreads();
+    if (W > 1 && !alone) __syncthreads();
     else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
@@ -595,7 +628,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
   int ids = 0;   // page of half-tile lane & 1 of the wavefront's tile number (a multiple of 32) + lane / 2
   const int last_half = (length - 1) >> 4;
   auto load = [&](Tile<NT>& t, int number) {   // the wavefront's tile of that number
-    const int tile = begin + wave % W + number * W;
+    const int tile = begin + wave + number * W;
     if ((number & 31) == 0) {
       const int half = min((tile + (lane >> 1) * W) * 2 + (lane & 1), last_half);
       const int p = row[(half << 4) >> c.page_shift];
@@ -614,8 +647,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
         for (int w = 0; w < NT; ++w) t.v[h * 4 + j][w] = ((const uint32_t*)(v + j * D * 2))[w];
     }
   };
-  auto compute = [&](Tile<NT>& t, int number) {
-    const int tile = begin + wave % W + number * W;
+  auto compute = [&](Tile<NT>& t, int number, auto last) {
     f32x4 s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -624,16 +656,17 @@ __global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
       for (int m = 0; m < NT; ++m) s[h] = T::mfma(__builtin_bit_cast(x8, t.k[h][m]), q[m], s[h]);
       s[h] *= a.scale;
     }
-    if (tile * 32 + 32 > length) {   // tokens behind the last: no score, and their values may hold anything
+    if (last.value) {   // tokens behind the sequence's last: no score, and their values may hold anything
+      const int first = (begin + wave + number * W) * 32 + g * 4;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (tile * 32 + h * 16 + g * 4 + r >= length) {
-            s[h][r] = -INFINITY;
+        for (int r = 0; r < 4; ++r) {
+          const bool there = first + h * 16 + r < length;
+          s[h][r] = there ? s[h][r] : -INFINITY;
 #pragma unroll
-            for (int w = 0; w < NT; ++w) t.v[h * 4 + r][w] = 0;
-          }
+          for (int w = 0; w < NT; ++w) t.v[h * 4 + r][w] = there ? t.v[h * 4 + r][w] : 0;
+        }
     }
     float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     if (__any(most > top + kSlack)) {
@@ -662,21 +695,30 @@ __global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
       acc[m] = T::mfma(__builtin_bit_cast(x8, x), low, acc[m]);
     }
   };
-  const int mine = (end - begin - wave % W + W - 1) / W;   // this wavefront's tiles
-  if (mine > 0) {
+  const int mine = (end - begin - wave + W - 1) / W;   // this wavefront's tiles
+  if (mine > 0) {   // the next tile is under way while one is computed (without a condition: the waits for memory are counted, not complete)
+    constexpr std::false_type inner{};
+    constexpr std::true_type outer{};
     Tile<NT> t0, t1;
     load(t0, 0);
-    for (int number = 0; number < mine; number += 2) {   // the next tile is under way while this one is computed
-      if (number + 1 < mine) load(t1, number + 1);
-      compute(t0, number);
-      if (number + 1 >= mine) break;
-      if (number + 2 < mine) load(t0, number + 2);
-      compute(t1, number + 1);
+    int number = 0;
+    for (; number + 2 < mine; number += 2) {
+      load(t1, number + 1);
+      compute(t0, number, inner);
+      load(t0, number + 2);
+      compute(t1, number + 1, inner);
+    }
+    if (number + 1 < mine) {
+      load(t1, number + 1);
+      compute(t0, number, inner);
+      compute(t1, number + 1, outer);
+    } else {
+      compute(t0, number, outer);
     }
   }
   sum = across_groups_sum(sum);
 
-  if (W > 1) {   // the four wavefronts' parts, into the first's registers
+  if (W > 1 && !alone) {   // the wavefronts' parts, into the first's registers
     if (g == 0) { joined_m[wave][col] = top; joined_l[wave][col] = sum; }
     __syncthreads();
     float now = -INFINITY;
@@ -706,8 +748,8 @@ __global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
     }
   }
 
-  if (W == 1 || active == 1) {
-    if (W > 1 && wave > 0) return;
+  if (active == 1) {
+    if (wave > 0) return;
     if (col >= heads_here) return;
     const float inverse = 1.0f / sum;
     char* out = a.out + i * a.out_entry + (head0 + col) * a.out_head + g * kOut * 2;
@@ -722,70 +764,136 @@ __global__ void __launch_bounds__(256) attend_kernel(Cache c, AttendArgs a) {
     return;
   }
 
-  // The row is split over `active` blocks: each leaves its part in memory, and the one that comes last joins them, in their order.
-  constexpr int kPart = kHeads * (D + 2);
-  float* parts = a.partial + unit * a.splits * kPart;
-  if (wave == 0 && col < heads_here) {
-    float* p = parts + (int64_t)split * kPart;
-    if (g == 0) { p[col] = top; p[kHeads + col] = sum; }
-    float* o = p + 2 * kHeads + col * D + g * kOut;
+  // The row is split over `active` blocks: each leaves its part in memory, and the one that comes last joins them, in an order of its own.
+  // All its loads are of 16 bytes and under way together: with 4-byte ones, one output each, joining 256 parts of 8 heads of 128 took 40 us.
+  if constexpr (W >= 4) {
+    constexpr int kPart = kHeads * (D + 2), kThreads = 64 * W, kPer = kMostSplits / (4 * W), kJoin = NT < 8 ? 16 : 8;
+    const uint32_t part_bytes = kPart * 4;
+    float* parts = a.partial + (int64_t)unit * a.splits * kPart;
+    const auto memory = __builtin_amdgcn_make_buffer_rsrc(parts, 0, a.splits * part_bytes, kBufferFlags);
+    if (wave == 0 && col < heads_here) {
+      const uint32_t at = (uint32_t)split * part_bytes;
+      if (g == 0) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(top), memory, at + col * 4, 0, kAcrossDies);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), memory, at + (kHeads + col) * 4, 0, kAcrossDies);
+      }
 #pragma unroll
-    for (int u = 0; u < kOut / 4; ++u) {
-      f32x4 x;
+      for (int u = 0; u < kOut / 4; ++u) {
+        f32x4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = acc[(u * 4 + e) % (2 * NT)][(u * 4 + e) / (2 * NT)];
-      *(f32x4_4*)(o + u * 4) = x;
+        for (int e = 0; e < 4; ++e) x[e] = acc[(u * 4 + e) % (2 * NT)][(u * 4 + e) / (2 * NT)];
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), memory, at + (2 * kHeads + col * D + g * kOut + u * 4) * 4, 0, kAcrossDies);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // they are where every die sees them
     }
-    __threadfence();
-  }
-  __shared__ int is_last;
-  __syncthreads();
-  if (threadIdx.x == 0) is_last = atomicAdd(&a.arrived[unit], 1u) == (uint32_t)active - 1u;
-  __syncthreads();
-  if (!is_last) return;
-  __threadfence();
-  if (threadIdx.x == 0) a.arrived[unit] = 0;
-  float* weights = joined_o;   // [active][kHeads], active <= 256
-  for (int h = wave; h < heads_here; h += 4) {
-    float m = -INFINITY;
-    for (int s = lane; s < active; s += 64) m = fmaxf(m, parts[(int64_t)s * kPart + h]);
+    __shared__ int is_last;
+    __syncthreads();
+    if (threadIdx.x == 0) is_last = atomicAdd(&a.arrived[unit], 1u) == (uint32_t)active - 1u;
+    __syncthreads();
+    if (!is_last) return;
+    if (threadIdx.x == 0) a.arrived[unit] = 0;
+
+    // lane 16 g + c of wavefront w: head c of parts 4 (w + W k) + g
+    float tops[kPer], sums[kPer];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    for (int k = 0; k < kPer; ++k) {
+      const int s = min(4 * (wave + W * k) + g, active - 1);
+      tops[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(memory, s * part_bytes + col * 4, 0, kAcrossDies));
+      sums[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(memory, s * part_bytes + (kHeads + col) * 4, 0, kAcrossDies));
+    }
+    // an output of four elements per thread; where there are fewer than threads, several share one
+    const int outputs = heads_here * D / 4, sharers = max(1, kThreads / outputs);
+    const int e0 = (int)threadIdx.x % (outputs * sharers) % outputs, sharer = (int)threadIdx.x / outputs;
+    u32x4 next[kJoin];
+    auto fetch = [&](int e, int first) {
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k)
+        next[k] = __builtin_amdgcn_raw_buffer_load_b128(memory, min(first + k * sharers, active - 1) * part_bytes + (2 * kHeads + e * 4) * 4, 0, kAcrossDies);
+    };
+    fetch(e0, sharer);
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) m = fmaxf(m, tops[k]);
+    m = across_groups_max(m);
+    if (g == 0) joined_m[wave][col] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, joined_m[w][col]);
     const float from = m > -INFINITY ? m : 0.0f;
-    float l = 0.0f;
-    for (int s = lane; s < active; s += 64) l += parts[(int64_t)s * kPart + kHeads + h] * __builtin_amdgcn_exp2f(parts[(int64_t)s * kPart + h] - from);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+    for (int k = 0; k < kPer; ++k) {
+      tops[k] = 4 * (wave + W * k) + g < active ? __builtin_amdgcn_exp2f(tops[k] - from) : 0.0f;
+      l += sums[k] * tops[k];
+    }
+    l = across_groups_sum(l);
+    if (g == 0) joined_l[wave][col] = l;
+    __syncthreads();
+    l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) l += joined_l[w][col];
     const float inverse = 1.0f / l;
-    for (int s = lane; s < active; s += 64) weights[s * kHeads + h] = __builtin_amdgcn_exp2f(parts[(int64_t)s * kPart + h] - from) * inverse;
-    if (a.lse && lane == 0) a.lse[(int64_t)i * a.heads + head0 + h] = (m + __log2f(l)) * kLn2;
-  }
-  __syncthreads();
-  for (int e = (int)threadIdx.x; e < heads_here * D; e += 256) {
-    const int h = e / D, d = e % D;
-    const float* o = parts + 2 * kHeads + e;
-    float x = 0.0f;
-#pragma unroll 8
-    for (int s = 0; s < active; ++s) x += weights[s * kHeads + h] * o[(int64_t)s * kPart];
-    ((typename T::elem*)(a.out + i * a.out_entry + (head0 + h) * a.out_head))[d] = (typename T::elem)x;
+    float* weights = joined_o;   // [kMostSplits][kHeads]
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) weights[(4 * (wave + W * k) + g) * kHeads + col] = tops[k] * inverse;
+    if (a.lse && wave == 0 && g == 0 && col < heads_here) a.lse[(int64_t)i * a.heads + head0 + col] = (m + __log2f(l)) * kLn2;
+    __syncthreads();
+    f32x4* shared_out = (f32x4*)(joined_o + kMostSplits * kHeads);   // [kThreads]
+    if (sharers == 1 && sharer > 0) return;   // threads left over
+    for (int e = e0; e < outputs; e += kThreads) {
+      const int h = e * 4 / D;
+      f32x4 x = {0, 0, 0, 0};
+      if (sharer < sharers) {
+        for (int s = sharer;;) {
+#pragma unroll
+          for (int k = 0; k < kJoin; ++k) {
+            const int at = s + k * sharers;
+            const float w = at < active ? weights[at * kHeads + h] : 0.0f;
+            x += at < active ? __builtin_bit_cast(f32x4, next[k]) * w : f32x4{0, 0, 0, 0};
+          }
+          s += kJoin * sharers;
+          if (s >= active) break;
+          fetch(e, s);
+        }
+      }
+      if (sharers > 1) {   // (then this loop has one turn)
+        shared_out[threadIdx.x] = x;
+        __syncthreads();
+        if (sharer > 0) return;
+        for (int k = 1; k < sharers; ++k) x += shared_out[threadIdx.x + k * outputs];
+      } else if (e + kThreads < outputs) {
+        fetch(e + kThreads, sharer);
+      }
+      typename T::elem* out = (typename T::elem*)(a.out + i * a.out_entry + (head0 + h) * a.out_head) + e * 4 % D;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) out[k] = (typename T::elem)x[k];
+    }
   }
 }
 
+template <class T, int NT, int W>
+hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t rows, hipStream_t stream) {
+  const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = a.splits > 1 ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
+  hipLaunchKernelGGL((attend_kernel<T, NT, W>), dim3((unsigned)(rows * a.splits)), dim3(64 * W), join > weights ? join : weights, stream, c, a);
+  return hipGetLastError();
+}
 template <class T, int NT>
 hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles;
-  // enough rows to give every wavefront slot of the machine one: a wavefront each; else four, and long rows are split over blocks
-  if (rows >= 4096) {
-    a.splits = 1;
-    hipLaunchKernelGGL((attend_kernel<T, NT, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, c, a);
-  } else {
-    const int64_t most_tiles = ((int64_t)c.width << c.page_shift) / 32 + 1, spread = kSplitBlocks / rows;
-    int64_t splits = spread < (most_tiles + 3) / 4 ? spread : (most_tiles + 3) / 4;
-    a.splits = (int32_t)(splits < 1 ? 1 : splits > 256 ? 256 : splits);
-    const size_t join = (size_t)3 * kHeads * NT * 32 * 4, weights = (size_t)a.splits * kHeads * 4;
-    hipLaunchKernelGGL((attend_kernel<T, NT, 4>), dim3((unsigned)(rows * a.splits)), dim3(256), join > weights ? join : weights, stream, c, a);
+  // The lengths are known on the device only, so the choice goes by how long a slot can be.
+  //  * Short ones and many rows: a wavefront each (1024 slots of 1 to 160 tokens, 2 key heads of 64: 10.3 us, with four 11.9; 4096 of 1 to 160
+  //    30.5 / 34.2). Longer ones: four (1024 of 1 to 722 tokens 37.8 / 33.3, 4096 147 / 139; one of 722 12.4 / 7.0; eight are slower throughout: 7.5).
+  //  * Few rows that can be longer than 32 tiles are split over blocks, 8 tiles to each if all tiles are there (one sequence of 722
+  //    tokens: 7.0 us in one block, 8.3 split; of 2048: 12.2 in two blocks, 8.5 in eight; of 8192: 12.5 in eight, 9.1 in 32), as long as the machine's 256
+  //    compute units have two blocks each at most (3 x 8 rows of 110000 tokens of 128 elements: 232 us with 504 blocks, 238 with 1008, 252 with 2016).
+  //    Beyond 128 parts the joining costs more than the reading (one of 131072 tokens: 29.3 us in 128 parts, 40.4 in 256).
+  const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles, most_tiles = (((int64_t)c.width << c.page_shift) + 31) / 32;
+  a.splits = 1;
+  if (most_tiles <= 8 && rows >= 1024) return launch_attend_by<T, NT, 1>(c, a, rows, stream);
+  if (most_tiles > 32) {
+    const int64_t spread = kSplitBlocks / rows, useful = (most_tiles + 7) / 8;
+    const int64_t splits = spread < useful ? spread : useful;
+    a.splits = (int32_t)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
   }
-  return hipGetLastError();
+  return launch_attend_by<T, NT, 4>(c, a, rows, stream);
 }
 template <class T>
 hipError_t launch_attend_for(const Cache& c, const AttendArgs& a, hipStream_t stream) {
@@ -808,13 +916,14 @@ bool opts_ok(const pgxcache_opts* o) {
 }
 
 struct Layout {
-  size_t free_bits, grown, plan, moved_to, moves, counts, arrived, partial, total;
+  size_t free_bits, taken, grown, plan, moved_to, moves, counts, arrived, partial, total;
 };
 Layout layout(const pgxcache_opts& o) {
   Layout l;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
   l.free_bits = take(((size_t)o.pages + 63) / 64 * 8);
+  l.taken = take(((size_t)o.pages + 63) / 64 * 8);
   l.grown = take((size_t)o.slots * 4);
   l.plan = take((size_t)o.slots * 4);
   l.moved_to = take((size_t)o.pages * 4);
@@ -828,7 +937,7 @@ Layout layout(const pgxcache_opts& o) {
 
 Cache cache_of(pgxcache_t h) {
   Cache c;
-  c.kv = (char*)h->kv; c.table = h->table; c.lengths = h->lengths; c.refs = h->refs; c.free_bits = h->free_bits; c.grown = h->grown;
+  c.kv = (char*)h->kv; c.table = h->table; c.lengths = h->lengths; c.refs = h->refs; c.free_bits = h->free_bits; c.taken = h->taken; c.grown = h->grown;
   c.slots = h->o.slots; c.pages = h->o.pages; c.width = h->o.width; c.page_shift = __builtin_ctz((unsigned)h->o.page_size);
   c.layers = h->o.layers; c.kv_heads = h->o.kv_heads; c.head_dim = h->o.head_dim;
   return c;
@@ -861,7 +970,7 @@ int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int3
   char* w = (char*)work_dev;
   h->o = *opts;
   h->kv = kv_dev; h->table = table_dev; h->lengths = lengths_dev; h->refs = refs_dev;
-  h->free_bits = (uint64_t*)(w + l.free_bits); h->grown = (int32_t*)(w + l.grown); h->plan = (int32_t*)(w + l.plan);
+  h->free_bits = (uint64_t*)(w + l.free_bits); h->taken = (uint64_t*)(w + l.taken); h->grown = (int32_t*)(w + l.grown); h->plan = (int32_t*)(w + l.plan);
   h->moved_to = (int32_t*)(w + l.moved_to); h->moves = (int2*)(w + l.moves); h->counts = (int32_t*)(w + l.counts);
   h->arrived = (uint32_t*)(w + l.arrived); h->partial = (float*)(w + l.partial);
   const int rc = pgxcache_rescan(h);
@@ -888,7 +997,8 @@ int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const in
   }
   hipLaunchKernelGGL((advance_kernel<false>), dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
   HIPCHK(hipGetLastError());
-  hipLaunchKernelGGL(advance_apply_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, c, n, slots_dev, counts_dev, count, h->plan);
+  const int words = (c.pages + 63) / 64, threads = n > words ? n : words;
+  hipLaunchKernelGGL(advance_apply_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, c, n, slots_dev, counts_dev, count, h->plan);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
@@ -934,7 +1044,8 @@ int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const i
   hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan, status_dev);
   HIPCHK(hipGetLastError());
   const size_t page = (size_t)h->o.layers * 2 * h->o.kv_heads * h->o.page_size * h->o.head_dim * 2;
-  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n), dim3(page <= 16384 ? 64 : page <= 32768 ? 128 : 256), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan);
+  const int threads = page <= 16384 ? 64 : page <= 32768 ? 128 : 256, words = (h->o.pages + 63) / 64;
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)(n + (words + threads - 1) / threads)), dim3((unsigned)threads), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
