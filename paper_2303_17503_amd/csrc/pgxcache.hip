@@ -8,6 +8,15 @@
 
 #include "pgxcache.h"
 
+constexpr int kNoTail = -1, kSkip = -2;
+struct __attribute__((aligned(16))) pgxcache_fork_entry {   // an entry of a fork call as its plan leaves it, so that the copying starts after one look at memory
+  int32_t tail;            // the page for the copy of the last page, kNoTail or kSkip
+  int32_t src, dst, length;
+  int32_t last;            // the source's partly filled last page
+  int32_t old;             // pages of the destination
+  int32_t unused[2];
+};
+
 struct pgxcache_ctx {
   pgxcache_opts o;
   void* kv;
@@ -15,7 +24,8 @@ struct pgxcache_ctx {
   uint64_t* free_bits;     // a bit per page: free; 0 behind the last page
   uint64_t* taken;         // the same shape: pages given out by a plan and still marked free; 0 between calls
   int32_t* grown;          // [slots] tokens that the slot's last advance made room for
-  int32_t* plan;           // [slots] fork: the page for the copy of the last page, kNoTail or kSkip
+  int32_t* plan;           // [slots] advance: whether the entry is done
+  pgxcache_fork_entry* forks;   // [slots] what fork does with its entries
   int32_t* moved_to;       // [pages] compact: where a page at or above `used` goes
   int2* moves;             // [pages] compact: (from, to)
   int32_t* counts;         // compact: used, number of moves
@@ -37,7 +47,7 @@ thread_local int g_last_hip = 0;
   } while (0)
 
 constexpr int kOneBlock = 1024;      // threads of the kernels that give out pages
-constexpr int kNoTail = -1, kSkip = -2;
+typedef pgxcache_fork_entry ForkEntry;
 constexpr int kSplitBlocks = 512;    // most blocks of an attend call that splits rows
 constexpr int kMostSplits = 128;     // most blocks of one row
 constexpr int kHeads = 16;           // query heads of a matrix tile
@@ -60,8 +70,31 @@ struct Cache {
   __device__ __forceinline__ bool is_page(int p) const { return (uint32_t)p < (uint32_t)pages; }
   __device__ __forceinline__ int64_t head_bytes() const { return ((int64_t)head_dim << page_shift) * 2; }      // one head's keys or values of a page
   __device__ __forceinline__ int64_t page_bytes() const { return head_bytes() * kv_heads * 2 * layers; }
-  __device__ __forceinline__ void release(int p) const {   // one table entry less names the page
-    if (is_page(p) && atomicSub(&refs[p], 1) == 1) atomicOr((unsigned long long*)&free_bits[p >> 6], 1ull << (p & 63));
+};
+
+// Pages that come free in a block.  Those of one word of the bits are gathered in LDS, so that a word is written once: pages given out together
+// often come free together, and 64 blocks that each add one to the same word take 4 us.
+struct Freed {
+  static constexpr int kWords = 64;
+  int key[kWords];
+  unsigned long long mask[kWords];
+  __device__ __forceinline__ void begin() {
+    if (threadIdx.x < kWords) {
+      key[threadIdx.x] = -1;
+      mask[threadIdx.x] = 0;
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ void release(const Cache& c, int p) {   // one table entry less names the page
+    if (!c.is_page(p) || atomicSub(&c.refs[p], 1) != 1) return;
+    const int w = p >> 6, k = w % kWords;
+    const int was = atomicCAS(&key[k], -1, w);
+    if (was == -1 || was == w) atomicOr(&mask[k], 1ull << (p & 63));
+    else atomicOr((unsigned long long*)&c.free_bits[w], 1ull << (p & 63));
+  }
+  __device__ __forceinline__ void end(const Cache& c) {
+    __syncthreads();
+    if (threadIdx.x < kWords && mask[threadIdx.x]) atomicOr((unsigned long long*)&c.free_bits[key[threadIdx.x]], mask[threadIdx.x]);
   }
 };
 
@@ -218,11 +251,13 @@ struct Advance {   // what an entry of an advance call asks for
 };
 __device__ __forceinline__ Advance asked(const Cache& c, int n, const int32_t* slots, const int32_t* counts, int count, int i) {
   Advance e;
-  const bool entry = i < n;
-  e.slot = !entry ? -1 : slots ? slots[i] : i;
-  e.more = !entry ? 0 : counts ? counts[i] : count;
-  e.is_slot = (uint32_t)e.slot < (uint32_t)c.slots;
-  e.length = e.is_slot ? c.length(e.slot) : 0;
+  const bool entry = i < n;   // (loads without a condition: those of several entries are then under way together)
+  const int at = min(i, n - 1);
+  e.slot = slots ? slots[at] : at;
+  e.more = counts ? counts[at] : count;
+  e.is_slot = entry && (uint32_t)e.slot < (uint32_t)c.slots;
+  e.length = c.length(e.is_slot ? e.slot : 0);
+  if (!entry) e.slot = -1;
   e.need = 0;
   e.said = e.slot == -1 || (e.is_slot && e.more >= 0) ? 0 : PGXCACHE_BAD_ENTRY;
   if (e.is_slot && e.said == 0) {
@@ -235,56 +270,78 @@ __device__ __forceinline__ void finish(const Cache& c, const Advance& e, bool do
   if (e.is_slot) c.grown[e.slot] = done ? e.more : 0;
   if (done && e.more > 0) c.lengths[e.slot] = e.length + e.more;
 }
-// Entries kOneBlock * blockIdx.x and on.  ALONE: there are no other blocks, and the call ends here; else advance_apply_kernel follows.
+// PER = 1: a block per kOneBlock entries; one block ends the call itself, more are followed by advance_apply_kernel.  PER > 1: one block, PER
+// neighbouring entries per thread, all their loads under way together (4096 entries: <<ADVANCE_TILES>> us, by the two kernels 9.1 + 4.1).
 // The pages that the entries get are the free ones of consecutive ranks (an entry that cannot have its pages is followed by others that cannot),
-// so they leave the bits a word at a time (4600 pages, taken out one by one: 52 us, now <<ADVANCE_BULK>>).
-template <bool ALONE>
+// so they leave the bits a word at a time (4600 pages, taken out one by one: 52 us, now 12).
+template <int PER, bool ALONE>
 __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, int32_t* plan, uint8_t* status) {
   __shared__ uint64_t lds_bits[kBitsInLds];
   __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64], ends[kOneBlock], taken_end;
   __shared__ int32_t row_of[kOneBlock], have_of[kOneBlock];
-  const int tid = (int)threadIdx.x, first = (int)blockIdx.x * kOneBlock, i = first + tid;
+  const int tid = (int)threadIdx.x, first = ALONE ? 0 : (int)blockIdx.x * kOneBlock;
   if (tid == 0) taken_end = 0;
   FreePages free;
   free.load(c);
-  const Advance e = asked(c, n, slots, counts, count, i);
-  uint32_t before = 0, all;   // needs of the blocks before this one (sums beyond 2^30 are as good as 2^30: no pool has so many pages left)
+  Advance e[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) e[k] = asked(c, n, slots, counts, count, first + tid * PER + k);
+  // needs of the entries before (sums beyond 2^30 are as good as 2^30: no pool has so many pages left)
+  uint32_t before = 0, all, mine = 0;
   if (!ALONE) {
     uint64_t sum = 0;
     for (int k = 0; k < (int)blockIdx.x; ++k) sum += asked(c, n, slots, counts, count, k * kOneBlock + tid).need;
     exclusive_sum((uint32_t)min(sum, (uint64_t)(1u << 20)), shared, &before);
   }
-  const uint32_t inside = exclusive_sum(e.need, shared, &all);
-  free.ready(lds_bits, at, shared);
-  const uint32_t rank = before + inside;
-  const uint8_t said = e.need > 0 && (rank > free.count || e.need > free.count - rank) ? PGXCACHE_NO_PAGES : e.said;
-  const bool done = e.is_slot && said == 0;
-  if (status && i < n) status[i] = said;
-  ends[tid] = inside + e.need;
-  row_of[tid] = done ? e.slot : -1;
-  have_of[tid] = c.pages_of(e.length);
-  if (done && e.need > 0) atomicMax(&taken_end, rank + e.need);
-  __syncthreads();
-  // a thread per page, whichever entry it is for
-  const uint32_t there = taken_end > before ? taken_end - before : 0;
-  for (uint32_t r = (uint32_t)tid; r < there; r += kOneBlock) {
-    int t = 0;   // the entry: the first whose pages end above r
 #pragma unroll
-    for (int d = kOneBlock / 2; d > 0; d >>= 1)
-      if (ends[t + d - 1] <= r) t += d;
-    const int slot = row_of[t];
-    const int k = (int)(r - (t > 0 ? ends[t - 1] : 0)), p = free.select(before + r);
-    c.row(slot)[have_of[t] + k] = p;
-    c.refs[p] = 1;
+  for (int k = 0; k < PER; ++k) mine = min(mine + e[k].need, 1u << 20);
+  const uint32_t inside = exclusive_sum(mine, shared, &all);
+  free.ready(lds_bits, at, shared);
+  uint32_t rank = before + inside;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = first + tid * PER + k;
+    const uint8_t said = e[k].need > 0 && (rank > free.count || e[k].need > free.count - rank) ? PGXCACHE_NO_PAGES : e[k].said;
+    const bool done = e[k].is_slot && said == 0;
+    if (status && i < n) status[i] = said;
+    if (done && e[k].need > 0) {
+      atomicMax(&taken_end, rank + e[k].need);
+      if (PER > 1) {
+        for (uint32_t j = 0; j < e[k].need; ++j) {
+          const int p = free.select(rank + j);
+          c.row(e[k].slot)[c.pages_of(e[k].length) + (int)j] = p;
+          c.refs[p] = 1;
+        }
+      }
+    }
+    if (PER == 1) {
+      ends[tid] = inside + e[k].need;
+      row_of[tid] = e[k].slot;
+      have_of[tid] = c.pages_of(e[k].length);
+    }
+    if (ALONE) finish(c, e[k], done);
+    else if (i < n) plan[i] = done ? 1 : 0;
+    rank = min(rank + e[k].need, 0x7FFFFFFFu);
   }
-  if (ALONE) {
-    finish(c, e, done);
-    __syncthreads();   // nobody looks at the bits any more
-    free.ranks(before, before + there, [&](int w, uint64_t b, uint64_t mask) { c.free_bits[w] = b & ~mask; });
-  } else {
-    if (i < n) plan[i] = done ? 1 : 0;
-    free.ranks(before, before + there, [&](int w, uint64_t, uint64_t mask) { atomicOr((unsigned long long*)&c.taken[w], mask); });
+  __syncthreads();
+  if (PER == 1) {   // a thread per page, whichever entry it is for
+    const uint32_t there = taken_end > before ? taken_end - before : 0;
+    for (uint32_t r = (uint32_t)tid; r < there; r += kOneBlock) {
+      int t = 0;   // the entry: the first whose pages end above r
+#pragma unroll
+      for (int d = kOneBlock / 2; d > 0; d >>= 1)
+        if (ends[t + d - 1] <= r) t += d;
+      const int page = (int)(r - (t > 0 ? ends[t - 1] : 0)), p = free.select(before + r);
+      c.row(row_of[t])[have_of[t] + page] = p;
+      c.refs[p] = 1;
+    }
+    __syncthreads();
   }
+  // nobody looks at the bits any more
+  free.ranks(before, taken_end, [&](int w, uint64_t b, uint64_t mask) {
+    if (ALONE) c.free_bits[w] = b & ~mask;
+    else atomicOr((unsigned long long*)&c.taken[w], mask);
+  });
 }
 __global__ void __launch_bounds__(256) advance_apply_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, const int32_t* plan) {
   const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
@@ -298,49 +355,58 @@ __global__ void __launch_bounds__(256) advance_apply_kernel(Cache c, int n, cons
   if (i < n) finish(c, asked(c, n, slots, counts, count, i), plan[i] != 0);
 }
 
-__global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, int32_t* plan, uint8_t* status) {
+__global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, ForkEntry* plan, uint8_t* status) {
   __shared__ uint64_t lds_bits[kBitsInLds];
   __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64];
   FreePages free;
   free.load(c);
-  auto look = [&](int i, bool* slots, bool* same) {   // whether the entry needs a page
-    const int s = i < n ? src[i] : -1, d = i < n ? dst[i] : -1;
-    *slots = (uint32_t)s < (uint32_t)c.slots && (uint32_t)d < (uint32_t)c.slots;
-    *same = s == d || s == -1 || d == -1;
-    return *slots && s != d && (c.length(s) & ((1 << c.page_shift) - 1)) != 0;
+  struct Look {
+    int s, d, length;
+    bool slots, nothing, need;
+  };
+  auto look = [&](int i) {
+    Look e;
+    e.s = i < n ? src[i] : -1;
+    e.d = i < n ? dst[i] : -1;
+    e.slots = (uint32_t)e.s < (uint32_t)c.slots && (uint32_t)e.d < (uint32_t)c.slots;
+    e.nothing = e.s == e.d || e.s == -1 || e.d == -1;
+    e.length = e.slots ? c.length(e.s) : 0;
+    e.need = e.slots && !e.nothing && (e.length & ((1 << c.page_shift) - 1)) != 0;
+    return e;
   };
   const int i = (int)blockIdx.x * kOneBlock + (int)threadIdx.x;
-  bool slots, nothing, unused1, unused2;
-  const bool need = look(i, &slots, &nothing);
+  const Look e = look(i);
+  const int last = e.need ? c.row(e.s)[e.length >> c.page_shift] : -1, old = e.slots ? c.pages_of(c.length(e.d)) : 0;
   uint32_t before = 0, all;
   if (blockIdx.x > 0) {
     uint32_t sum = 0;
 #pragma unroll 4
-    for (int k = 0; k < (int)blockIdx.x; ++k) sum += look(k * kOneBlock + (int)threadIdx.x, &unused1, &unused2);
+    for (int k = 0; k < (int)blockIdx.x; ++k) sum += look(k * kOneBlock + (int)threadIdx.x).need;
     exclusive_sum(sum, shared, &before);
   }
-  const uint32_t rank = before + exclusive_sum(need, shared, &all);
+  const uint32_t rank = before + exclusive_sum(e.need, shared, &all);
   free.ready(lds_bits, at, shared);
-  uint8_t said = slots || nothing ? 0 : PGXCACHE_BAD_ENTRY;
-  int tail = !slots || nothing ? kSkip : kNoTail;
-  if (need) {
+  uint8_t said = e.slots || e.nothing ? 0 : PGXCACHE_BAD_ENTRY;
+  int tail = !e.slots || e.nothing ? kSkip : kNoTail;
+  if (e.need) {
     if (rank < free.count) tail = free.select(rank);
     else { tail = kSkip; said = PGXCACHE_NO_PAGES; }
   }
   if (i < n) {
-    plan[i] = tail;
+    plan[i] = ForkEntry{tail, e.s, e.d, e.length, last, old, {0, 0}};
     if (status) status[i] = said;
   }
   free.ranks(before, min(before + all, free.count), [&](int w, uint64_t, uint64_t mask) { atomicOr((unsigned long long*)&c.taken[w], mask); });
 }
 
-// A block per entry, of one wavefront for pages of up to 16 KB (4096 entries whose tails are 8 KB on average: 20.3 us with four wavefronts
-// each, 17.9 us with one, all of which the machine holds at once) and more for larger ones.  A page that both slots name keeps the
-// source's reference throughout, so none comes free in between.
-__global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const int32_t* src, const int32_t* dst, const int32_t* plan) {
-  const int tid = (int)threadIdx.x, threads = (int)blockDim.x;
-  if ((int)blockIdx.x >= n) {   // the blocks behind the entries' take the plan's pages out of the bits
-    const int w = ((int)blockIdx.x - n) * threads + tid;
+// `per` threads for each entry: a wavefront where pages have up to 16 KB (4096 entries whose tails are 8 KB on average: 20.3 us with four
+// wavefronts each, <<FORK_4096>> with one, all of which the machine holds at once), more for larger ones.  A page that both slots name keeps
+// the source's reference throughout, so none comes free in between.
+__global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const ForkEntry* plan, int per) {
+  __shared__ Freed freed;
+  const int entries = 256 / per, blocks = (n + entries - 1) / entries;
+  if ((int)blockIdx.x >= blocks) {   // the blocks behind the entries' take the plan's pages out of the bits
+    const int w = ((int)blockIdx.x - blocks) * 256 + (int)threadIdx.x;
     if (w >= (c.pages + 63) / 64) return;
     const uint64_t taken = c.taken[w];
     if (taken) {
@@ -349,57 +415,75 @@ __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const int32_t
     }
     return;
   }
-  const int i = (int)blockIdx.x, tail = plan[i], s = src[i], d = dst[i];
-  if (tail == kSkip) return;
-  const int length = c.length(s), full = length >> c.page_shift, filled = length & ((1 << c.page_shift) - 1);
-  const int old = c.pages_of(c.length(d)), most = max(old, full + (tail >= 0));
-  const int32_t* from = c.row(s);
-  int32_t* to = c.row(d);
-  if (tail >= 0 && c.is_page(from[full])) {   // the filled beginning of every head's keys and values
-    const uint32_t units = (uint32_t)(filled * c.head_dim / 8), all = (uint32_t)(c.layers * 2 * c.kv_heads) * units;
-    const uint32_t head = (uint32_t)(c.head_bytes() / 16);
-    const u32x4* a = (const u32x4*)(c.kv + from[full] * c.page_bytes());
-    u32x4* b = (u32x4*)(c.kv + tail * c.page_bytes());
+  const int tid = (int)threadIdx.x & (per - 1), i = (int)blockIdx.x * entries + (int)threadIdx.x / per;
+  ForkEntry e = plan[min(i, n - 1)];
+  if (i >= n) e.tail = kSkip;
+  freed.begin();
+  const int tail = e.tail, length = e.length, old = e.old, last = tail >= 0 ? e.last : -1;
+  const int full = length >> c.page_shift, filled = length & ((1 << c.page_shift) - 1), most = tail == kSkip ? 0 : max(old, full + (tail >= 0));
+  if (tail != kSkip) {
+    const int32_t* from = c.row(e.src);
+    int32_t* to = c.row(e.dst);
+    // the rows' entries and the page that is copied are asked for together
+    auto entry = [&](int k, int* now, int* before) {
+      *now = k < full ? from[k] : k == full ? tail : -1;
+      *before = k < old ? to[k] : -1;
+    };
+    auto exchange = [&](int k, int now, int before) {
+      if (now == before) return;   // a page that both had, as the nodes of one search tree have their root's
+      if (k < full && c.is_page(now)) atomicAdd(&c.refs[now], 1);
+      freed.release(c, before);
+      to[k] = now;
+    };
+    int now0 = -1, before0 = -1;
+    if (tid < most) entry(tid, &now0, &before0);
     constexpr int kAhead = 8;
-    for (uint32_t u = (uint32_t)tid; u < all; u += (uint32_t)threads * kAhead) {
+    const uint32_t units = (uint32_t)(filled * c.head_dim / 8), all = c.is_page(last) ? (uint32_t)(c.layers * 2 * c.kv_heads) * units : 0;
+    const uint32_t head = (uint32_t)(c.head_bytes() / 16);
+    const u32x4* a = (const u32x4*)(c.kv + last * c.page_bytes());
+    u32x4* b = (u32x4*)(c.kv + tail * c.page_bytes());
+    for (uint32_t u = (uint32_t)tid; u < all; u += (uint32_t)per * kAhead) {   // the filled beginning of every head's keys and values
       u32x4 x[kAhead];
       uint32_t at[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const uint32_t v = min(u + (uint32_t)(k * threads), all - 1), h = v / units;
+        const uint32_t v = min(u + (uint32_t)(k * per), all - 1), h = v / units;
         at[k] = h * head + (v - h * units);
         x[k] = a[at[k]];
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
-        if (u + (uint32_t)(k * threads) < all) b[at[k]] = x[k];
+        if (u + (uint32_t)(k * per) < all) b[at[k]] = x[k];
+    }
+    if (tid < most) exchange(tid, now0, before0);
+    for (int k = tid + per; k < most; k += per) {
+      int now, before;
+      entry(k, &now, &before);
+      exchange(k, now, before);
+    }
+    if (tid == 0) {
+      c.lengths[e.dst] = length;
+      c.grown[e.dst] = 0;
+      if (tail >= 0) c.refs[tail] = 1;
     }
   }
-  for (int k = tid; k < most; k += threads) {
-    const int now = k < full ? from[k] : k == full && tail >= 0 ? tail : -1;
-    if (k < full && c.is_page(now)) atomicAdd(&c.refs[now], 1);
-    if (k < old) c.release(to[k]);
-    to[k] = now;
-  }
-  __syncthreads();   // everyone has read the old length
-  if (tid == 0) {
-    c.lengths[d] = length;
-    c.grown[d] = 0;
-    if (tail >= 0) c.refs[tail] = 1;
-  }
+  freed.end(c);
 }
 
 __global__ void __launch_bounds__(256) free_kernel(Cache c, int n, const int32_t* slots) {
+  __shared__ Freed freed;
   const int i = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
-  if (i >= n) return;
-  const int slot = slots ? slots[i] : i;
-  if ((uint32_t)slot >= (uint32_t)c.slots) return;
-  int32_t* row = c.row(slot);
-  for (int k = lane, old = c.pages_of(c.length(slot)); k < old; k += 64) c.release(atomicExch(&row[k], -1));
-  if (lane == 0) {
-    c.lengths[slot] = 0;
-    c.grown[slot] = 0;
+  const int slot = i >= n ? -1 : slots ? slots[i] : i;
+  freed.begin();
+  if ((uint32_t)slot < (uint32_t)c.slots) {
+    int32_t* row = c.row(slot);
+    for (int k = lane, old = c.pages_of(c.length(slot)); k < old; k += 64) freed.release(c, atomicExch(&row[k], -1));
+    if (lane == 0) {
+      c.lengths[slot] = 0;
+      c.grown[slot] = 0;
+    }
   }
+  freed.end(c);
 }
 
 // a thread per page that moves: the r-th of those in use at and above `used` goes to the r-th free one
@@ -570,8 +654,17 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
   const uint32_t unit = (uint32_t)i * per_part + in_part;
   const int slot = a.slots ? a.slots[i] : i;
   const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
-  const int length = is_slot ? c.length(slot) : 0;
   const int first_head = head_tile * kHeads, heads_here = min(kHeads, a.group - first_head), head0 = kv_head * a.group + first_head;
+
+  // what depends on the entry only is asked for first, beside the slot's length
+  u32x4 query[NT], fresh = {0, 0, 0, 0};
+#pragma unroll
+  for (int m = 0; m < NT; ++m) query[m] = *(const u32x4_2*)(a.q + i * a.q_entry + (head0 + min(col, heads_here - 1)) * a.q_head + g * 16 + m * 64);
+  const bool writes = lane < 2 * D / 8;
+  const int fresh_at = lane % (D / 8) * 16;
+  if (a.k && wave == 0 && writes)
+    fresh = *(const u32x4_2*)((lane < D / 8 ? a.k + i * a.k_entry + kv_head * a.k_head : a.v + i * a.v_entry + kv_head * a.v_head) + fresh_at);
+  const int length = is_slot ? c.length(slot) : 0, grown = a.k && is_slot ? c.grown[slot] : 0;
 
   if (length == 0) {   // nothing to attend to
     if (split == 0 && wave == 0 && col < heads_here) {
@@ -597,28 +690,18 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
   if (alone && wave > 0) return;
 
   // the new token's key and value go into the cache first, by the block that reads the last tile
-  if (a.k && end == tiles && c.grown[slot] > 0) {
+  if (grown > 0 && end == tiles) {
     const int at = length - 1, page = row[at >> c.page_shift];
-    if (wave == 0 && c.is_page(page) && lane < 2 * D / 8) {
-      const int u = lane % (D / 8) * 16;
-      const char* x = lane < D / 8 ? a.k + i * a.k_entry + kv_head * a.k_head : a.v + i * a.v_entry + kv_head * a.v_head;
-      *(u32x4*)((char*)(lane < D / 8 ? keys : values) + page * page_bytes + (int64_t)(at & in_page) * D * 2 + u) = *(const u32x4_2*)(x + u);
-    }
+    if (wave == 0 && c.is_page(page) && writes)
+      *(u32x4*)((char*)(lane < D / 8 ? keys : values) + page * page_bytes + (int64_t)(at & in_page) * D * 2 + fresh_at) = fresh;
     // (a wavefront's own memory operations are in order; other wavefronts wait)
     if (W > 1 && !alone) __syncthreads();
     else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
   x8 q[NT];
-  {
-    const char* p = a.q + i * a.q_entry + (head0 + min(col, heads_here - 1)) * a.q_head + g * 16;
 #pragma unroll
-    for (int m = 0; m < NT; ++m) {
-      u32x4 x = *(const u32x4_2*)(p + m * 64);
-      if (col >= heads_here) x = u32x4{0, 0, 0, 0};
-      q[m] = __builtin_bit_cast(x8, x);
-    }
-  }
+  for (int m = 0; m < NT; ++m) q[m] = __builtin_bit_cast(x8, col < heads_here ? query[m] : u32x4{0, 0, 0, 0});
 
   float top = -INFINITY, sum = 0.0f;   // of the lane's head: the maximum that all four groups use, and this group's sum
   f32x4 acc[2 * NT];
@@ -916,7 +999,7 @@ bool opts_ok(const pgxcache_opts* o) {
 }
 
 struct Layout {
-  size_t free_bits, taken, grown, plan, moved_to, moves, counts, arrived, partial, total;
+  size_t free_bits, taken, grown, plan, forks, moved_to, moves, counts, arrived, partial, total;
 };
 Layout layout(const pgxcache_opts& o) {
   Layout l;
@@ -926,6 +1009,7 @@ Layout layout(const pgxcache_opts& o) {
   l.taken = take(((size_t)o.pages + 63) / 64 * 8);
   l.grown = take((size_t)o.slots * 4);
   l.plan = take((size_t)o.slots * 4);
+  l.forks = take((size_t)o.slots * sizeof(ForkEntry));
   l.moved_to = take((size_t)o.pages * 4);
   l.moves = take((size_t)o.pages * 8);
   l.counts = take(8);
@@ -970,7 +1054,7 @@ int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int3
   char* w = (char*)work_dev;
   h->o = *opts;
   h->kv = kv_dev; h->table = table_dev; h->lengths = lengths_dev; h->refs = refs_dev;
-  h->free_bits = (uint64_t*)(w + l.free_bits); h->taken = (uint64_t*)(w + l.taken); h->grown = (int32_t*)(w + l.grown); h->plan = (int32_t*)(w + l.plan);
+  h->free_bits = (uint64_t*)(w + l.free_bits); h->taken = (uint64_t*)(w + l.taken); h->grown = (int32_t*)(w + l.grown); h->plan = (int32_t*)(w + l.plan); h->forks = (ForkEntry*)(w + l.forks);
   h->moved_to = (int32_t*)(w + l.moved_to); h->moves = (int2*)(w + l.moves); h->counts = (int32_t*)(w + l.counts);
   h->arrived = (uint32_t*)(w + l.arrived); h->partial = (float*)(w + l.partial);
   const int rc = pgxcache_rescan(h);
@@ -990,12 +1074,13 @@ int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const in
   if (n == 0) return PGXCACHE_OK;
   const hipStream_t stream = (hipStream_t)h->o.stream;
   const Cache c = cache_of(h);
-  if (n <= kOneBlock) {   // one launch
-    hipLaunchKernelGGL((advance_kernel<true>), dim3(1), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
+  if (n <= 4 * kOneBlock) {   // one launch
+    if (n <= kOneBlock) hipLaunchKernelGGL((advance_kernel<1, true>), dim3(1), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
+    else hipLaunchKernelGGL((advance_kernel<4, true>), dim3(1), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
     HIPCHK(hipGetLastError());
     return PGXCACHE_OK;
   }
-  hipLaunchKernelGGL((advance_kernel<false>), dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
+  hipLaunchKernelGGL((advance_kernel<1, false>), dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
   HIPCHK(hipGetLastError());
   const int words = (c.pages + 63) / 64, threads = n > words ? n : words;
   hipLaunchKernelGGL(advance_apply_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, c, n, slots_dev, counts_dev, count, h->plan);
@@ -1041,11 +1126,11 @@ int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const i
   if (!list_ok(h, n)) return PGXCACHE_EINVAL;
   if (n == 0) return PGXCACHE_OK;
   if (!src_slots_dev || !dst_slots_dev) return PGXCACHE_EINVAL;
-  hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan, status_dev);
+  hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->forks, status_dev);
   HIPCHK(hipGetLastError());
   const size_t page = (size_t)h->o.layers * 2 * h->o.kv_heads * h->o.page_size * h->o.head_dim * 2;
-  const int threads = page <= 16384 ? 64 : page <= 32768 ? 128 : 256, words = (h->o.pages + 63) / 64;
-  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)(n + (words + threads - 1) / threads)), dim3((unsigned)threads), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->plan);
+  const int per = page <= 16384 ? 64 : page <= 32768 ? 128 : 256, entries = 256 / per, words = (h->o.pages + 63) / 64;
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)((n + entries - 1) / entries + (words + 255) / 256)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, h->forks, per);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
