@@ -27,7 +27,7 @@ thread_local int g_last_hip = 0;
 constexpr float kNone = -INFINITY;
 constexpr int kThreads = 256;
 
-enum Op { kLogits, kSample, kLoss };
+enum Op { kLogits, kSample, kLossShares, kLossMoves };
 
 struct Args {
   const void* logits;
@@ -202,27 +202,46 @@ __device__ __forceinline__ void count_record(const Args& a, uint32_t* counts, in
   const int b = first_row + r;
   if (b < a.rows) {
     const int begin = a.begin ? max(a.begin[b], 0) : 0, end = a.end ? min(a.end[b], a.record_len) : a.record_len;
-    const int32_t* p = a.record + (int64_t)b * a.record_row;
+    uint32_t* mine = counts + r * words;
+    const int64_t step = (int64_t)G * a.record_ply;
+    const int32_t* p = a.record + (int64_t)b * a.record_row + (int64_t)(begin + t0) * a.record_ply;
+    auto add = [&](int move) {
+      if ((uint32_t)move < (uint32_t)a.actions) atomicAdd(&mine[move >> 1], 1u << (16 * (move & 1)));
+    };
     constexpr int kAhead = 8;   // loads under way at once
-    for (int t = begin + t0; t < end; t += G * kAhead) {
+    int t = begin + t0;
+    for (; t + (kAhead - 1) * G < end; t += G * kAhead) {
       int move[kAhead];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) move[j] = t + j * G < end ? p[(int64_t)(t + j * G) * a.record_ply] : -1;
+      for (int j = 0; j < kAhead; ++j, p += step) move[j] = *p;
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j)
-        if ((uint32_t)move[j] < (uint32_t)a.actions) atomicAdd(&counts[r * words + (move[j] >> 1)], 1u << (16 * (move[j] & 1)));
+      for (int j = 0; j < kAhead; ++j) add(move[j]);
     }
+    int move[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j, p += step) move[j] = t + j * G < end ? *p : -1;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) add(move[j]);
   }
   __syncthreads();
 }
 
-// G lanes and NC chunks per row: up to G * NC * 8 actions
-template <class T, int G, int NC, bool RECORD, int OP>
+// x / d, rounded to nearest, for a d whose reciprocal y is: the product's error is found exactly and taken off (P. Markstein, 1990: with y
+// correctly rounded the result is).  5 instructions instead of 11; below 2^-100 the last bit may differ.  For d from 2^-20 to 2^20.
+__device__ __forceinline__ float divided(float x, float d, float y) {
+  const float q = x * y, r = __builtin_fmaf(-q, d, x), better = __builtin_fmaf(r, y, q);
+  return __builtin_isfinite(q) ? better : q;
+}
+__device__ __forceinline__ bool plain_divisor(float d) { return d >= 0x1p-20f && d <= 0x1p20f; }
+
+// G lanes and NC chunks per row: up to G * NC * 8 actions, and with FULL more than G * (NC - 1) * 8, so that only the last chunk can pass the row's end
+template <class T, int G, int NC, bool FULL, bool RECORD, int OP>
 __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
 #pragma clang fp contract(off)   // every operation of the adjustment is rounded by itself, as the header defines it
   extern __shared__ uint32_t counts[];
   __shared__ float shared[16];
   typedef typename T::type Elem;
+  constexpr bool kLoss = OP == kLossShares || OP == kLossMoves;
   const int rows_per_block = (int)blockDim.x / G, words = (a.actions + 1) / 2 | 1;
   const int first_row = (int)blockIdx.x * rows_per_block, lane = (int)threadIdx.x % G, slot = (int)threadIdx.x / G;
   const int A = a.actions;
@@ -230,51 +249,76 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
   const bool mine = first_row + slot < a.rows;
 
   const Elem* logits = (const Elem*)a.logits + (int64_t)b * a.logits_pitch;
-  float z[NC][8], other[NC][8];
+  float z[NC][8], other[NC][8];   // other: noise, or target shares
   uint32_t mask[NC][2];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const Chunk k(c * G + lane, A);
     load_chunk<T>(logits, k, A, z[c]);
     if (a.mask) load_mask(a.mask + (int64_t)b * a.mask_pitch, k, A, mask[c]);
-    if (OP != kLogits && a.second) load_chunk<F32>(a.second + (int64_t)b * a.second_pitch, k, A, other[c]);
+    if (OP == kLossShares || (OP == kSample && a.second)) load_chunk<F32>(a.second + (int64_t)b * a.second_pitch, k, A, other[c]);
   }
   const float own_temperature = a.temperature_row ? a.temperature_row[b] : a.temperature;
   const bool greedy = !(own_temperature > 0.0f);
   const float temperature = greedy ? 1.0f : own_temperature;
+  const float weight = kLoss && a.weight ? a.weight[b] : 1.0f;
+  const int taken = OP == kLossMoves ? a.taken[b] : -1;
   if (RECORD) count_record<G>(a, counts, words, first_row);
 
+  // the adjustment, a step at a time over all of the lane's actions
   uint32_t seen[NC], positive[NC];   // bits: the action occurs in the record; its logit is above 0 (for the gradient)
-  float top = kNone;
+  if (RECORD) {
+    const float inverse = 1.0f / a.repetition;
+    const bool quick = plain_divisor(a.repetition);
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const Chunk k(c * G + lane, A);
-    seen[c] = positive[c] = 0;
-    float bias[8];
-    if (a.bias) load_chunk<F32>(a.bias + (int64_t)b * a.bias_pitch, k, A, bias);
+    for (int c = 0; c < NC; ++c) {
+      const Chunk k(c * G + lane, A);
+      const uint16_t* n_of = (const uint16_t*)(counts + slot * words);
+      seen[c] = positive[c] = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float x = z[c][j];
-      if (RECORD) {
-        const int at = min(k.base + j, A - 1);
-        const uint32_t n = counts[slot * words + (at >> 1)] >> (16 * (at & 1)) & 0xFFFFu;
-        const float times = (float)n;
-        if (OP == kLoss) {
+      for (int j = 0; j < 8; ++j) {
+        float x = z[c][j];
+        const uint32_t n = n_of[A >= 8 ? k.base + j : min(j, A - 1)];
+        if (kLoss) {
           seen[c] |= (uint32_t)(n > 0) << j;
           positive[c] |= (uint32_t)(x > 0.0f) << j;
         }
-        const float punished = x > 0.0f ? x / a.repetition : x * a.repetition;
+        const float less = quick ? divided(x, a.repetition, inverse) : x / a.repetition;
+        const float punished = x > 0.0f ? less : x * a.repetition;
         x = n > 0 ? punished : x;
-        x = x - a.frequency * times;
-        x = n > 0 ? x - a.presence : x;
+        x = x - a.frequency * (float)n;
+        z[c][j] = x - (n > 0 ? a.presence : 0.0f);
       }
-      if (a.bias) x = x + bias[j];
-      if (a.temperature_row || a.temperature != 1.0f) x = x / temperature;
-      if (a.mask && (mask[c][j >> 2] >> (8 * (j & 3)) & 0xFFu) == 0) x = kNone;
-      z[c][j] = x;
-      const bool counts_here = j >= k.skip && k.base + j < A;
-      if (counts_here && x > kNone) top = fmaxf(top, x);
     }
+  }
+  if (a.bias) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float bias[8];
+      load_chunk<F32>(a.bias + (int64_t)b * a.bias_pitch, Chunk(c * G + lane, A), A, bias);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[c][j] = z[c][j] + bias[j];
+    }
+  }
+  if (__any(temperature != 1.0f)) {
+    if (__all(plain_divisor(temperature))) {
+      const float inverse = 1.0f / temperature;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[c][j] = divided(z[c][j], temperature, inverse);
+    } else {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[c][j] = z[c][j] / temperature;
+    }
+  }
+  if (a.mask) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[c][j] = (mask[c][j >> 2] >> (8 * (j & 3)) & 0xFFu) != 0 ? z[c][j] : kNone;
   }
   if (OP == kLogits && !a.normalize) {
     if (mine) {
@@ -283,6 +327,12 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
     }
     return;
   }
+  // from here on an action that is not possible has z = -infinity (fmaxf leaves NaN out)
+  float top = kNone;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, z[c][j]);   // (what a last chunk shares with the one before it may count twice here)
   top = reduced<Max, G>(top, shared);
   const bool some = top > kNone;
   const float from = some ? top : 0.0f;
@@ -294,74 +344,88 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const Chunk k(c * G + lane, A);
+    const bool check = !FULL || c == NC - 1;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool alive = z[c][j] > kNone, possible = alive && j >= k.skip && k.base + j < A;   // an action counts once
-      const float d = z[c][j] - from, e = possible ? __expf(d) : 0.0f;
-      total += e;
+      const bool alive = z[c][j] > kNone, counts_here = !check || (j >= k.skip && k.base + j < A);   // an action counts once
+      const float d = z[c][j] - from, e = alive ? __expf(d) : 0.0f;
+      total += counts_here ? e : 0.0f;
       if (OP == kSample) {
-        float score = a.second && !greedy ? z[c][j] + other[c][j] : z[c][j];
-        score = score == score ? score : kNone;
-        const bool take = possible && (score > best || (score == best && k.base + j < best_at));
+        const float score = a.second && !greedy ? z[c][j] + other[c][j] : z[c][j];
+        const bool take = score > best;   // ascending within the lane: the lowest index among equals
         best = take ? score : best;
         best_z = take ? z[c][j] : best_z;
         best_at = take ? k.base + j : best_at;
       }
-      if (OP == kLoss) {
-        float y = a.second ? other[c][j] : (k.base + j == a.taken[b] ? 1.0f : 0.0f);
-        y = alive ? y : 0.0f;
-        other[c][j] = y;
-        moment += possible ? e * d : 0.0f;
-        share += possible ? y : 0.0f;
-        cross += possible ? y * d : 0.0f;
+      if (kLoss) {
+        const float safe = alive ? d : 0.0f, counted = counts_here ? e : 0.0f;
+        const float y = OP == kLossShares ? (alive ? other[c][j] : 0.0f) : (alive && k.base + j == taken ? 1.0f : 0.0f);
+        const float y_counted = counts_here ? y : 0.0f;
+        moment += counted * safe;
+        share += y_counted;
+        cross += y_counted * safe;
+        z[c][j] = safe;
+        other[c][j] = alive ? y : kNone;   // marks those that are not possible
       }
     }
   }
   total = reduced<Sum, G>(total, shared);
   const float log_total = __logf(total);
 
-  if (OP == kLogits) {
-    if (mine) {
+  if (OP == kLogits && mine) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float out[8];
+    for (int c = 0; c < NC; ++c) {
+      float out[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) out[j] = z[c][j] > kNone ? z[c][j] - from - log_total : kNone;
-        store_chunk<F32>((float*)a.out + (int64_t)b * a.out_pitch, Chunk(c * G + lane, A), A, out);
-      }
+      for (int j = 0; j < 8; ++j) out[j] = z[c][j] > kNone ? z[c][j] - from - log_total : kNone;
+      store_chunk<F32>((float*)a.out + (int64_t)b * a.out_pitch, Chunk(c * G + lane, A), A, out);
     }
   }
   if (OP == kSample) {
+    if (some && best_at == 0x7FFFFFFF) {   // this lane's scores are all -infinity or NaN: its lowest possible action
+#pragma unroll
+      for (int c = NC - 1; c >= 0; --c) {
+        const Chunk k(c * G + lane, A);
+#pragma unroll
+        for (int j = 7; j >= 0; --j) {
+          const bool take = z[c][j] > kNone && k.base + j < A;
+          best_z = take ? z[c][j] : best_z;
+          best_at = take ? k.base + j : best_at;
+        }
+      }
+    }
     const int own = best_at;
     reduce_best<G>(best, best_at, shared);
-    // the lane that holds the action writes; a row without one is written by its first lane
+    // the lane that holds the action writes (two if the row's last chunks share it: the same); a row without one is written by its first lane
     if (mine && own == best_at && (some || lane == 0)) {
       ((int32_t*)a.out)[b] = some ? best_at : -1;
       if (a.row_out) a.row_out[b] = some ? best_z - from - log_total : 0.0f;
     }
   }
-  if (OP == kLoss) {
+  if (kLoss) {
     moment = reduced<Sum, G>(moment, shared);
     share = reduced<Sum, G>(share, shared);
     cross = reduced<Sum, G>(cross, shared);
-    const float weight = a.weight ? a.weight[b] : 1.0f, inverse = some ? 1.0f / total : 0.0f;
+    const float inverse = some ? 1.0f / total : 0.0f;
     const float entropy = some ? log_total - moment * inverse : 0.0f;
     if (mine && lane == 0) {
       if (a.row_out) a.row_out[b] = some ? weight * (share * log_total - cross) - a.entropy_bonus * entropy : 0.0f;
       if (a.row_out2) a.row_out2[b] = entropy;
     }
-    const float slope = a.grad_scale / temperature;
+    // with p = e / total:  weight (share p - y) + bonus p (d - log_total + entropy)  =  p (bonus d + level) - weight y
+    const float slope = a.grad_scale / temperature, level = some ? weight * share + a.entropy_bonus * (entropy - log_total) : 0.0f;
+    const float bend = a.entropy_bonus;
+    const float pull = weight * slope, each = inverse * slope;
     if (mine) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         float out[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const bool possible = z[c][j] > kNone;
-          const float d = z[c][j] - from, p = possible ? __expf(d) * inverse : 0.0f;
-          float g = weight * (share * p - other[c][j]) + a.entropy_bonus * p * (d - log_total + entropy);
+          const float d = z[c][j], e = __expf(d);
+          float g = e * each * __builtin_fmaf(bend, d, level) - pull * other[c][j];
           if (RECORD) g = seen[c] >> j & 1u ? (positive[c] >> j & 1u ? g / a.repetition : g * a.repetition) : g;
-          out[j] = possible ? g * slope : 0.0f;
+          out[j] = other[c][j] > kNone ? g : 0.0f;
         }
         store_chunk<T>((Elem*)a.out + (int64_t)b * a.out_pitch, Chunk(c * G + lane, A), A, out);
       }
@@ -369,7 +433,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
   }
 }
 
-template <class T, int G, int NC, int OP>
+template <class T, int G, int NC, bool FULL, int OP>
 hipError_t launch(const Args& a, hipStream_t stream) {
   // a block of one wavefront while that leaves the machine's 256 compute units a block each at most; rows of a larger batch share blocks of four
   const int threads = G > 64 ? G : (int64_t)a.rows * G <= 64 * 1024 ? 64 : kThreads;
@@ -377,18 +441,19 @@ hipError_t launch(const Args& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.rows + rows_per_block - 1) / rows_per_block)), block((unsigned)threads);
   if (a.record) {
     const size_t lds = (size_t)rows_per_block * ((a.actions + 1) / 2 | 1) * 4;
-    hipLaunchKernelGGL((policy_kernel<T, G, NC, true, OP>), grid, block, lds, stream, a);
+    hipLaunchKernelGGL((policy_kernel<T, G, NC, FULL, true, OP>), grid, block, lds, stream, a);
   } else {
-    hipLaunchKernelGGL((policy_kernel<T, G, NC, false, OP>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((policy_kernel<T, G, NC, FULL, false, OP>), grid, block, 0, stream, a);
   }
   return hipGetLastError();
 }
 template <class T, int OP>
 hipError_t launch_for_actions(const Args& a, hipStream_t stream) {
-  if (a.actions <= 128) return launch<T, 16, 1, OP>(a, stream);
-  if (a.actions <= 384) return launch<T, 16, 3, OP>(a, stream);
-  if (a.actions <= 2048) return launch<T, 64, 4, OP>(a, stream);
-  return launch<T, 256, 4, OP>(a, stream);
+  if (a.actions <= 128) return launch<T, 16, 1, true, OP>(a, stream);
+  if (a.actions <= 256) return launch<T, 16, 2, true, OP>(a, stream);
+  if (a.actions <= 384) return launch<T, 16, 3, true, OP>(a, stream);
+  if (a.actions <= 2048) return launch<T, 64, 4, false, OP>(a, stream);
+  return launch<T, 256, 4, false, OP>(a, stream);
 }
 template <int OP>
 int run(const Args& a, int32_t type, void* stream) {
@@ -465,7 +530,7 @@ int pgxpolicy_loss(int32_t rows, int32_t actions, const void* logits_dev, int32_
   a.second = target_dev; a.second_pitch = target_pitch; a.taken = taken_dev; a.weight = weight_dev;
   a.entropy_bonus = entropy_bonus; a.grad_scale = grad_scale;
   a.row_out = loss_dev; a.row_out2 = entropy_dev; a.out = grad_dev; a.out_pitch = grad_pitch;
-  return run<kLoss>(a, type, stream);
+  return target_dev ? run<kLossShares>(a, type, stream) : run<kLossMoves>(a, type, stream);
 }
 
 const char* pgxpolicy_strerror(int code) {
