@@ -9,6 +9,8 @@
 #include <stdint.h>
 #include <stdlib.h>
 
+#include <type_traits>
+
 #include "pgxpolicy.h"
 
 namespace {
@@ -47,7 +49,7 @@ struct Args {
   void* out;                // adjusted logits, actions, or the gradient
   int64_t out_pitch;
   float *row_out, *row_out2;   // log-probability; loss, entropy
-  int32_t rows, actions, record_len, normalize, record_by_row;
+  int32_t rows, actions, record_len, normalize, record_by_row, record_near, by_die;
   float repetition, frequency, presence, temperature, entropy_bonus, grad_scale;
 };
 
@@ -191,40 +193,52 @@ __device__ __forceinline__ void reduce_best(float& score, int& index, float* sha
   }
 }
 
-// How often each action occurs in the rows' records: 16-bit counters in LDS, two to a word, `words` words per row.
+// The part of the rows' records that this thread looks at, asked for ahead of everything else.
 template <int G>
-__device__ __forceinline__ void count_record(const Args& a, uint32_t* counts, int words, int first_row) {
-  const int threads = (int)blockDim.x, rows = threads / G, tid = (int)threadIdx.x;
-  for (int i = tid; i < rows * words; i += threads) counts[i] = 0;
-  __syncthreads();
-  // neighbouring threads read what is next to each other in memory: the plies of a row, or the rows of a ply
-  const int r = a.record_by_row ? tid / G : tid % rows, t0 = a.record_by_row ? tid % G : tid / rows;
-  const int b = first_row + r;
-  if (b < a.rows) {
-    const int begin = a.begin ? max(a.begin[b], 0) : 0, end = a.end ? min(a.end[b], a.record_len) : a.record_len;
-    uint32_t* mine = counts + r * words;
-    const int64_t step = (int64_t)G * a.record_ply;
-    const int32_t* p = a.record + (int64_t)b * a.record_row + (int64_t)(begin + t0) * a.record_ply;
-    auto add = [&](int move) {
-      if ((uint32_t)move < (uint32_t)a.actions) atomicAdd(&mine[move >> 1], 1u << (16 * (move & 1)));
-    };
-    constexpr int kAhead = 8;   // loads under way at once
-    int t = begin + t0;
-    for (; t + (kAhead - 1) * G < end; t += G * kAhead) {
-      int move[kAhead];
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j, p += step) move[j] = *p;
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) add(move[j]);
-    }
-    int move[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j, p += step) move[j] = t + j * G < end ? *p : -1;
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) add(move[j]);
+struct RecordPart {
+  int row, row_index;     // of the block; of the call
+  int first;              // this thread's first ply after the record's begin, then every G-th
+  int from, to;           // as the caller has them
+  __device__ __forceinline__ void begin(const Args& a, int first_row) {
+    // neighbouring threads read what is next to each other in memory: the plies of a row, or the rows of a ply
+    const int rows = (int)blockDim.x / G, tid = (int)threadIdx.x;
+    row = a.record_by_row ? tid / G : tid % rows;
+    first = a.record_by_row ? tid % G : tid / rows;
+    const int b = min(first_row + row, a.rows - 1);
+    from = a.begin ? a.begin[b] : 0;
+    to = first_row + row >= a.rows ? 0 : a.end ? a.end[b] : a.record_len;
+    row_index = b;
   }
-  __syncthreads();
-}
+  // How often each action occurs: 16-bit counters in LDS, two to a word, `words` words per row.
+  __device__ __forceinline__ void count(const Args& a, uint32_t* counts, int words) {
+    const int threads = (int)blockDim.x;
+    for (int i = (int)threadIdx.x; i < threads / G * words; i += threads) counts[i] = 0;
+    __syncthreads();
+    uint32_t* mine = counts + row * words;
+    int t = max(from, 0) + first;
+    const int end = min(to, a.record_len);
+    auto add = [&](int move, bool there) {
+      if (there && (uint32_t)move < (uint32_t)a.actions) atomicAdd(&mine[move >> 1], 1u << (16 * (move & 1)));
+    };
+    constexpr int kAhead = 24;   // loads under way at once (65536 rows of up to 361 plies: 81 us with 8 and 64-bit addresses, 76 with 24 and 32-bit ones)
+    if (a.record_near) {   // every move within 32 bits of the first: loads without a condition, those behind the end repeat the last
+      const uint32_t row_at = (uint32_t)row_index * (uint32_t)a.record_row, ply = (uint32_t)a.record_ply, last = row_at + (uint32_t)max(end - 1, 0) * ply;
+      for (; t < end; t += G * kAhead) {
+        const uint32_t p = row_at + (uint32_t)t * ply;
+        int move[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) move[j] = a.record[min(p + (uint32_t)(j * G) * ply, last)];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) add(move[j], t + j * G < end);
+      }
+    } else {
+      const int64_t step = (int64_t)G * a.record_ply;
+      const int32_t* p = a.record + (int64_t)row_index * a.record_row + (int64_t)t * a.record_ply;
+      for (; t < end; t += G, p += step) add(*p, true);
+    }
+    __syncthreads();
+  }
+};
 
 // x / d, rounded to nearest, for a d whose reciprocal y is: the product's error is found exactly and taken off (P. Markstein, 1990: with y
 // correctly rounded the result is).  5 instructions instead of 11; below 2^-100 the last bit may differ.  For d from 2^-20 to 2^20.
@@ -243,11 +257,16 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
   typedef typename T::type Elem;
   constexpr bool kLoss = OP == kLossShares || OP == kLossMoves;
   const int rows_per_block = (int)blockDim.x / G, words = (a.actions + 1) / 2 | 1;
-  const int first_row = (int)blockIdx.x * rows_per_block, lane = (int)threadIdx.x % G, slot = (int)threadIdx.x / G;
+  // blocks go to the eight dies in turn: each die takes a stretch of rows, so that rows that share a line of memory meet in its L2
+  const uint32_t eighth = gridDim.x >> 3, piece = a.by_die ? (blockIdx.x & 7u) * eighth + (blockIdx.x >> 3) : blockIdx.x;
+  const int first_row = (int)piece * rows_per_block, lane = (int)threadIdx.x % G, slot = (int)threadIdx.x / G;
   const int A = a.actions;
+  if (first_row >= a.rows) return;
   const int b = min(first_row + slot, a.rows - 1);   // lanes beyond the last row repeat it and write nothing
   const bool mine = first_row + slot < a.rows;
 
+  RecordPart<G> part;
+  if (RECORD) part.begin(a, first_row);
   const Elem* logits = (const Elem*)a.logits + (int64_t)b * a.logits_pitch;
   float z[NC][8], other[NC][8];   // other: noise, or target shares
   uint32_t mask[NC][2];
@@ -263,33 +282,36 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
   const float temperature = greedy ? 1.0f : own_temperature;
   const float weight = kLoss && a.weight ? a.weight[b] : 1.0f;
   const int taken = OP == kLossMoves ? a.taken[b] : -1;
-  if (RECORD) count_record<G>(a, counts, words, first_row);
+  if (RECORD) part.count(a, counts, words);
 
   // the adjustment, a step at a time over all of the lane's actions
   uint32_t seen[NC], positive[NC];   // bits: the action occurs in the record; its logit is above 0 (for the gradient)
   if (RECORD) {
+    const uint16_t* n_of = (const uint16_t*)(counts + slot * words);
     const float inverse = 1.0f / a.repetition;
-    const bool quick = plain_divisor(a.repetition);
+    auto punish = [&](auto quick) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const Chunk k(c * G + lane, A);
-      const uint16_t* n_of = (const uint16_t*)(counts + slot * words);
-      seen[c] = positive[c] = 0;
+      for (int c = 0; c < NC; ++c) {
+        const Chunk k(c * G + lane, A);
+        seen[c] = positive[c] = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float x = z[c][j];
-        const uint32_t n = n_of[A >= 8 ? k.base + j : min(j, A - 1)];
-        if (kLoss) {
-          seen[c] |= (uint32_t)(n > 0) << j;
-          positive[c] |= (uint32_t)(x > 0.0f) << j;
+        for (int j = 0; j < 8; ++j) {
+          float x = z[c][j];
+          const uint32_t n = n_of[k.base + (A >= 8 ? j : min(j, A - 1))];
+          if (kLoss) {
+            seen[c] |= (uint32_t)(n > 0) << j;
+            positive[c] |= (uint32_t)(x > 0.0f) << j;
+          }
+          const float less = quick.value ? divided(x, a.repetition, inverse) : x / a.repetition;
+          const float punished = x > 0.0f ? less : x * a.repetition;
+          x = n > 0 ? punished : x;
+          x = x - a.frequency * (float)n;
+          z[c][j] = x - (n > 0 ? a.presence : 0.0f);
         }
-        const float less = quick ? divided(x, a.repetition, inverse) : x / a.repetition;
-        const float punished = x > 0.0f ? less : x * a.repetition;
-        x = n > 0 ? punished : x;
-        x = x - a.frequency * (float)n;
-        z[c][j] = x - (n > 0 ? a.presence : 0.0f);
       }
-    }
+    };
+    if (plain_divisor(a.repetition)) punish(std::true_type{});
+    else punish(std::false_type{});
   }
   if (a.bias) {
 #pragma unroll
@@ -434,11 +456,13 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
 }
 
 template <class T, int G, int NC, bool FULL, int OP>
-hipError_t launch(const Args& a, hipStream_t stream) {
+hipError_t launch(Args a, hipStream_t stream) {
   // a block of one wavefront while that leaves the machine's 256 compute units a block each at most; rows of a larger batch share blocks of four
   const int threads = G > 64 ? G : (int64_t)a.rows * G <= 64 * 1024 ? 64 : kThreads;
   const int rows_per_block = threads / G;
-  const dim3 grid((unsigned)((a.rows + rows_per_block - 1) / rows_per_block)), block((unsigned)threads);
+  const unsigned blocks = (unsigned)((a.rows + rows_per_block - 1) / rows_per_block);
+  a.by_die = blocks >= 64;
+  const dim3 grid(a.by_die ? (blocks + 7) / 8 * 8 : blocks), block((unsigned)threads);
   if (a.record) {
     const size_t lds = (size_t)rows_per_block * ((a.actions + 1) / 2 | 1) * 4;
     hipLaunchKernelGGL((policy_kernel<T, G, NC, FULL, true, OP>), grid, block, lds, stream, a);
@@ -493,6 +517,9 @@ bool common(Args& a, int32_t rows, int32_t actions, const void* logits, int32_t 
     a.record = adjust->record_dev; a.record_len = adjust->record_len;
     a.record_row = adjust->record_row_stride; a.record_ply = adjust->record_ply_stride;
     a.begin = adjust->begin_dev; a.end = adjust->end_dev;
+    const int64_t most = (int64_t)1 << 29;   // elements
+    a.record_near = a.record_row >= 0 && a.record_ply >= 0 && a.record_row < most && a.record_ply < most &&
+                    (rows - 1) * a.record_row + (int64_t)(a.record_len - 1) * a.record_ply < most;
     a.record_by_row = llabs(a.record_ply) <= llabs(a.record_row);
   }
   return true;
