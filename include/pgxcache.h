@@ -40,6 +40,9 @@ extern "C" {
 #define PGXCACHE_F16 1
 #define PGXCACHE_BF16 2
 
+#define PGXCACHE_MAX_LENGTH (1 << 30)     /* tokens that a slot's pages can hold */
+#define PGXCACHE_MAX_PAGE_BYTES (1 << 30)
+
 #define PGXCACHE_NO_PAGES 1    /* status: too few free pages */
 #define PGXCACHE_FULL 2        /* status: more tokens than width pages hold */
 #define PGXCACHE_BAD_ENTRY 255 /* status: no such slot, or a negative number of tokens */

@@ -995,6 +995,8 @@ bool opts_ok(const pgxcache_opts* o) {
   if (o->width > (1 << 20) || o->layers > 4096 || o->kv_heads > 4096 || o->pages > 0x7FFFFFC0) return false;
   if (o->page_size < 16 || o->page_size > 1024 || (o->page_size & (o->page_size - 1)) != 0) return false;
   if (o->head_dim != 32 && o->head_dim != 64 && o->head_dim != 96 && o->head_dim != 128 && o->head_dim != 256) return false;
+  // tokens of a slot and bytes of a page are counted in 32 bits
+  if ((int64_t)o->width * o->page_size > PGXCACHE_MAX_LENGTH || (int64_t)o->layers * o->kv_heads * o->page_size * o->head_dim * 4 > PGXCACHE_MAX_PAGE_BYTES) return false;
   return o->type == PGXCACHE_F16 || o->type == PGXCACHE_BF16;
 }
 

@@ -30,6 +30,7 @@ def test_sizes_and_argument_errors_need_no_gpu():
     for bad in (dict(slots=0), dict(pages=0), dict(width=0), dict(width=2 ** 20 + 1), dict(layers=0), dict(kv_heads=0), dict(page_size=8), dict(page_size=24),
                 dict(page_size=2048), dict(head_dim=48), dict(head_dim=0), dict(type=0), dict(type=3), dict(pages=2 ** 31 - 1)):
         assert size(**bad) == 0, bad
+    assert size(width=2 ** 20, page_size=1024) > 0 and size(width=2 ** 20, page_size=1024, layers=4096, kv_heads=8) == 0   # pages of 16 GB
     assert L.pgxcache_work_bytes(None) == 0
     h, p, n = C.c_void_p(), C.c_void_p(4096), size()
     init = lambda o=None, kv=p, table=p, lengths=p, refs=p, work=p, nbytes=n, out=C.byref(h): L.pgxcache_init(  # noqa: E731
