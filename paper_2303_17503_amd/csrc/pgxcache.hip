@@ -274,11 +274,13 @@ __device__ __forceinline__ void finish(const Cache& c, const Advance& e, bool do
 // neighbouring entries per thread, all their loads under way together (4096 entries: <<ADVANCE_TILES>> us, by the two kernels 9.1 + 4.1).
 // The pages that the entries get are the free ones of consecutive ranks (an entry that cannot have its pages is followed by others that cannot),
 // so they leave the bits a word at a time (4600 pages, taken out one by one: 52 us, now 12).
+constexpr uint32_t kWanted = 1536;
 template <int PER, bool ALONE>
 __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, const int32_t* slots, const int32_t* counts, int count, int32_t* plan, uint8_t* status) {
   __shared__ uint64_t lds_bits[kBitsInLds];
   __shared__ uint32_t at[kOneBlock], shared[kOneBlock / 64], ends[kOneBlock], taken_end;
   __shared__ int32_t row_of[kOneBlock], have_of[kOneBlock];
+  __shared__ int2 wanted[PER > 1 ? kWanted : 1];   // (slot, place in its row) of each page
   const int tid = (int)threadIdx.x, first = ALONE ? 0 : (int)blockIdx.x * kOneBlock;
   if (tid == 0) taken_end = 0;
   FreePages free;
@@ -308,9 +310,14 @@ __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, cons
       atomicMax(&taken_end, rank + e[k].need);
       if (PER > 1) {
         for (uint32_t j = 0; j < e[k].need; ++j) {
-          const int p = free.select(rank + j);
-          c.row(e[k].slot)[c.pages_of(e[k].length) + (int)j] = p;
-          c.refs[p] = 1;
+          const int place = c.pages_of(e[k].length) + (int)j;
+          if (all <= kWanted) {
+            wanted[rank - before + j] = make_int2(e[k].slot, place);
+          } else {
+            const int p = free.select(rank + j);
+            c.row(e[k].slot)[place] = p;
+            c.refs[p] = 1;
+          }
         }
       }
     }
@@ -324,8 +331,16 @@ __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, cons
     rank = min(rank + e[k].need, 0x7FFFFFFFu);
   }
   __syncthreads();
-  if (PER == 1) {   // a thread per page, whichever entry it is for
-    const uint32_t there = taken_end > before ? taken_end - before : 0;
+  const uint32_t there = taken_end > before ? taken_end - before : 0;
+  if (PER > 1) {
+    if (all <= kWanted) {
+      for (uint32_t r = (uint32_t)tid; r < there; r += kOneBlock) {
+        const int p = free.select(before + r);
+        c.row(wanted[r].x)[wanted[r].y] = p;
+        c.refs[p] = 1;
+      }
+    }
+  } else {   // a thread per page, whichever entry it is for
     for (uint32_t r = (uint32_t)tid; r < there; r += kOneBlock) {
       int t = 0;   // the entry: the first whose pages end above r
 #pragma unroll
@@ -335,8 +350,8 @@ __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, cons
       c.row(row_of[t])[have_of[t] + page] = p;
       c.refs[p] = 1;
     }
-    __syncthreads();
   }
+  __syncthreads();
   // nobody looks at the bits any more
   free.ranks(before, taken_end, [&](int w, uint64_t b, uint64_t mask) {
     if (ALONE) c.free_bits[w] = b & ~mask;
@@ -664,6 +679,10 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
   const int fresh_at = lane % (D / 8) * 16;
   if (a.k && wave == 0 && writes)
     fresh = *(const u32x4_2*)((lane < D / 8 ? a.k + i * a.k_entry + kv_head * a.k_head : a.v + i * a.v_entry + kv_head * a.v_head) + fresh_at);
+  const int32_t* row = c.row(is_slot ? slot : 0);
+  // page of half-tile lane & 1 of the wavefront's tile number (a multiple of 32) + lane / 2; the first ones are asked for before the length is known
+  int ids = 0;
+  if (a.splits == 1) ids = row[min((((wave + (lane >> 1) * W) * 2 + (lane & 1)) << 4) >> c.page_shift, c.width - 1)];
   const int length = is_slot ? c.length(slot) : 0, grown = a.k && is_slot ? c.grown[slot] : 0;
 
   if (length == 0) {   // nothing to attend to
@@ -680,7 +699,6 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
   if (split >= active) return;
   const int begin = split * chunk, end = min(tiles, begin + chunk);
 
-  const int32_t* row = c.row(slot);
   const int64_t page_bytes = c.page_bytes(), head_bytes = c.head_bytes();
   const char* keys = c.kv + ((int64_t)a.layer * 2 * c.kv_heads + kv_head) * head_bytes;
   const char* values = keys + c.kv_heads * head_bytes;
@@ -708,11 +726,11 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
 #pragma unroll
   for (int m = 0; m < 2 * NT; ++m) acc[m] = f32x4{0, 0, 0, 0};
 
-  int ids = 0;   // page of half-tile lane & 1 of the wavefront's tile number (a multiple of 32) + lane / 2
+  if (!c.is_page(ids)) ids = 0;   // (behind the sequence: what is read there does not count)
   const int last_half = (length - 1) >> 4;
   auto load = [&](Tile<NT>& t, int number) {   // the wavefront's tile of that number
     const int tile = begin + wave + number * W;
-    if ((number & 31) == 0) {
+    if ((number & 31) == 0 && (number > 0 || a.splits > 1)) {
       const int half = min((tile + (lane >> 1) * W) * 2 + (lane & 1), last_half);
       const int p = row[(half << 4) >> c.page_shift];
       ids = c.is_page(p) ? p : 0;
