@@ -68,8 +68,8 @@ struct Cache {
   __device__ __forceinline__ int length(int slot) const { return min(max(lengths[slot], 0), capacity()); }
   __device__ __forceinline__ int32_t* row(int slot) const { return table + (int64_t)slot * width; }
   __device__ __forceinline__ bool is_page(int p) const { return (uint32_t)p < (uint32_t)pages; }
-  __device__ __forceinline__ int64_t head_bytes() const { return ((int64_t)head_dim << page_shift) * 2; }      // one head's keys or values of a page
-  __device__ __forceinline__ int64_t page_bytes() const { return head_bytes() * kv_heads * 2 * layers; }
+  __host__ __device__ __forceinline__ int64_t head_bytes() const { return ((int64_t)head_dim << page_shift) * 2; }      // one head's keys or values of a page
+  __host__ __device__ __forceinline__ int64_t page_bytes() const { return head_bytes() * kv_heads * 2 * layers; }
 };
 
 // Pages that come free in a block.  Those of one word of the bits are gathered in LDS, so that a word is written once: pages given out together
@@ -653,8 +653,12 @@ struct Tile {   // 32 tokens: keys [half][32-element part], values [token][dword
   uint32_t v[8][NT];
 };
 
-// W wavefronts share a row (an entry and a key head); with four a row may also be split over blocks
-template <class T, int NT, int W>
+template <bool STREAM, class V>
+__device__ __forceinline__ V read_once(const V* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; }
+
+// W wavefronts share a row (an entry and a key head); with four a row may also be split over blocks.  STREAM: keys and values are read with
+// the hint that they are not read again soon.
+template <class T, int NT, int W, bool STREAM>
 __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c, AttendArgs a) {
   typedef typename T::x8 x8;
   constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
@@ -740,12 +744,12 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
       const int64_t page = (int64_t)__builtin_amdgcn_readlane(ids, (number & 31) * 2 + h) * page_bytes + (int64_t)((tile * 32 + h * 16) & in_page) * (D * 2);
       const char* k = keys + page + (col * D * 2 + g * 16);
 #pragma unroll
-      for (int m = 0; m < NT; ++m) t.k[h][m] = *(const u32x4*)(k + m * 64);
+      for (int m = 0; m < NT; ++m) t.k[h][m] = read_once<STREAM>((const u32x4*)(k + m * 64));
       const char* v = values + page + (g * 4 * D * 2 + col * NT * 4);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int w = 0; w < NT; ++w) t.v[h * 4 + j][w] = ((const uint32_t*)(v + j * D * 2))[w];
+        for (int w = 0; w < NT; ++w) t.v[h * 4 + j][w] = read_once<STREAM>((const uint32_t*)(v + j * D * 2) + w);
     }
   };
   auto compute = [&](Tile<NT>& t, int number, auto last) {
@@ -973,8 +977,13 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
 
 template <class T, int NT, int W>
 hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t rows, hipStream_t stream) {
+  // A pool beyond the 256 MB memory-side cache is streamed (4096 slots of 1 to 722 tokens, 757 MB: 141 -> 136 us, all of 722: 261 -> 240, 3
+  // sequences of 110000, 1.35 GB: 230 -> 203; 1024 slots of 1 to 722, 189 MB, which stay in that cache from step to step: 34 -> 39).
+  const bool streamed = (int64_t)c.pages * c.page_bytes() > (int64_t)256 << 20;
   const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = a.splits > 1 ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
-  hipLaunchKernelGGL((attend_kernel<T, NT, W>), dim3((unsigned)(rows * a.splits)), dim3(64 * W), join > weights ? join : weights, stream, c, a);
+  const dim3 grid((unsigned)(rows * a.splits)), block(64 * W);
+  if (streamed) hipLaunchKernelGGL((attend_kernel<T, NT, W, true>), grid, block, join > weights ? join : weights, stream, c, a);
+  else hipLaunchKernelGGL((attend_kernel<T, NT, W, false>), grid, block, join > weights ? join : weights, stream, c, a);
   return hipGetLastError();
 }
 template <class T, int NT>

@@ -402,3 +402,17 @@ def test_native_and_python_checks_make_the_same_calls(monkeypatch):
     monkeypatch.setattr(pg.cache_binding, "_fast", None)
     for a, b in zip(native, history()):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n,head_dim,heads", [(6, 64, 4), (6, 256, 2), (600, 32, 6), (1300, 96, 2), (3, 128, 24)])
+def test_a_pool_beyond_every_cache_gives_the_same(n, head_dim, heads):
+    """pools of more than 256 MB are read with another hint"""
+    r = random.Random(1)
+    lengths = [r.choice(EDGES[:14] if n > 100 else [33, 722, 5000]) for _ in range(n)]
+    small = filled(lengths, 1, 1, head_dim, 16, torch.bfloat16, seed=4)
+    more = (300 << 20) // (2 * 16 * head_dim * 2)
+    kv = torch.cat([small.kv, torch.full((more, *small.kv.shape[1:]), float("nan"), dtype=torch.bfloat16, device="cuda")])
+    big = pg.PagedCache(kv, small.table, small.lengths, torch.cat([small.refs, torch.zeros(more, dtype=torch.int32, device="cuda")]))
+    q = torch.randn(n, heads, head_dim, device="cuda", dtype=torch.bfloat16)
+    a, b = small.attend(0, q, lse=True), big.attend(0, q, lse=True)
+    assert torch.equal(bits(a[0]), bits(b[0])) and torch.equal(bits(a[1]), bits(b[1])) and torch.isfinite(a[0][torch.tensor(lengths) > 0].float()).all()
