@@ -202,6 +202,13 @@ struct FreePages {
     }
     return w * 64 + place(b, left);
   }
+  // the next free page above p (there has to be one)
+  __device__ __forceinline__ int next(int p) const {
+    int w = p >> 6;
+    uint64_t b = (p & 63) == 63 ? 0 : bits[w] & ~0ull << ((p & 63) + 1);
+    while (b == 0) b = bits[++w];
+    return w * 64 + (int)__builtin_ctzll(b);
+  }
   // the page in use with `rank` ones in use below it (there has to be one)
   __device__ __forceinline__ int select_used(uint32_t rank) const {
     int t = 0;
@@ -340,15 +347,21 @@ __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, cons
         c.refs[p] = 1;
       }
     }
-  } else {   // a thread per page, whichever entry it is for
-    for (uint32_t r = (uint32_t)tid; r < there; r += kOneBlock) {
-      int t = 0;   // the entry: the first whose pages end above r
+  } else {   // an equal share of the pages for each thread, whichever entries they are for
+    const uint32_t share = (there + kOneBlock - 1) / kOneBlock, begin = (uint32_t)tid * share, end = min(begin + share, there);
+    if (begin < end) {
+      int t = 0;   // the entry of the first: the one whose pages end above it
 #pragma unroll
       for (int d = kOneBlock / 2; d > 0; d >>= 1)
-        if (ends[t + d - 1] <= r) t += d;
-      const int page = (int)(r - (t > 0 ? ends[t - 1] : 0)), p = free.select(before + r);
-      c.row(row_of[t])[have_of[t] + page] = p;
-      c.refs[p] = 1;
+        if (ends[t + d - 1] <= begin) t += d;
+      int p = free.select(before + begin);
+      for (uint32_t r = begin;;) {
+        c.row(row_of[t])[have_of[t] + (int)(r - (t > 0 ? ends[t - 1] : 0))] = p;
+        c.refs[p] = 1;
+        if (++r == end) break;
+        while (ends[t] <= r) ++t;
+        p = free.next(p);
+      }
     }
   }
   __syncthreads();

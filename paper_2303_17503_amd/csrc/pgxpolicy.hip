@@ -241,12 +241,21 @@ struct RecordPart {
 };
 
 // x / d, rounded to nearest, for a d whose reciprocal y is: the product's error is found exactly and taken off (P. Markstein, 1990: with y
-// correctly rounded the result is).  5 instructions instead of 11; below 2^-100 the last bit may differ.  For d from 2^-20 to 2^20.
+// correctly rounded is).  3 instructions instead of 11; below 2^-100 the last bit may differ.  For |x| up to 2^100 and d from 2^-20 to 2^20.
 __device__ __forceinline__ float divided(float x, float d, float y) {
-  const float q = x * y, r = __builtin_fmaf(-q, d, x), better = __builtin_fmaf(r, y, q);
-  return __builtin_isfinite(q) ? better : q;
+  const float q = x * y;
+  return __builtin_fmaf(__builtin_fmaf(-q, d, x), y, q);
 }
 __device__ __forceinline__ bool plain_divisor(float d) { return d >= 0x1p-20f && d <= 0x1p20f; }
+template <int NC>
+__device__ __forceinline__ bool plain_dividends(const float (&z)[NC][8]) {   // (false for infinities; NaN stays NaN either way)
+  float most = 0.0f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(z[c][j]));
+  return most <= 0x1p100f;
+}
 
 // G lanes and NC chunks per row: up to G * NC * 8 actions, and with FULL more than G * (NC - 1) * 8, so that only the last chunk can pass the row's end
 template <class T, int G, int NC, bool FULL, bool RECORD, int OP>
@@ -310,7 +319,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
         }
       }
     };
-    if (plain_divisor(a.repetition)) punish(std::true_type{});
+    if (__all(plain_divisor(a.repetition) && plain_dividends(z))) punish(std::true_type{});
     else punish(std::false_type{});
   }
   if (a.bias) {
@@ -323,7 +332,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
     }
   }
   if (__any(temperature != 1.0f)) {
-    if (__all(plain_divisor(temperature))) {
+    if (__all(plain_divisor(temperature) && plain_dividends(z))) {
       const float inverse = 1.0f / temperature;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
@@ -349,15 +358,25 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
     }
     return;
   }
-  // from here on an action that is not possible has z = -infinity (fmaxf leaves NaN out)
+  // from here on an action that is not possible has z = -infinity
   float top = kNone;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, z[c][j]);   // (what a last chunk shares with the one before it may count twice here)
+    for (int j = 0; j < 8; ++j) {
+      z[c][j] = fmaxf(z[c][j], kNone);   // NaN is not possible
+      top = fmaxf(top, z[c][j]);         // (what a last chunk shares with the one before it may count twice here)
+    }
   top = reduced<Max, G>(top, shared);
   const bool some = top > kNone;
   const float from = some ? top : 0.0f;
+
+  if (OP == kSample && a.second && __any(greedy)) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) other[c][j] = greedy ? 0.0f : other[c][j];
+  }
 
   // sums over the possible actions: of e = exp(z - top), and for the loss of e (z - top), y and y (z - top)
   float total = 0.0f, moment = 0.0f, share = 0.0f, cross = 0.0f;
@@ -370,10 +389,10 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const bool alive = z[c][j] > kNone, counts_here = !check || (j >= k.skip && k.base + j < A);   // an action counts once
-      const float d = z[c][j] - from, e = alive ? __expf(d) : 0.0f;
+      const float d = z[c][j] - from, e = __expf(d);   // 0 where it is not possible
       total += counts_here ? e : 0.0f;
       if (OP == kSample) {
-        const float score = a.second && !greedy ? z[c][j] + other[c][j] : z[c][j];
+        const float score = a.second ? z[c][j] + other[c][j] : z[c][j];
         const bool take = score > best;   // ascending within the lane: the lowest index among equals
         best = take ? score : best;
         best_z = take ? z[c][j] : best_z;
