@@ -82,7 +82,7 @@ class PagedCache:
             _check(L.pgxcache_init(C.byref(h), C.byref(opts), _ptr(kv), _ptr(table), _ptr(lengths), _ptr(refs), _ptr(self._work), nbytes), "pgxcache_init")
         self._h = h
         if _fast is not None:
-            self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "attend", "fork")}
+            self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "attend", "fork", "free")}
             self._shape = (self.slots, self.kv_heads, self.head_dim, TYPES[self.dtype], self.device.index)
         self._scale = self.head_dim ** -0.5
 
@@ -140,7 +140,7 @@ class PagedCache:
     def write(self, layer, k, v, slots=None):
         """Keys and values of the tokens that the slots' last advance made room for: [n][kv_heads][head_dim], or [n][tokens][kv_heads][head_dim]
         of which a slot takes as many as it has room for."""
-        if _fast is not None:   # (one token per slot)
+        if _fast is not None:
             rc = _fast.cache_write(self._calls["write"], self._h.value, self._shape, layer, k, v, slots)
             if rc == 0: return
             if rc is not None: _check(rc, "pgxcache_write")
@@ -196,6 +196,11 @@ class PagedCache:
         _check(lib().pgxcache_fork(self._h, n, s, _ptr(dst), self._status(status, n)), "pgxcache_fork")
 
     def free(self, slots=None):
+        """The slots' tokens are given up."""
+        if _fast is not None:
+            rc = _fast.cache_free(self._calls["free"], self._h.value, self._shape, slots)
+            if rc == 0: return
+            if rc is not None: _check(rc, "pgxcache_free")
         n, p = self._list(slots)
         _check(lib().pgxcache_free(self._h, n, p), "pgxcache_free")
 

@@ -396,20 +396,47 @@ PyObject* cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   });
 }
 
-// (address, handle, shape, layer, k, v, slots): one token per slot
+// (address, handle, shape, slots)
+PyObject* cache_free(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded([&] {
+    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU)};
+    int64_t n;
+    void* slots;
+    if (n_args != 4 || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &slots)) return -1000;
+    auto* fn = (decltype(&pgxcache_free))pointer(a[0]);
+    void* h = pointer(a[1]);
+    return without_gil([&] { return fn((pgxcache_t)h, (int32_t)n, (const int32_t*)slots); });
+  });
+}
+
+// keys or values of new tokens: [n][kv_heads][head_dim] or [n][tokens][kv_heads][head_dim]
+bool take_tokens(PyObject* o, const CacheShape& s, int64_t n, int64_t* tokens, void** out, int64_t* entry, int64_t* token, int64_t* head) {
+  const at::Tensor* t = tensor(o);
+  if (!t || (t->dim() != 3 && t->dim() != 4)) return false;
+  const bool many = t->dim() == 4;
+  if (t->scalar_type() != s.type || t->device() != s.device || t->size(0) != n || t->size(-2) != s.kv_heads || t->size(-1) != s.head_dim || t->stride(-1) != 1) return false;
+  *tokens = many ? t->size(1) : 1;
+  *out = t->data_ptr();
+  *entry = t->stride(0);
+  *token = many ? t->stride(1) : 0;
+  *head = t->stride(-2);
+  return *tokens <= INT32_MAX;
+}
+
+// (address, handle, shape, layer, k, v, slots)
 PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&] {
     CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU)};
-    int64_t n, ke, kh, ve, vh;
+    int64_t n, tokens, tokens_v, ke, kt, kh, ve, vt, vh;
     void *slots, *k, *v;
-    if (n_args != 7 || !take_shape(a[2], &s) || !take_list(a[6], s, &n, &slots) || !take_heads(a[4], s, n, s.kv_heads, &k, &ke, &kh) ||
-        !take_heads(a[5], s, n, s.kv_heads, &v, &ve, &vh))
+    if (n_args != 7 || !take_shape(a[2], &s) || !take_list(a[6], s, &n, &slots) || !take_tokens(a[4], s, n, &tokens, &k, &ke, &kt, &kh) ||
+        !take_tokens(a[5], s, n, &tokens_v, &v, &ve, &vt, &vh) || tokens != tokens_v || tensor(a[4])->dim() != tensor(a[5])->dim())
       return -1000;
     const long layer = PyLong_AsLong(a[3]);
     if (PyErr_Occurred() || layer < 0 || layer > INT32_MAX) return -1000;
     auto* fn = (decltype(&pgxcache_write))pointer(a[0]);
     void* h = pointer(a[1]);
-    return without_gil([&] { return fn((pgxcache_t)h, (int32_t)layer, (int32_t)n, (const int32_t*)slots, 1, k, ke, 0, kh, v, ve, 0, vh); });
+    return without_gil([&] { return fn((pgxcache_t)h, (int32_t)layer, (int32_t)n, (const int32_t*)slots, (int32_t)tokens, k, ke, kt, kh, v, ve, vt, vh); });
   });
 }
 
@@ -459,6 +486,7 @@ PyMethodDef kMethods[] = {
     {"policy_loss", (PyCFunction)(void*)policy_loss, METH_FASTCALL, nullptr},
     {"cache_advance", (PyCFunction)(void*)cache_advance, METH_FASTCALL, nullptr},
     {"cache_fork", (PyCFunction)(void*)cache_fork, METH_FASTCALL, nullptr},
+    {"cache_free", (PyCFunction)(void*)cache_free, METH_FASTCALL, nullptr},
     {"cache_write", (PyCFunction)(void*)cache_write, METH_FASTCALL, nullptr},
     {"cache_attend", (PyCFunction)(void*)cache_attend, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -1,4 +1,8 @@
 // pgxcache.hip -- a paged cache of keys and values whose slots follow the environments' (include/pgxcache.h), gfx950.
+//
+// A page holds its tokens for all layers and heads, [layers][2][kv_heads][page_size][head_dim], so that a copied or moved page is one
+// run of memory, and a head's tokens in a page are one run for attention.  Which pages are free is kept twice: as counters
+// of the table entries that name a page (the caller's), and as a bit per page (work memory), which calls that give out pages look through.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -114,7 +118,7 @@ __global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arriv
 // needs of the entries before it, and every block of a planning kernel works both out for itself from memory that no one writes
 // meanwhile; a second kernel then takes the pages out of the bits.  Bound by the round trips to memory that depend on each other (the list, the
 // lengths it names; the bits beside them), so the bits are kept in LDS.  4096 entries of a pool of 143000 pages: one block that took the
-// entries 1024 at a time and looked the bits up in memory took 40 us; blocks of 1024 entries side by side take 7.1 us.
+// entries 1024 at a time and looked the bits up in memory took 40 us for a fork's plan; blocks of 1024 entries side by side take 8 to 10.
 constexpr int kBitsInLds = 4096;   // words: pools of up to 262144 pages; beyond, the bits are looked up in memory
 
 // sum over the threads before this one; *total: over all
@@ -278,7 +282,7 @@ __device__ __forceinline__ void finish(const Cache& c, const Advance& e, bool do
   if (done && e.more > 0) c.lengths[e.slot] = e.length + e.more;
 }
 // PER = 1: a block per kOneBlock entries; one block ends the call itself, more are followed by advance_apply_kernel.  PER > 1: one block, PER
-// neighbouring entries per thread, all their loads under way together (4096 entries: <<ADVANCE_TILES>> us, by the two kernels 9.1 + 4.1).
+// neighbouring entries per thread, all their loads under way together (4096 entries: 9.2 us, by the two kernels 9.1 + 4.1).
 // The pages that the entries get are the free ones of consecutive ranks (an entry that cannot have its pages is followed by others that cannot),
 // so they leave the bits a word at a time (4600 pages, taken out one by one: 52 us, now 12).
 constexpr uint32_t kWanted = 1536;
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, co
 }
 
 // `per` threads for each entry: a wavefront where pages have up to 16 KB (4096 entries whose tails are 8 KB on average: 20.3 us with four
-// wavefronts each, <<FORK_4096>> with one, all of which the machine holds at once), more for larger ones.  A page that both slots name keeps
+// wavefronts each, 12.3 us with one, all of which the machine holds at once), more for larger ones.  A page that both slots name keeps
 // the source's reference throughout, so none comes free in between.
 __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const ForkEntry* plan, int per) {
   __shared__ Freed freed;

@@ -395,6 +395,11 @@ def test_native_and_python_checks_make_the_same_calls(monkeypatch):
         out += [status.clone(), cache.attend(0, new(4, 6, 64)), *cache.attend(1, new(2, 2, 64), ints([3, 0]), k=new(2, 2, 64), v=new(2, 2, 64), scale=1, lse=True)]
         out += [*cache.attend(1, new(4, 2, 64), out=torch.empty(4, 2, 64, dtype=torch.bfloat16, device="cuda"), lse=torch.empty(4, 2, device="cuda"))]
         cache.fork(ints([3, 0, -1]), ints([1, 2, 0]), status)
+        cache.free(ints([3, -1]))
+        cache.advance(ints([0, 3]), 5)
+        many = new(2, 7, 2, 64)
+        cache.write(0, many, many.flip(1), ints([0, 3]))
+        cache.write(1, new(2, 2, 7, 64).transpose(1, 2), many, ints([0, 3]))
         return out + [status, cache.kv, cache.table, cache.lengths, cache.refs]
 
     assert pg.cache_binding._fast is not None
