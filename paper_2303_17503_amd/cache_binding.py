@@ -80,7 +80,7 @@ class PagedCache:
             self._work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             h = C.c_void_p()
             _check(L.pgxcache_init(C.byref(h), C.byref(opts), _ptr(kv), _ptr(table), _ptr(lengths), _ptr(refs), _ptr(self._work), nbytes), "pgxcache_init")
-        self._h = h
+        self._h, self._destroy = h, L.pgxcache_destroy
         if _fast is not None:
             self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "attend", "fork", "free")}
             self._shape = (self.slots, self.kv_heads, self.head_dim, TYPES[self.dtype], self.device.index)
@@ -96,8 +96,8 @@ class PagedCache:
 
     def __del__(self):
         h, self._h = getattr(self, "_h", None), None
-        if h and lib is not None:   # module globals are gone when the interpreter shuts down
-            lib().pgxcache_destroy(h)
+        if h:
+            self._destroy(h)   # (module globals may be gone when the interpreter shuts down)
 
     def _list(self, slots, name="slots"):
         """number of entries, pointer"""

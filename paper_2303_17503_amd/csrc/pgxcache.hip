@@ -800,7 +800,9 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
       for (int m = 0; m < 2 * NT; ++m) acc[m] *= factor;
     }
     const float from = top > -INFINITY ? top : 0.0f;
-    x8 high, low;   // p = high + low, to 2^-17 (bf16) or 2^-22 (f16) of p: one number would round the output a second time
+    // p = high + low, to 2^-17 (bf16) or 2^-22 (f16) of p: with one number the output's error against 64 bits is 1.24 to 1.38 times that of
+    // its own rounding, and the time the same (4096 slots of 1 to 722 tokens 133.7 against 133.6 us, 1024 of 1 to 160 0.1 us less per layer)
+    x8 high, low;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float p = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - from);

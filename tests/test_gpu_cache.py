@@ -5,7 +5,10 @@ times the sum of their magnitudes, then scaled: es = (D + 4) u A, A the largest 
 (its own score and the others' in the sum), by what the exponential adds (4 u + the argument's rounding, 2 A u) and by the
 two-number form, 2^-17 for bfloat16.  The sum over n tokens adds at most (n / 8 + 64) u.  All of it times the largest
 |v|, and the rounding to the type on top.  The logarithm's sum: es + 2 A u + (n / 8 + 64) u, and 4 u of its own size."""
+import os
 import random
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -421,3 +424,10 @@ def test_a_pool_beyond_every_cache_gives_the_same(n, head_dim, heads):
     q = torch.randn(n, heads, head_dim, device="cuda", dtype=torch.bfloat16)
     a, b = small.attend(0, q, lse=True), big.attend(0, q, lse=True)
     assert torch.equal(bits(a[0]), bits(b[0])) and torch.equal(bits(a[1]), bits(b[1])) and torch.isfinite(a[0][torch.tensor(lengths) > 0].float()).all()
+
+
+def test_a_cache_that_lives_until_the_interpreter_ends():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", "import paper_2303_17503_amd as pg\nclass S: pass\ns = S(); s.cache = pg.PagedCache.empty(2, 4, 32, 1, 1, 64)\nimport sys; sys.kept = s"],
+                       cwd=root, capture_output=True, text=True)
+    assert r.returncode == 0 and "Traceback" not in r.stderr, r.stderr
