@@ -65,7 +65,7 @@ int pgxpolicy_logits(int32_t rows, int32_t actions, const void* logits_dev, int3
 
 /* actions_dev[b] = the possible action with the largest z + noise[b][a] (in 32 bits; the lowest index among equals), and
  * logp_dev[b] (may be NULL) its log-probability under softmax(z).  noise_dev: float32, pitch in elements, NULL: none; with
- * Gumbel noise, -log(-log u), the action is a draw from softmax(z).  An action whose noise is NaN is taken only if no other is possible.
+ * Gumbel noise, -log(-log u), the action is a draw from softmax(z).  Noise that is NaN counts as -infinity.
  * A row without possible actions gets action -1, which the environments' step calls leave untouched, and log-probability 0. */
 int pgxpolicy_sample(int32_t rows, int32_t actions, const void* logits_dev, int32_t type, int64_t logits_pitch, const pgxpolicy_adjust* adjust,
                      const float* noise_dev, int64_t noise_pitch, int32_t* actions_dev, float* logp_dev, void* stream);

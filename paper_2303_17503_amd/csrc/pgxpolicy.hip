@@ -5,7 +5,7 @@
 // bytes they move; 16 lanes per row (rather than the wavefront) let a row's reductions run on four rows at once by DPP rotations
 // inside the 16-lane rows, and 3 chunks x 16 lanes x 8 hold the 362 actions of 19x19 with 6 % of the lanes' slots idle.
 //
-// Measured: the loss of 65536 x 362 logits in bfloat16 29.5 us, 4.1 TB/s of what it has to move; 16384 x 122 log-probabilities 5.2 us; sampling of
+// Measured: the loss of 65536 x 362 logits in bfloat16 25.8 us, 4.6 TB/s of what it has to move; 16384 x 122 log-probabilities 5.2 us; sampling of
 // 65536 x 362 with records of up to 361 plies, [plies][games], 75 us, 3.3 TB/s (vector instructions keep 60 % of the time busy, and waves
 // that wait for moves the rest: blocks of 8, 32 and 64 rows instead of 16 take 82, 85 and 104 us).
 #include <hip/hip_runtime.h>
@@ -294,7 +294,8 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
   const bool greedy = !(own_temperature > 0.0f);
   const float temperature = greedy ? 1.0f : own_temperature;
   const float weight = kLoss && a.weight ? a.weight[b] : 1.0f;
-  const int taken = OP == kLossMoves ? a.taken[b] : -1;
+  int taken = OP == kLossMoves ? a.taken[b] : -1;
+  if ((uint32_t)taken >= (uint32_t)A) taken = -1;
   if (RECORD) part.count(a, counts, words);
 
   // the adjustment, a step at a time over all of the lane's actions
@@ -362,15 +363,11 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
     }
     return;
   }
-  // from here on an action that is not possible has z = -infinity
-  float top = kNone;
+  float top = kNone;   // (NaN, which is not possible, is left out; what a last chunk shares with the one before it may count twice here)
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      z[c][j] = fmaxf(z[c][j], kNone);   // NaN is not possible
-      top = fmaxf(top, z[c][j]);         // (what a last chunk shares with the one before it may count twice here)
-    }
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, z[c][j]);
   top = reduced<Max, G>(top, shared);
   const bool some = top > kNone;
   const float from = some ? top : 0.0f;
@@ -382,19 +379,22 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
       for (int j = 0; j < 8; ++j) other[c][j] = greedy ? 0.0f : other[c][j];
   }
 
-  // sums over the possible actions: of e = exp(z - top), and for the loss of e (z - top), y and y (z - top)
-  float total = 0.0f, moment = 0.0f, share = 0.0f, cross = 0.0f;
+  // Sums over the possible actions: of e = exp(d), d = z - top, and for the loss of e d, y and y d.  Where an action is not possible d is set to a finite
+  // number far below any that matters, so that e is 0 and products with it are.
+  constexpr float kFar = -1e30f;
+  float total = 0.0f, moment = 0.0f, share = 0.0f, cross = 0.0f, found = kNone;   // found: d of the move that was taken
   float best = kNone, best_z = kNone;
   int best_at = 0x7FFFFFFF;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const Chunk k(c * G + lane, A);
     const bool check = !FULL || c == NC - 1;
+    const int rel = taken - k.base;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool alive = z[c][j] > kNone, counts_here = !check || (j >= k.skip && k.base + j < A);   // an action counts once
-      const float d = z[c][j] - from, e = __expf(d);   // 0 where it is not possible
-      total += counts_here ? e : 0.0f;
+      const bool counts_here = !check || (j >= k.skip && k.base + j < A);   // an action counts once
+      const float raw = z[c][j] - from, d = fmaxf(raw, kFar), e = __expf(d), counted = counts_here ? e : 0.0f;
+      total += counted;
       if (OP == kSample) {
         const float score = a.second ? z[c][j] + other[c][j] : z[c][j];
         const bool take = score > best;   // ascending within the lane: the lowest index among equals
@@ -403,14 +403,16 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
         best_at = take ? k.base + j : best_at;
       }
       if (kLoss) {
-        const float safe = alive ? d : 0.0f, counted = counts_here ? e : 0.0f;
-        const float y = OP == kLossShares ? (alive ? other[c][j] : 0.0f) : (alive && k.base + j == taken ? 1.0f : 0.0f);
-        const float y_counted = counts_here ? y : 0.0f;
-        moment += counted * safe;
-        share += y_counted;
-        cross += y_counted * safe;
-        z[c][j] = safe;
-        other[c][j] = alive ? y : kNone;   // marks those that are not possible
+        moment = __builtin_fmaf(counted, d, moment);
+        if (OP == kLossShares) {
+          const float y = z[c][j] > kNone ? other[c][j] : 0.0f, y_counted = counts_here ? y : 0.0f;
+          other[c][j] = y;
+          share += y_counted;
+          cross = __builtin_fmaf(y_counted, fmaxf(raw, -3e38f), cross);
+        } else {
+          found = rel == j ? raw : found;
+        }
+        z[c][j] = d;
       }
     }
   }
@@ -449,30 +451,41 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
   }
   if (kLoss) {
     moment = reduced<Sum, G>(moment, shared);
-    share = reduced<Sum, G>(share, shared);
-    cross = reduced<Sum, G>(cross, shared);
+    if (OP == kLossShares) {
+      share = reduced<Sum, G>(share, shared);
+      cross = reduced<Sum, G>(cross, shared);
+    } else {
+      found = reduced<Max, G>(fmaxf(found, kNone), shared);
+      share = found > kNone ? 1.0f : 0.0f;
+      cross = found > kNone ? found : 0.0f;
+    }
     const float inverse = some ? 1.0f / total : 0.0f;
     const float entropy = some ? log_total - moment * inverse : 0.0f;
     if (mine && lane == 0) {
       if (a.row_out) a.row_out[b] = some ? weight * (share * log_total - cross) - a.entropy_bonus * entropy : 0.0f;
       if (a.row_out2) a.row_out2[b] = entropy;
     }
-    // with p = e / total:  weight (share p - y) + bonus p (d - log_total + entropy)  =  p (bonus d + level) - weight y
-    const float slope = a.grad_scale / temperature, level = some ? weight * share + a.entropy_bonus * (entropy - log_total) : 0.0f;
-    const float bend = a.entropy_bonus;
-    const float pull = weight * slope, each = inverse * slope;
+    // with p = e / total:  weight (share p - y) + bonus p (d - log_total + entropy)  =  e (bend d + level) - pull y
+    const float slope = a.grad_scale / temperature, pull = weight * slope, each = inverse * slope, bend = a.entropy_bonus * each;
+    const float level = some ? (weight * share + a.entropy_bonus * (entropy - log_total)) * each : 0.0f;
     if (mine) {
+      Elem* row = (Elem*)a.out + (int64_t)b * a.out_pitch;
+      auto through = [&](int c, int j, float g) {   // back through the penalty for repeated moves
+        return RECORD && (seen[c] >> j & 1u) ? (positive[c] >> j & 1u ? g / a.repetition : g * a.repetition) : g;
+      };
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
+        const Chunk k(c * G + lane, A);
         float out[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float d = z[c][j], e = __expf(d);
-          float g = e * each * __builtin_fmaf(bend, d, level) - pull * other[c][j];
-          if (RECORD) g = seen[c] >> j & 1u ? (positive[c] >> j & 1u ? g / a.repetition : g * a.repetition) : g;
-          out[j] = other[c][j] > kNone ? g : 0.0f;
+          const float g = __expf(z[c][j]) * __builtin_fmaf(bend, z[c][j], level);
+          out[j] = through(c, j, OP == kLossShares ? __builtin_fmaf(-pull, other[c][j], g) : g);
         }
-        store_chunk<T>((Elem*)a.out + (int64_t)b * a.out_pitch, Chunk(c * G + lane, A), A, out);
+        store_chunk<T>(row, k, A, out);
+        const int rel = taken - k.base;
+        if (OP == kLossMoves && (uint32_t)rel < 8u && k.at < A && found > kNone)   // the move that was taken is written once more
+          row[k.base + rel] = (Elem)through(c, rel, __expf(found) * __builtin_fmaf(bend, fmaxf(found, kFar), level) - pull);
       }
     }
   }

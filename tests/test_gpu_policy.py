@@ -157,6 +157,38 @@ def test_masks_of_the_lowest_value_and_of_minus_infinity_in_the_bias():
     assert abs(float(entropy[2]) - math.log(4.0)) <= 200 * U
 
 
+@pytest.mark.parametrize("actions", [5, 82, 362, 700])
+def test_nan_logits_are_not_possible_and_nan_noise_counts_as_minus_infinity(actions):
+    rows, nan, inf = 12, float("nan"), float("inf")
+    x, how, g = inputs(rows, actions, "f32", 31, record=15)
+    how["mask"][:] = 1
+    hurt = torch.rand(rows, actions, generator=g).cuda() < 0.3
+    hurt[:, actions // 2] = False
+    y = torch.where(hurt, torch.full_like(x, nan), x)
+    without = {**how, "mask": (~hurt).to(torch.uint8)}                 # the same with those actions masked
+    raw = pg.adjust_logits(y, **how)
+    assert torch.isnan(raw[hurt]).all() and torch.equal(raw[~hurt], pg.adjust_logits(x, **how)[~hurt])
+    noise = torch.randn(rows, actions, generator=g).cuda()
+    target, moves = torch.rand(rows, actions, generator=g).cuda(), torch.randint(0, actions, (rows,), generator=g, dtype=torch.int32).cuda()
+    for f in (lambda l, h: [pg.adjust_logits(l, normalize=True, **h)], lambda l, h: pg.sample_actions(l, noise=noise, **h),
+              lambda l, h: pg.policy_loss(l, target, entropy=0.1, **h), lambda l, h: pg.policy_loss(l, moves, entropy=0.1, **h)):
+        for a, b in zip(f(y, how), f(x, without)):
+            assert torch.equal(a + 0, b + 0)
+    odd = noise.clone()
+    odd[:, ::2] = nan
+    odd[:, 1::2] = -inf
+    odd[0, actions - 1] = -1e30
+    odd[1] = nan
+    how["temperature"] = torch.ones(rows, device="cuda")
+    a, logp = pg.sample_actions(y, noise=odd, **how)
+    first = [int((~hurt[b]).nonzero()[0]) for b in range(rows)]
+    if not hurt[0, actions - 1]:
+        first[0] = actions - 1
+    assert a.tolist() == first and torch.isfinite(logp).all()
+    odd[2, actions // 2] = inf
+    assert pg.sample_actions(y, noise=odd, **how)[0][2] == actions // 2
+
+
 @pytest.mark.parametrize("target", ["visits", "moves"])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("actions", [1, 3, 8, 13, 82, 122, 362, 385, 2048, 5000])
