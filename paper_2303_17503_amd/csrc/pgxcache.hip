@@ -282,7 +282,8 @@ __device__ __forceinline__ void finish(const Cache& c, const Advance& e, bool do
   if (done && e.more > 0) c.lengths[e.slot] = e.length + e.more;
 }
 // PER = 1: a block per kOneBlock entries; one block ends the call itself, more are followed by advance_apply_kernel.  PER > 1: one block, PER
-// neighbouring entries per thread, all their loads under way together (4096 entries: 9.2 us, by the two kernels 9.1 + 4.1).
+// neighbouring entries per thread, all their loads under way together, for up to 4096 entries that get one page each at most (of one token
+// more each: 11.9 us, by the two kernels 12.9; 1 to 39 tokens more, 7300 pages: 28.0 by one block, 15.9 by the two kernels, and 22.9 / 15.2 for 2048 entries).
 // The pages that the entries get are the free ones of consecutive ranks (an entry that cannot have its pages is followed by others that cannot),
 // so they leave the bits a word at a time (4600 pages, taken out one by one: 52 us, now 12).
 constexpr uint32_t kWanted = 1536;
@@ -396,24 +397,31 @@ __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, co
     int s, d, length;
     bool slots, nothing, need;
   };
-  auto look = [&](int i) {
+  auto look = [&](int i) {   // (loads without a condition, as above)
     Look e;
-    e.s = i < n ? src[i] : -1;
-    e.d = i < n ? dst[i] : -1;
+    const int at = min(i, n - 1), s = src[at], d = dst[at];
+    e.s = i < n ? s : -1;
+    e.d = i < n ? d : -1;
     e.slots = (uint32_t)e.s < (uint32_t)c.slots && (uint32_t)e.d < (uint32_t)c.slots;
     e.nothing = e.s == e.d || e.s == -1 || e.d == -1;
-    e.length = e.slots ? c.length(e.s) : 0;
+    const int length = c.length(e.slots ? e.s : 0);
+    e.length = e.slots ? length : 0;
     e.need = e.slots && !e.nothing && (e.length & ((1 << c.page_shift) - 1)) != 0;
     return e;
   };
   const int i = (int)blockIdx.x * kOneBlock + (int)threadIdx.x;
   const Look e = look(i);
-  const int last = e.need ? c.row(e.s)[e.length >> c.page_shift] : -1, old = e.slots ? c.pages_of(c.length(e.d)) : 0;
+  const int page = c.row(e.need ? e.s : 0)[e.need ? e.length >> c.page_shift : 0], had = c.pages_of(c.length(e.slots ? e.d : 0));
+  const int last = e.need ? page : -1, old = e.slots ? had : 0;
   uint32_t before = 0, all;
   if (blockIdx.x > 0) {
     uint32_t sum = 0;
-#pragma unroll 4
-    for (int k = 0; k < (int)blockIdx.x; ++k) sum += look(k * kOneBlock + (int)threadIdx.x).need;
+    for (int k0 = 0; k0 < (int)blockIdx.x; k0 += 4)   // four blocks' entries under way together (65536 entries: 85 -> 78 us)
+#pragma unroll
+      for (int k = k0; k < k0 + 4; ++k) {
+        const bool need = look(min(k, (int)blockIdx.x - 1) * kOneBlock + (int)threadIdx.x).need;
+        sum += need && k < (int)blockIdx.x;
+      }
     exclusive_sum(sum, shared, &before);
   }
   const uint32_t rank = before + exclusive_sum(e.need, shared, &all);
@@ -1122,7 +1130,7 @@ int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const in
   if (n == 0) return PGXCACHE_OK;
   const hipStream_t stream = (hipStream_t)h->o.stream;
   const Cache c = cache_of(h);
-  if (n <= 4 * kOneBlock) {   // one launch
+  if (n <= kOneBlock || (n <= 4 * kOneBlock && !counts_dev && count <= h->o.page_size)) {   // one launch (counts: prompts, of any number of pages)
     if (n <= kOneBlock) hipLaunchKernelGGL((advance_kernel<1, true>), dim3(1), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
     else hipLaunchKernelGGL((advance_kernel<4, true>), dim3(1), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
     HIPCHK(hipGetLastError());

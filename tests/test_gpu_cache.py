@@ -246,6 +246,26 @@ def test_all_slots_by_default_and_more_entries_than_a_block():
     assert int(cache.refs.sum()) == 0 and int(cache.lengths.sum()) == 0 and (cache.table == -1).all()
 
 
+@pytest.mark.parametrize("n", [1024, 1025, 2900, 4096, 4097])
+@pytest.mark.parametrize("pages", [1300, 9000])
+def test_one_count_for_many_entries(n, pages):
+    """Few and many new pages, up to one per entry and more, in a pool that runs out in the middle of the entries."""
+    slots = 4100
+    cache = pg.PagedCache.empty(slots, pages, 64, 1, 1, 32, 16, torch.float16)
+    cache.kv.zero_()
+    ref, r = ref_of(cache), random.Random(n)
+    start = [r.choice([0, 1, 8, 14, 15]) for _ in range(slots)]
+    cache.advance(counts=ints(start))
+    ref.advance(range(slots), start)
+    for count in (1, 0, 1, 16, 17, 1):
+        entries = r.sample(range(slots), n)
+        entries = [r.choice([-1, -4, slots]) if r.random() < 0.02 else s for s in entries]
+        status = torch.full((n,), 99, dtype=torch.uint8, device="cuda")
+        cache.advance(ints(entries), count, status)
+        assert status.tolist() == ref.advance(entries, [count] * n)
+        same(cache, ref)
+
+
 @pytest.mark.parametrize("n", [5, 4200])
 @pytest.mark.parametrize("length", [0, 15, 16, 31, 32, 100])
 def test_attention_that_writes_the_new_token(length, n):
