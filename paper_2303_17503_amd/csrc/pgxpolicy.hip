@@ -219,7 +219,7 @@ struct RecordPart {
     for (int i = (int)threadIdx.x; i < threads / G * words; i += threads) counts[i] = 0;
     __syncthreads();
     uint32_t* mine = counts + row * words;
-    int t = max(from, 0) + first;
+    int t = min(max(from, 0), a.record_len) + first;   // (a begin of the largest int32 is "no ply": the sum must not wrap)
     const int end = min(to, a.record_len);
     auto add = [&](int move, bool there) {
       if (there && (uint32_t)move < (uint32_t)a.actions) atomicAdd(&mine[move >> 1], 1u << (16 * (move & 1)));

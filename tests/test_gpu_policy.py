@@ -395,3 +395,30 @@ def test_native_and_python_checks_make_the_same_calls(actions, monkeypatch):
     monkeypatch.setattr(pg.policy_binding, "_fast", None)
     for a, b in zip(native, every()):
         assert a.dtype == b.dtype and torch.equal(a.view(torch.int16 if a.dtype == torch.bfloat16 else torch.int32), b.view(torch.int16 if b.dtype == torch.bfloat16 else torch.int32))
+
+
+@pytest.mark.parametrize("layout", ["plies", "games", "far"])
+@pytest.mark.parametrize("actions", [82, 700, 3000])
+def test_begins_and_ends_at_the_limits_of_their_type(actions, layout):
+    """max(begin, 0) <= t < min(end, plies) for every int32; with 16, 64 and 256 lanes to a row; "far": moves beyond 32-bit offsets in bytes"""
+    low, high = -2 ** 31, 2 ** 31 - 1
+    ranges = [(high, high), (high, low), (low, high), (low, low), (high - 3, high), (high - 15, 7), (high - 254, high), (0, high), (6, high), (7, high), (8, 8), (high, 7), (-1, 1)]
+    rows, plies = 2 if layout == "far" else len(ranges), 9
+    g = torch.Generator().manual_seed(actions)
+    moves = torch.randint(0, 5, (len(ranges), plies), generator=g, dtype=torch.int32).cuda()
+    x = torch.randn(len(ranges), actions, generator=g).cuda()
+    begin, end = (torch.tensor([r[i] for r in ranges], dtype=torch.int64).int().cuda() for i in (0, 1))
+    how = dict(repetition=1.5, frequency=0.25, presence=0.5)
+    if layout == "far":
+        memory = torch.full((2 ** 29 + plies,), -1, dtype=torch.int32, device="cuda")
+    for first in range(0, len(ranges), rows):
+        part = slice(first, min(first + rows, len(ranges)))
+        record = moves[part]
+        n = record.shape[0]
+        if layout == "games": record = record.t().contiguous().t()
+        if layout == "far":
+            far = memory.as_strided((n, plies), (2 ** 29, 1))
+            record = far.copy_(record)
+        now = dict(how, record=record, begin=begin[part], end=end[part])
+        want, _ = ref.adjusted(x[part], dtype=torch.float32, **dict(now, record=moves[part]))
+        assert torch.equal(bits(pg.adjust_logits(x[part], **now).cpu()), bits(want))
