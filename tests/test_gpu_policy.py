@@ -422,3 +422,24 @@ def test_begins_and_ends_at_the_limits_of_their_type(actions, layout):
         now = dict(how, record=record, begin=begin[part], end=end[part])
         want, _ = ref.adjusted(x[part], dtype=torch.float32, **dict(now, record=moves[part]))
         assert torch.equal(bits(pg.adjust_logits(x[part], **now).cpu()), bits(want))
+
+
+@pytest.mark.parametrize("target", ["visits", "moves"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("actions", [5, 82, 362, 700, 3000])
+def test_the_gradient_is_0_where_an_action_is_not_possible(actions, dtype, target):
+    """whatever the temperature, the scale and the bonus multiply to, and beside a logit of +infinity, which makes the possible ones NaN"""
+    rows = 14
+    x, how, g = inputs(rows, actions, "f32", 50 + actions, record=12)
+    how["mask"][:, actions // 2] = 1
+    x, dead = x.to(TYPES[dtype]), how["mask"][:, :actions] == 0
+    y = torch.rand(rows, actions, generator=g).cuda() if target == "visits" else torch.randint(-1, actions, (rows,), generator=g, dtype=torch.int32).cuda()
+    for t, scale, bonus in ((1e-4, 65536.0, 1.0), (1e-6, 65536.0, 0.01), (1e-30, 1.0, 0.5), (1e-36, 1e9, 0.5), (1.0, 3e38, 3e38), (0.5, -65536.0, 1e30)):
+        how["temperature"] = torch.full((rows,), t, device="cuda")
+        grad = pg.policy_loss(x, y, entropy=bonus, grad_scale=scale, **how)[2]
+        assert (grad[dead] == 0).all() and (scale / t > 1e12 or not torch.isnan(grad).any()), (t, scale, bonus)
+    how["temperature"] = torch.ones(rows, device="cuda")
+    x[:, actions // 2] = float("inf")
+    for bonus in (0.0, 0.1):
+        loss, entropy, grad = pg.policy_loss(x, y, entropy=bonus, **how)
+        assert (grad[dead] == 0).all() and torch.isnan(grad[~dead]).all() and torch.isnan(loss).all() and torch.isnan(entropy).all()
