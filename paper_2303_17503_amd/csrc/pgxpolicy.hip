@@ -370,8 +370,9 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
     for (int j = 0; j < 8; ++j) top = fmaxf(top, z[c][j]);
   top = reduced<Max, G>(top, shared);
   const bool some = top > kNone;
+  constexpr float kLowest = -0x1.fffffep127f;   // the lowest finite number
   // (the loss: beside a logit of +infinity, which makes the row NaN, z - from is at least 0 for every possible action, so that these are told from the others)
-  const float from = !some ? 0.0f : !kLoss || top < INFINITY ? top : -0x1.fffffep127f;
+  const float from = !some ? 0.0f : !kLoss || top < INFINITY ? top : kLowest;
 
   if (OP == kSample && a.second && __any(greedy)) {
 #pragma unroll
@@ -383,7 +384,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
   // Sums over the possible actions: of e = exp(d), d = z - top, and for the loss of e d, y and y d.  d is kept at or above kFar, where e is 0
   // already (below -104 it is in 32 bits), so that an action that is not possible adds 0 to each of them.
   constexpr float kFar = -256.0f;
-  float total = 0.0f, moment = 0.0f, share = 0.0f, cross = 0.0f, found = kNone;   // found: d of the move that was taken
+  float total = 0.0f, moment = 0.0f, share = 0.0f, cross = 0.0f, found = kNone;   // found: z, later z - top, of the move that was taken
   float best = kNone, best_z = kNone;
   int best_at = 0x7FFFFFFF;
 #pragma unroll
@@ -409,9 +410,9 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
           const float y = z[c][j] > kNone ? other[c][j] : 0.0f, y_counted = counts_here ? y : 0.0f;
           other[c][j] = y;
           share += y_counted;
-          cross = __builtin_fmaf(y_counted, fmaxf(raw, -3e38f), cross);
+          cross = __builtin_fmaf(y_counted, fmaxf(raw, kLowest), cross);   // (a finite number: y is 0 where the action is not possible)
         } else {
-          found = rel == j ? raw : found;
+          found = rel == j ? z[c][j] : found;
         }
         z[c][j] = d;
       }
@@ -457,6 +458,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
       cross = reduced<Sum, G>(cross, shared);
     } else {
       found = reduced<Max, G>(fmaxf(found, kNone), shared);
+      found = found > kNone ? fmaxf(found - from, kLowest) : kNone;
       share = found > kNone ? 1.0f : 0.0f;
       cross = found > kNone ? found : 0.0f;
     }

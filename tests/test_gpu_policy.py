@@ -443,3 +443,23 @@ def test_the_gradient_is_0_where_an_action_is_not_possible(actions, dtype, targe
     for bonus in (0.0, 0.1):
         loss, entropy, grad = pg.policy_loss(x, y, entropy=bonus, **how)
         assert (grad[dead] == 0).all() and torch.isnan(grad[~dead]).all() and torch.isnan(loss).all() and torch.isnan(entropy).all()
+
+
+@pytest.mark.parametrize("actions", [4, 82, 700])
+def test_the_loss_at_logits_of_the_lowest_value(actions):
+    """A mask of the type's lowest value leaves the action possible, with a log-probability of about that value: the loss for a target there is as large,
+    to one rounding each of the difference, its product with the share and the weight (4 u), and beside the highest value it is capped there."""
+    low, high = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+    x = torch.randn(6, actions, generator=torch.Generator().manual_seed(1))
+    x[:, 1] = torch.tensor([low, low, -3.1e38, -2.9e38, low, low])
+    x[4, 2] = x[5, 2] = high
+    share = torch.zeros(6, actions)
+    share[:, 1], share[:, 0] = 0.25, 0.5
+    want = -x[:, 1].double() + torch.tensor([0, 0, 0, 0, high, high]).double()   # (what lies beside it is below its rounding)
+    want = torch.minimum(want, torch.full_like(want, high))
+    loss = pg.policy_loss(x.cuda(), torch.full((6,), 1, dtype=torch.int32, device="cuda"))[0].cpu().double()
+    assert ((loss - want).abs() <= 4 * U * want).all()
+    loss, _, grad = pg.policy_loss(x.cuda(), share.cuda(), entropy=0.25)
+    loss = loss[:4].cpu().double()
+    assert ((loss - 0.25 * want[:4]).abs() <= 4 * U * want[:4]).all()
+    assert torch.isfinite(grad).all() and (grad[:, 1] == -0.25).all()
