@@ -245,10 +245,10 @@ struct RecordPart {
 };
 
 // x / d, rounded to nearest, for a d whose reciprocal y is: the product's error is found exactly and taken off (P. Markstein, 1990: with y
-// correctly rounded is).  3 instructions instead of 11; below 2^-100 the last bit may differ.  For |x| up to 2^100 and d from 2^-20 to 2^20.
+// correctly rounded is).  3 instructions instead of 11; quotients below 2^-100 may differ in the last bit.  For |x| up to 2^100 and d from 2^-20 to 2^20.
 __device__ __forceinline__ float divided(float x, float d, float y) {
   const float q = x * y;
-  return __builtin_fmaf(__builtin_fmaf(-q, d, x), y, q);
+  return __builtin_fmaf(-__builtin_fmaf(q, d, -x), y, q);   // (the error's negative, so that -0 stays -0)
 }
 __device__ __forceinline__ bool plain_divisor(float d) { return d >= 0x1p-20f && d <= 0x1p20f; }
 template <int NC>

@@ -463,3 +463,17 @@ def test_the_loss_at_logits_of_the_lowest_value(actions):
     loss = loss[:4].cpu().double()
     assert ((loss - 0.25 * want[:4]).abs() <= 4 * U * want[:4]).all()
     assert torch.isfinite(grad).all() and (grad[:, 1] == -0.25).all()
+
+
+@pytest.mark.parametrize("divisor", ["temperature", "repetition", "both"])
+def test_the_sign_of_zero_is_kept(divisor):
+    """every operation rounded by itself: -0 / T is -0; to the bit, zeros of both signs beside numbers of all sizes"""
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(9, 82, generator=g) * 2.0 ** torch.randint(-60, 60, (9, 82), generator=g)
+    x[:, ::3], x[:, 1::6] = -0.0, 0.0
+    x = x.cuda()
+    how = {} if divisor == "repetition" else {"temperature": torch.rand(9, generator=g).cuda() + 0.3}
+    if divisor != "temperature":
+        how.update(record=torch.randint(0, 82, (9, 60), generator=g, dtype=torch.int32).cuda(), repetition=1.3)
+    want = ref.adjusted(x, dtype=torch.float32, **how)[0]
+    assert torch.equal(bits(pg.adjust_logits(x, **how).cpu()), bits(want)) and torch.signbit(want[want == 0]).any()
