@@ -87,7 +87,7 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
  * last token, [i][head][.], written to the cache by this call where the slot's last pgxcache_advance made room for it (and otherwise
  * ignored), so that a step takes one launch per layer; without them entries may repeat.  A slot without tokens, and an entry that is no slot, gives zeros and -infinity.
  * Scores, sums and the output before its rounding are held in 32 bits; probabilities are multiplied as two numbers of the
- * cache's type that add up to them. */
+ * cache's type that add up to them within 2^-17 (float16: of the sum of 32 tokens' probabilities), however small they are. */
 int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t heads, const void* q_dev, int64_t q_entry_stride,
                     int64_t q_head_stride, const void* k_dev, int64_t k_entry_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride,
                     int64_t v_head_stride, float scale, void* out_dev, int64_t out_entry_stride, int64_t out_head_stride, float* lse_dev);

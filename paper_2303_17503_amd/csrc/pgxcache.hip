@@ -641,21 +641,29 @@ struct AttendArgs {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_4 __attribute__((aligned(4)));
 
+// Probabilities go into the second product as two numbers of the type that add up to them, relative to an exponent that is moved only when a tile
+// requires it, so that most tiles need no exchange between lanes.
+//  * bfloat16 has the range of 32 bits: the sum is within 2^-17 of p whatever its size.  The exponent is the running maximum, raised when a score passes it by 2^8.
+//  * float16 ends at 65504 and at steps of 2^-24: the sum is within 2^-22 of p or within 2^-25.  The exponent goes up and down with the tiles, so that the
+//    largest p of a head in a tile is between 2^-3 and 2^15 (2^11 where it is moved), and the tile's 32 errors add up to 2^-17 of the tile's sum at most.  It goes no further down than 2^60
+//    below the largest score, where nothing counts any more and the sums stay far from the end of 32 bits.  With the running maximum for exponent, p
+//    below 2^-25 of it was lost (721 tokens at e^-15 beside one: 0.7 % of what they add), and the time is the same.
 struct F16 {
   typedef _Float16 elem;
+  static constexpr bool kNarrow = true;
+  static constexpr float kRoom = 11.0f, kMost = 15.0f, kLeast = -3.0f, kDepth = 60.0f;
   typedef elem x8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 struct BF16 {
   typedef __bf16 elem;
+  static constexpr bool kNarrow = false;
+  static constexpr float kRoom = 0.0f, kMost = 8.0f, kLeast = 0.0f, kDepth = 0.0f;
   typedef elem x8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
 constexpr float kLn2 = 0.69314718055994530942f;
-// The running maximum is raised only when a score passes it by 2^8: probabilities up to that are exact enough in either type (they are
-// held as two numbers), and the tiles' maxima need no exchange between lanes.
-constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ float across_groups_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -750,7 +758,8 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
 #pragma unroll
   for (int m = 0; m < NT; ++m) q[m] = __builtin_bit_cast(x8, col < heads_here ? query[m] : u32x4{0, 0, 0, 0});
 
-  float top = -INFINITY, sum = 0.0f;   // of the lane's head: the maximum that all four groups use, and this group's sum
+  float top = -INFINITY, sum = 0.0f;   // of the lane's head: the exponent that all four groups use, and this group's sum
+  float peak = -INFINITY;              // kNarrow: the largest score when the exponent was last moved
   f32x4 acc[2 * NT];
 #pragma unroll
   for (int m = 0; m < 2 * NT; ++m) acc[m] = f32x4{0, 0, 0, 0};
@@ -799,8 +808,17 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
         }
     }
     float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    if (__any(most > top + kSlack)) {
-      const float now = across_groups_max(fmaxf(most, top));
+    const bool below = T::kNarrow && most < top + T::kLeast && most > -INFINITY && top > peak - (T::kDepth + T::kRoom);
+    if (__any(most > top + T::kMost || below)) {
+      float now;
+      if (T::kNarrow) {
+        const float here = across_groups_max(most);   // the tile's largest score
+        peak = fmaxf(peak, here);
+        const bool move = here > top + T::kMost || (here < top + T::kLeast && here > -INFINITY);
+        now = move ? fmaxf(here, peak - T::kDepth) - T::kRoom : top;
+      } else {
+        now = across_groups_max(fmaxf(most, top));
+      }
       const float factor = now > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 1.0f;
       top = now;
       sum *= factor;
@@ -808,8 +826,7 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
       for (int m = 0; m < 2 * NT; ++m) acc[m] *= factor;
     }
     const float from = top > -INFINITY ? top : 0.0f;
-    // p = high + low, to 2^-17 (bf16) or 2^-22 (f16) of p: with one number the output's error against 64 bits is 1.24 to 1.38 times that of
-    // its own rounding, and the time the same (4096 slots of 1 to 722 tokens 133.7 against 133.6 us, 1024 of 1 to 160 0.1 us less per layer)
+    // with one number for p the output's error against 64 bits is 1.24 to 1.38 times that of its own rounding, and the time the same (4096 slots of 1 to 722 tokens 133.7 against 133.6 us, 1024 of 1 to 160 0.1 us less per layer)
     x8 high, low;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
