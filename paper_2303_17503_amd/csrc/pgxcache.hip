@@ -122,21 +122,22 @@ __global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arriv
 constexpr int kBitsInLds = 4096;   // words: pools of up to 262144 pages; beyond, the bits are looked up in memory
 
 // sum over the threads before this one; *total: over all
-__device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* shared /* kOneBlock / 64 words */, uint32_t* total) {
+template <class U>
+__device__ __forceinline__ U exclusive_sum(U x, U* shared /* kOneBlock / 64 numbers */, U* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t s = x;
+  U s = x;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t up = __shfl_up(s, d);
+    const U up = __shfl_up(s, d);
     if (lane >= d) s += up;
   }
   __syncthreads();
   if (lane == 63) shared[wave] = s;
   __syncthreads();
-  uint32_t before = 0, all = 0;
+  U before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kOneBlock / 64; ++w) {
-    const uint32_t v = shared[w];
+    const U v = shared[w];
     before += w < wave ? v : 0;
     all += v;
   }
@@ -300,15 +301,18 @@ __global__ void __launch_bounds__(kOneBlock) advance_kernel(Cache c, int n, cons
   Advance e[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) e[k] = asked(c, n, slots, counts, count, first + tid * PER + k);
-  // needs of the entries before (sums beyond 2^30 are as good as 2^30: no pool has so many pages left)
+  // Needs of the entries before.  An entry needs 2^20 pages at most (the widest row), so a block's needs fit 32 bits; those of all earlier
+  // blocks are added in 64 and cut off at 2^31, which no pool's pages reach.
   uint32_t before = 0, all, mine = 0;
-  if (!ALONE) {
-    uint64_t sum = 0;
+  if constexpr (!ALONE) {
+    __shared__ uint64_t shared_sums[kOneBlock / 64];
+    uint64_t sum = 0, total;
     for (int k = 0; k < (int)blockIdx.x; ++k) sum += asked(c, n, slots, counts, count, k * kOneBlock + tid).need;
-    exclusive_sum((uint32_t)min(sum, (uint64_t)(1u << 20)), shared, &before);
+    exclusive_sum(sum, shared_sums, &total);
+    before = (uint32_t)min(total, (uint64_t)1 << 31);
   }
 #pragma unroll
-  for (int k = 0; k < PER; ++k) mine = min(mine + e[k].need, 1u << 20);
+  for (int k = 0; k < PER; ++k) mine += e[k].need;
   const uint32_t inside = exclusive_sum(mine, shared, &all);
   free.ready(lds_bits, at, shared);
   uint32_t rank = before + inside;
@@ -424,7 +428,7 @@ __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, co
       }
     exclusive_sum(sum, shared, &before);
   }
-  const uint32_t rank = before + exclusive_sum(e.need, shared, &all);
+  const uint32_t rank = before + exclusive_sum((uint32_t)e.need, shared, &all);
   free.ready(lds_bits, at, shared);
   uint8_t said = e.slots || e.nothing ? 0 : PGXCACHE_BAD_ENTRY;
   int tail = !e.slots || e.nothing ? kSkip : kNoTail;

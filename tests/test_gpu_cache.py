@@ -503,3 +503,30 @@ def test_scores_of_every_spread_and_order(head_dim, kv_heads, group, dtype):
         q[..., 0] *= torch.tensor([1.0, -1.0], device="cuda").repeat(kv_heads * group)[: kv_heads * group]
         out, lse = cache.attend(0, q, lse=True, scale=1.0)
         check_attend(cache, ref_of(cache), out, lse, 0, q, range(4), 1.0)
+
+
+@pytest.mark.parametrize("short", [False, True])
+def test_entries_that_need_more_than_a_million_pages_before_others(short):
+    """The pages of entry 2048 follow those of entries 0 and 1024, which are added up by one thread; a pool of 2 KB pages beyond what fits LDS."""
+    each, last = 524800, 5
+    pages = 2 * each + (last - 1 if short else last)
+    cache = pg.PagedCache.empty(2049, pages, (each + 1) * 16, 1, 1, 32, 16, torch.float16)
+    counts = torch.zeros(2049, dtype=torch.int32, device="cuda")
+    counts[0] = counts[1024] = each * 16
+    counts[2048] = last * 16
+    status = torch.full((2049,), 99, dtype=torch.uint8, device="cuda")
+    cache.advance(counts=counts, status=status)
+    pages_in_order = torch.arange(pages, dtype=torch.int32, device="cuda")
+    assert torch.equal(cache.table[0, :each], pages_in_order[:each]) and torch.equal(cache.table[1024, :each], pages_in_order[each: 2 * each])
+    assert status[:2048].max() == 0 and int(status[2048]) == (1 if short else 0)
+    assert cache.table[2048, :last].tolist() == ([-1] * last if short else list(range(2 * each, pages))) and int(cache.lengths[2048]) == (0 if short else 16 * last)
+    assert int(cache.refs.sum()) == 2 * each + (0 if short else last) and int(cache.refs.max()) == 1 and int((cache.table >= 0).sum()) == int(cache.refs.sum())
+    cache.fork(ints([2048, 0]), ints([1, 2]))                          # whole pages only: shared
+    cache.free(ints([0]))
+    cache.free(ints([2]))
+    used = ints([0])
+    cache.compact(used)
+    assert int(used) == each + (0 if short else last) and torch.equal(cache.refs, (pages_in_order < int(used)).int() + (0 if short else ((cache.table[1, :last, None] == pages_in_order).any(0)).int()))
+    moved = cache.table[1024, :each]
+    assert int(moved.min()) >= 0 and int(moved.max()) < int(used) and moved.unique().numel() == each
+    assert torch.equal(cache.table[1], cache.table[2048])
