@@ -62,8 +62,10 @@ typedef struct {
 /* Bytes of work memory for these sizes (256-byte aligned); 0 if they are out of range. */
 size_t pgxcache_work_bytes(const pgxcache_opts* opts);
 
-/* Takes the memory as it is: an empty cache has table -1, lengths 0 and refs 0; a saved one goes on where it was.  kv_dev
- * 16-byte aligned.  Enqueues one kernel that looks through refs_dev; to be called again (pgxcache_rescan) after the caller has written to refs_dev. */
+/* Takes the memory as it is: an empty cache has table -1, lengths 0 and refs 0; a saved one goes on where it was (save it when the tokens
+ * that there is room for have been written: what an advance before the call made room for is not remembered).  kv_dev 16-byte
+ * aligned.  Enqueues one kernel that looks through refs_dev; to be called again (pgxcache_rescan) after the caller has written to
+ * refs_dev, which leaves all else as it is. */
 int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
                   void* work_dev, size_t work_bytes);
 int pgxcache_destroy(pgxcache_t h); /* frees the host handle only */

@@ -102,15 +102,15 @@ struct Freed {
   }
 };
 
-__global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arrived) {
+__global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arrived, int first) {   // first: the work memory holds nothing yet
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t free = __ballot(i < c.pages && c.refs[min(i, (int64_t)c.pages - 1)] == 0);
   if ((threadIdx.x & 63) == 0 && i < ((int64_t)c.pages + 63) / 64 * 64) {
     c.free_bits[i >> 6] = free;
     c.taken[i >> 6] = 0;
   }
-  if (i < c.slots) c.grown[i] = 0;
-  if (i < kSplitBlocks) arrived[i] = 0;
+  if (first && i < c.slots) c.grown[i] = 0;
+  if (first && i < kSplitBlocks) arrived[i] = 0;
 }
 
 // ---- giving out pages ----------------------------------------------------------------------------------------------------------------
@@ -1104,6 +1104,12 @@ Cache cache_of(pgxcache_t h) {
   return c;
 }
 bool list_ok(pgxcache_t h, int32_t n) { return h && n >= 0 && n <= h->o.slots; }
+int scan(pgxcache_t h, int first) {
+  const int64_t most = h->o.pages > h->o.slots ? h->o.pages : h->o.slots, threads = most > kSplitBlocks ? most : kSplitBlocks;
+  hipLaunchKernelGGL(scan_refs_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), h->arrived, first);
+  HIPCHK(hipGetLastError());
+  return PGXCACHE_OK;
+}
 
 }  // namespace
 
@@ -1111,13 +1117,7 @@ extern "C" {
 
 size_t pgxcache_work_bytes(const pgxcache_opts* opts) { return opts_ok(opts) ? layout(*opts).total : 0; }
 
-int pgxcache_rescan(pgxcache_t h) {
-  if (!h) return PGXCACHE_EINVAL;
-  const int64_t most = h->o.pages > h->o.slots ? h->o.pages : h->o.slots, threads = most > kSplitBlocks ? most : kSplitBlocks;
-  hipLaunchKernelGGL(scan_refs_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), h->arrived);
-  HIPCHK(hipGetLastError());
-  return PGXCACHE_OK;
-}
+int pgxcache_rescan(pgxcache_t h) { return h ? scan(h, 0) : PGXCACHE_EINVAL; }
 
 int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
                   void* work_dev, size_t work_bytes) {
@@ -1134,7 +1134,7 @@ int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int3
   h->free_bits = (uint64_t*)(w + l.free_bits); h->taken = (uint64_t*)(w + l.taken); h->grown = (int32_t*)(w + l.grown); h->plan = (int32_t*)(w + l.plan); h->forks = (ForkEntry*)(w + l.forks);
   h->moved_to = (int32_t*)(w + l.moved_to); h->moves = (int2*)(w + l.moves); h->counts = (int32_t*)(w + l.counts);
   h->arrived = (uint32_t*)(w + l.arrived); h->partial = (float*)(w + l.partial);
-  const int rc = pgxcache_rescan(h);
+  const int rc = scan(h, 1);
   if (rc != PGXCACHE_OK) { delete h; return rc; }
   *out = h;
   return PGXCACHE_OK;

@@ -530,3 +530,21 @@ def test_entries_that_need_more_than_a_million_pages_before_others(short):
     moved = cache.table[1024, :each]
     assert int(moved.min()) >= 0 and int(moved.max()) < int(used) and moved.unique().numel() == each
     assert torch.equal(cache.table[1], cache.table[2048])
+
+
+def test_room_that_was_made_is_still_there_after_a_rescan():
+    cache = pg.PagedCache.empty(2, 6, 64, 1, 1, 64)
+    cache.kv.zero_()
+    ref = ref_of(cache)
+    k, v = torch.randn(2, 2, 3, 1, 64, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    cache.advance(counts=3)
+    ref.advance(range(2), [3, 3])
+    cache.refs[5] = ref.refs[5] = 1                    # a page that the caller keeps for itself
+    cache.rescan()
+    cache.write(0, k, v)
+    ref.write(0, k, v, range(2))
+    same(cache, ref)
+    status = torch.full((2,), 99, dtype=torch.uint8, device="cuda")
+    cache.advance(counts=ints([32, 32]), status=status)
+    assert status.tolist() == ref.advance(range(2), [32, 32]) == [0, 1]
+    same(cache, ref)
