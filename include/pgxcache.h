@@ -84,7 +84,8 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
 
 /* Attention of one token per entry over all tokens of its slot, in one layer:
  *     out[i][h] = sum_t softmax_t(scale * q[i][h] . K[t][h / group]) V[t][h / group],     group = heads / kv_heads
- * q_dev, out_dev: elements of the cache's type, [i][h][.] at i * entry_stride + h * head_stride; heads a multiple of kv_heads.  lse_dev
+ * q_dev, out_dev: elements of the cache's type, [i][h][.] at i * entry_stride + h * head_stride (those of the output may not
+ * overlap: strides below head_dim are refused); heads a multiple of kv_heads.  lse_dev
  * (nullable): float32 [n][heads], log sum_t exp(scale * q . K[t]).  k_dev and v_dev (both or neither): the key and value of each slot's
  * last token, [i][head][.], written to the cache by this call where the slot's last pgxcache_advance made room for it (and otherwise
  * ignored), so that a step takes one launch per layer; without them entries may repeat.  A slot without tokens, and an entry that is no slot, gives zeros and -infinity.

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <stdlib.h>
 
 #include <new>
 #include <type_traits>
@@ -1183,6 +1184,7 @@ int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots
                     int64_t q_head_stride, const void* k_dev, int64_t k_entry_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride,
                     int64_t v_head_stride, float scale, void* out_dev, int64_t out_entry_stride, int64_t out_head_stride, float* lse_dev) {
   if (!list_ok(h, n) || layer < 0 || layer >= h->o.layers || heads < 1 || heads > 65536 || heads % h->o.kv_heads != 0) return PGXCACHE_EINVAL;
+  if ((n > 1 && llabs(out_entry_stride) < h->o.head_dim) || (heads > 1 && llabs(out_head_stride) < h->o.head_dim)) return PGXCACHE_EINVAL;   // rows written twice
   if (!(scale - scale == 0.0f) || (k_dev != nullptr) != (v_dev != nullptr)) return PGXCACHE_EINVAL;
   if (n == 0) return PGXCACHE_OK;
   if (!q_dev || !out_dev || (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)out_dev) & 1u) != 0) return PGXCACHE_EINVAL;

@@ -548,3 +548,19 @@ def test_room_that_was_made_is_still_there_after_a_rescan():
     cache.advance(counts=ints([32, 32]), status=status)
     assert status.tolist() == ref.advance(range(2), [32, 32]) == [0, 1]
     same(cache, ref)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_outputs_that_overlap_are_refused(native, monkeypatch):
+    cache, q, _ = cache_and_more()
+    if not native:
+        monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    new = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    for out in (new(1, 4, 64).expand(2, 4, 64), new(2, 1, 64).expand(2, 4, 64), new(4000).as_strided((2, 4, 64), (1000, 32, 1)), new(4000).as_strided((2, 4, 64), (63, 64, 1))):
+        with pytest.raises(pg.PgxGoError):
+            cache.attend(0, q, out=out)
+    want = cache.attend(0, q)
+    for out in (new(4, 2, 64).transpose(0, 1), new(2, 9, 64)[:, ::2][:, :4], new(4000).as_strided((2, 4, 64), (300, 64, 1))):    # heads first, every other head, rows apart
+        assert torch.equal(cache.attend(0, q, out=out), want)
+    one = cache.attend(0, q[:1, :2], ints([0]), out=new(1, 2, 64).as_strided((1, 2, 64), (0, 64, 1)))
+    assert torch.equal(one, cache.attend(0, q[:1, :2], ints([0])))
