@@ -54,7 +54,8 @@ class PagedCache:
     The memory is the caller's: kv [pages][layers][2][kv_heads][page_size][head_dim] in float16 or bfloat16, table int32 [slots][width],
     lengths int32 [slots], refs int32 [pages].  The handle takes them as they are (PagedCache.empty makes empty ones), so a cache
     is saved by copying the four and restored by making a handle on them; after writing to refs oneself, call rescan().
-    All calls run on the stream that was current when the handle was made."""
+    All calls run on the stream that was current when the handle was made, and attend's new outputs belong to it, whichever stream is
+    current: a program that works on another one has the two wait for each other, as for tensors of any other stream."""
 
     def __init__(self, kv, table, lengths, refs):
         L = lib()
@@ -83,7 +84,7 @@ class PagedCache:
         self._h, self._destroy = h, L.pgxcache_destroy
         if _fast is not None:
             self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "attend", "fork", "free")}
-            self._shape = (self.slots, self.kv_heads, self.head_dim, TYPES[self.dtype], self.device.index)
+            self._shape = (self.slots, self.kv_heads, self.head_dim, TYPES[self.dtype], self.device.index, self._stream.stream_id)
         self._scale = self.head_dim ** -0.5
 
     @classmethod
@@ -176,9 +177,11 @@ class PagedCache:
             shape = (n, self.kv_heads, self.head_dim)
             kp, vp = self._heads(k, shape, "k"), self._heads(v, shape, "v")
             ks, vs = k.stride()[:2], v.stride()[:2]
-        out = torch.empty((n, heads, self.head_dim), dtype=self.dtype, device=self.device) if out is None else out
+        with torch.cuda.stream(self._stream):   # new outputs belong to the stream that writes them
+            if out is None: out = torch.empty((n, heads, self.head_dim), dtype=self.dtype, device=self.device)
+            made = torch.empty((n, heads), dtype=torch.float32, device=self.device) if lse is True else None
         op = self._heads(out, (n, heads, self.head_dim), "out")
-        if lse is True: lse = torch.empty((n, heads), dtype=torch.float32, device=self.device)
+        if lse is True: lse = made
         elif lse is not False: _need(lse, torch.float32, (n, heads), "lse")
         _check(lib().pgxcache_attend(self._h, int(layer), n, p, heads, qp, *q.stride()[:2], kp, *ks, vp, *vs, float(scale), op, *out.stride()[:2],
                                      None if lse is False else lse.data_ptr()), "pgxcache_attend")

@@ -6,6 +6,7 @@
 // anything is not as it has to be, and then the Python path runs and raises its error.  Nothing is kept between calls.
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/StreamGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -328,18 +329,19 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // ---- the paged cache -------------------------------------------------------------------------------------------------------------------
-// (address, handle, shape, ...) where shape = (slots, kv_heads, head_dim, type, device index)
+// (address, handle, shape, ...) where shape = (slots, kv_heads, head_dim, type, device index, the handle's stream as torch numbers it)
 struct CacheShape {
   int64_t slots, kv_heads, head_dim;
   at::ScalarType type;
   c10::Device device;
+  c10::StreamId stream;
 };
 bool take_shape(PyObject* o, CacheShape* s) {
-  if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 5) return false;
-  int64_t v[5];
-  for (int i = 0; i < 5; ++i) v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(o, i));
+  if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 6) return false;
+  int64_t v[6];
+  for (int i = 0; i < 6; ++i) v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(o, i));
   if (PyErr_Occurred()) return false;
-  *s = CacheShape{v[0], v[1], v[2], v[3] == PGXCACHE_F16 ? at::kHalf : at::kBFloat16, c10::Device(c10::kCUDA, (c10::DeviceIndex)v[4])};
+  *s = CacheShape{v[0], v[1], v[2], v[3] == PGXCACHE_F16 ? at::kHalf : at::kBFloat16, c10::Device(c10::kCUDA, (c10::DeviceIndex)v[4]), v[5]};
   return true;
 }
 bool take_list(PyObject* o, const CacheShape& s, int64_t* n, void** out) {
@@ -365,7 +367,7 @@ bool take_heads(PyObject* o, const CacheShape& s, int64_t n, int64_t heads, void
 // (address, handle, shape, slots, counts, status)
 PyObject* cache_advance(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&] {
-    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU)};
+    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
     int64_t n, count = 0;
     void *slots, *counts = nullptr, *status;
     if (n_args != 6 || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &slots) || !take_or_null(a[5], kByte, n, -1, &status)) return -1000;
@@ -384,7 +386,7 @@ PyObject* cache_advance(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 // (address, handle, shape, src, dst, status)
 PyObject* cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&] {
-    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU)};
+    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
     int64_t n;
     void *src, *dst, *status;
     if (n_args != 6 || a[3] == Py_None || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &src) || !take(a[4], kInt, n, -1, &dst) ||
@@ -399,7 +401,7 @@ PyObject* cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 // (address, handle, shape, slots)
 PyObject* cache_free(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&] {
-    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU)};
+    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
     int64_t n;
     void* slots;
     if (n_args != 4 || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &slots)) return -1000;
@@ -426,7 +428,7 @@ bool take_tokens(PyObject* o, const CacheShape& s, int64_t n, int64_t* tokens, v
 // (address, handle, shape, layer, k, v, slots)
 PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded([&] {
-    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU)};
+    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
     int64_t n, tokens, tokens_v, ke, kt, kh, ve, vt, vh;
     void *slots, *k, *v;
     if (n_args != 7 || !take_shape(a[2], &s) || !take_list(a[6], s, &n, &slots) || !take_tokens(a[4], s, n, &tokens, &k, &ke, &kt, &kh) ||
@@ -443,7 +445,7 @@ PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 // (address, handle, shape, layer, q, slots, k, v, scale, out, lse)
 PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded_outputs([&]() -> PyObject* {
-    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU)};
+    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
     int64_t n, qe, qh, ke = 0, kh = 0, ve = 0, vh = 0;
     void *slots, *q, *k = nullptr, *v = nullptr, *lse_data = nullptr;
     float scale;
@@ -457,7 +459,7 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (!number(a[8], &scale)) return nullptr;
     const long layer = PyLong_AsLong(a[3]);
     if (PyErr_Occurred() || layer < 0 || layer > INT32_MAX) return nullptr;
-    const c10::DeviceGuard guard(s.device);
+    const c10::StreamGuard guard(c10::Stream(c10::Stream::UNSAFE, s.device, s.stream));   // new outputs belong to the stream that writes them
     if (!output(a[9], {n, heads, s.head_dim}, s.type, s.device, &out)) return nullptr;
     PyObject* given_lse = a[10] == Py_True ? Py_None : a[10];
     if (a[10] != Py_False) {

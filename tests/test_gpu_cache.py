@@ -564,3 +564,27 @@ def test_outputs_that_overlap_are_refused(native, monkeypatch):
         assert torch.equal(cache.attend(0, q, out=out), want)
     one = cache.attend(0, q[:1, :2], ints([0]), out=new(1, 2, 64).as_strided((1, 2, 64), (0, 64, 1)))
     assert torch.equal(one, cache.attend(0, q[:1, :2], ints([0])))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_new_outputs_belong_to_the_handles_stream(native, monkeypatch):
+    """so that their memory is not at the same time another's on the stream that happens to be current"""
+    if not native:
+        monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    here = torch.cuda.current_stream()
+    torch.cuda.synchronize()
+    for mine, now in ((side, here), (here, side), (side, other)):
+        with torch.cuda.stream(mine):
+            cache = filled([20, 5], 2, 2, 64, 16, torch.bfloat16)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(now):
+            q = torch.randn(2, 4, 64, device="cuda").bfloat16()
+            now.synchronize()
+            out, lse = cache.attend(0, q, lse=True)
+            assert torch.cuda.current_stream() == now
+        for t in (out, lse):
+            at = t.data_ptr()
+            assert [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]] == [mine.cuda_stream]
+        mine.synchronize()
+        check_attend(cache, ref_of(cache), out, lse, 0, q, range(2), 0.125)
