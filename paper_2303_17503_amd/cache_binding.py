@@ -109,11 +109,17 @@ class PagedCache:
         n = slots.shape[0]
         if n > self.slots:
             raise PgxGoError(f"{name}: {n} entries for {self.slots} slots")
-        _need(slots, torch.int32, (n,), name)
+        self._own(slots, torch.int32, (n,), name)
         return n, slots.data_ptr()
 
+    def _own(self, t, dtype, shape, name):
+        """a contiguous tensor on the cache's device"""
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            raise PgxGoError(f"{name}: expected a tensor on {self.device}, as the cache is, got {t.device if isinstance(t, torch.Tensor) else type(t).__name__}")
+        return _need(t, dtype, shape, name)
+
     def _status(self, status, n):
-        return None if status is None else _need(status, torch.uint8, (n,), "status").data_ptr()
+        return None if status is None else self._own(status, torch.uint8, (n,), "status").data_ptr()
 
     def _heads(self, t, shape, name):
         """pointer of a tensor of the cache's type whose last dimension is dense"""
@@ -134,7 +140,7 @@ class PagedCache:
             if rc is not None: _check(rc, "pgxcache_advance")
         n, p = self._list(slots)
         each = isinstance(counts, torch.Tensor)
-        if each: _need(counts, torch.int32, (n,), "counts")
+        if each: self._own(counts, torch.int32, (n,), "counts")
         elif not 0 <= counts < 2 ** 31: raise PgxGoError(f"counts: 0 or more tokens, got {counts}")
         _check(lib().pgxcache_advance(self._h, n, p, _ptr(counts) if each else None, 0 if each else int(counts), self._status(status, n)), "pgxcache_advance")
 
@@ -182,7 +188,7 @@ class PagedCache:
             made = torch.empty((n, heads), dtype=torch.float32, device=self.device) if lse is True else None
         op = self._heads(out, (n, heads, self.head_dim), "out")
         if lse is True: lse = made
-        elif lse is not False: _need(lse, torch.float32, (n, heads), "lse")
+        elif lse is not False: self._own(lse, torch.float32, (n, heads), "lse")
         _check(lib().pgxcache_attend(self._h, int(layer), n, p, heads, qp, *q.stride()[:2], kp, *ks, vp, *vs, float(scale), op, *out.stride()[:2],
                                      None if lse is False else lse.data_ptr()), "pgxcache_attend")
         return out if lse is False else (out, lse)
@@ -195,7 +201,7 @@ class PagedCache:
             if rc == 0: return
             if rc is not None: _check(rc, "pgxcache_fork")
         n, s = self._list(src, "src")
-        _need(dst, torch.int32, (n,), "dst")
+        self._own(dst, torch.int32, (n,), "dst")
         _check(lib().pgxcache_fork(self._h, n, s, _ptr(dst), self._status(status, n)), "pgxcache_fork")
 
     def free(self, slots=None):
@@ -209,5 +215,5 @@ class PagedCache:
 
     def compact(self, used=None):
         """Moves pages so that those in use are the first ones; used (int32 [1]) gets their number."""
-        if used is not None: _need(used, torch.int32, (1,), "used")
+        if used is not None: self._own(used, torch.int32, (1,), "used")
         _check(lib().pgxcache_compact(self._h, _ptr(used)), "pgxcache_compact")

@@ -344,6 +344,14 @@ bool take_shape(PyObject* o, CacheShape* s) {
   *s = CacheShape{v[0], v[1], v[2], v[3] == PGXCACHE_F16 ? at::kHalf : at::kBFloat16, c10::Device(c10::kCUDA, (c10::DeviceIndex)v[4]), v[5]};
   return true;
 }
+// a contiguous tensor of one value per entry, on the cache's device
+bool take_entries(PyObject* o, const CacheShape& s, at::ScalarType type, int64_t n, void** out) {
+  return take(o, type, n, -1, out) && tensor(o)->device() == s.device;
+}
+bool take_status(PyObject* o, const CacheShape& s, int64_t n, void** out) {
+  *out = nullptr;
+  return o == Py_None || take_entries(o, s, kByte, n, out);
+}
 bool take_list(PyObject* o, const CacheShape& s, int64_t* n, void** out) {
   *n = s.slots;
   *out = nullptr;
@@ -351,7 +359,7 @@ bool take_list(PyObject* o, const CacheShape& s, int64_t* n, void** out) {
   const at::Tensor* t = tensor(o);
   if (!t || t->dim() != 1 || t->size(0) > s.slots) return false;
   *n = t->size(0);
-  return take(o, kInt, *n, -1, out);
+  return take_entries(o, s, kInt, *n, out);
 }
 // [n][heads][head_dim] of the cache's type, strides in elements
 bool take_heads(PyObject* o, const CacheShape& s, int64_t n, int64_t heads, void** out, int64_t* entry, int64_t* head) {
@@ -370,11 +378,11 @@ PyObject* cache_advance(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
     int64_t n, count = 0;
     void *slots, *counts = nullptr, *status;
-    if (n_args != 6 || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &slots) || !take_or_null(a[5], kByte, n, -1, &status)) return -1000;
+    if (n_args != 6 || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &slots) || !take_status(a[5], s, n, &status)) return -1000;
     if (PyLong_CheckExact(a[4])) {
       count = PyLong_AsLongLong(a[4]);
       if (PyErr_Occurred() || count < 0 || count > INT32_MAX) return -1000;
-    } else if (!take(a[4], kInt, n, -1, &counts)) {
+    } else if (!take_entries(a[4], s, kInt, n, &counts)) {
       return -1000;
     }
     auto* fn = (decltype(&pgxcache_advance))pointer(a[0]);
@@ -389,8 +397,8 @@ PyObject* cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
     int64_t n;
     void *src, *dst, *status;
-    if (n_args != 6 || a[3] == Py_None || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &src) || !take(a[4], kInt, n, -1, &dst) ||
-        !take_or_null(a[5], kByte, n, -1, &status))
+    if (n_args != 6 || a[3] == Py_None || !take_shape(a[2], &s) || !take_list(a[3], s, &n, &src) || !take_entries(a[4], s, kInt, n, &dst) ||
+        !take_status(a[5], s, n, &status))
       return -1000;
     auto* fn = (decltype(&pgxcache_fork))pointer(a[0]);
     void* h = pointer(a[1]);

@@ -588,3 +588,27 @@ def test_new_outputs_belong_to_the_handles_stream(native, monkeypatch):
             assert [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]] == [mine.cuda_stream]
         mine.synchronize()
         check_attend(cache, ref_of(cache), out, lse, 0, q, range(2), 0.125)
+
+
+def test_lists_on_another_device_are_left_alone():
+    """A handle that says it is on another device stands for a list on another device: neither the native checks nor Python's pass it on."""
+    cache, q, k = cache_and_more()
+    before = cache.lengths.clone()
+    one, status = ints([0]), torch.zeros(1, dtype=torch.uint8, device="cuda")
+    cache._shape = cache._shape[:4] + (1,) + cache._shape[5:]
+    cache.device = torch.device("cuda:1")
+    for call in (lambda: cache.advance(one), lambda: cache.advance(one, one, status), lambda: cache.free(one), lambda: cache.fork(one, ints([1])), lambda: cache.compact(one),
+                 lambda: cache.write(0, k[:1], k[:1], one), lambda: cache.attend(0, q[:1], one), lambda: cache.advance(status=torch.zeros(2, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(pg.PgxGoError):
+            call()
+    assert torch.equal(cache.lengths, before)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_what_is_no_tensor_is_refused(native, monkeypatch):
+    cache, q, _ = cache_and_more()
+    if not native:
+        monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    for call in (lambda: cache.fork(ints([0]), [1]), lambda: cache.advance(status=[0, 0]), lambda: cache.attend(0, q, lse=1), lambda: cache.compact(3), lambda: cache.free([0])):
+        with pytest.raises(pg.PgxGoError):
+            call()
