@@ -612,3 +612,118 @@ def test_what_is_no_tensor_is_refused(native, monkeypatch):
     for call in (lambda: cache.fork(ints([0]), [1]), lambda: cache.advance(status=[0, 0]), lambda: cache.attend(0, q, lse=1), lambda: cache.compact(3), lambda: cache.free([0])):
         with pytest.raises(pg.PgxGoError):
             call()
+
+
+def spread_of_lengths(most, count, seed):
+    """`count` different lengths up to `most`, the edges of a tile of 32 among them"""
+    edges = [0, 1, 31, 32, 33, 64, most - 1, most]
+    r = random.Random(seed)
+    lengths = edges + r.sample([n for n in range(2, most - 1) if n not in edges], count - len(edges))
+    assert len(set(lengths)) == count
+    r.shuffle(lengths)
+    return lengths
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("head_dim", [32, 64, 96, 128, 256])
+@pytest.mark.parametrize("tiles,n", [(8, 20), (8, 520), (9, 20), (9, 520), (32, 20), (32, 300), (33, 5), (80, 20), (80, 300), (600, 2)])
+def test_attention_in_each_way_that_rows_are_spread(tiles, n, head_dim, dtype):
+    """By how long a slot can be and how many rows there are (2 key heads here): one wavefront to a row (8 tiles of 32 tokens, 1024 rows or more), four, or four
+    in each of several blocks (more than 32 tiles, 256 rows or fewer).  Different lengths, each row against 64 bits."""
+    some = min(n, 16)
+    lengths = spread_of_lengths(tiles * 32, max(some, 8), 7)[:some]
+    if n <= 5:
+        lengths = [tiles * 32, 0, 33, tiles * 32 - 1, 1][:n]
+    cache = filled(lengths + [0] * (n - len(lengths)), 1, 2, head_dim, 16, dtype, seed=3, width=tiles * 2)
+    ref, g = ref_of(cache), torch.Generator("cuda").manual_seed(4)
+    slots = [i % len(lengths) for i in range(n)]
+    q = torch.randn(len(lengths), 6, head_dim, generator=g, device="cuda", dtype=dtype)
+    out, lse = cache.attend(0, q[torch.tensor(slots)], ints(slots), lse=True)
+    check_attend(cache, ref, out[: len(lengths)], lse[: len(lengths)], 0, q, range(len(lengths)), head_dim ** -0.5)
+    for i in range(n):
+        assert torch.equal(bits(out[i]), bits(out[i % len(lengths)])) and torch.equal(bits(lse[i]), bits(lse[i % len(lengths)]))
+
+
+@pytest.mark.parametrize("tiles,n", [(8, 600), (8, 7), (20, 40), (60, 6), (60, 300)])
+@pytest.mark.parametrize("head_dim,dtype", [(64, torch.bfloat16), (128, torch.float16), (32, torch.float16), (256, torch.bfloat16)])
+def test_the_new_token_is_read_in_a_pool_that_is_streamed(head_dim, dtype, tiles, n):
+    """what a call writes and reads with the hint of a large pool, in each way that rows are spread; against write and attend one after the other"""
+    lengths = [m % (tiles * 32) for m in (0, 15, 16, 31, 32, 33, 200, tiles * 32 - 1)]
+    lengths = [lengths[i % 8] for i in range(n)]
+    a, b = (filled(lengths, 1, 2, head_dim, 16, dtype, seed=2, width=tiles * 2, spare=n + (270 << 20) // (2 * 2 * 16 * head_dim * 2)) for _ in range(2))
+    assert a.kv.numel() * 2 > 256 << 20
+    g = torch.Generator("cuda").manual_seed(1)
+    q, k, v = (torch.randn(n, h, head_dim, generator=g, device="cuda", dtype=dtype) for h in (40, 2, 2))
+    for cache in (a, b):
+        cache.advance()
+    b.write(0, k, v)
+    got, want = a.attend(0, q, k=k, v=v, lse=True), b.attend(0, q, lse=True)
+    assert torch.equal(bits(got[0]), bits(want[0])) and torch.equal(bits(got[1]), bits(want[1]))
+    assert torch.equal(a.kv.view(torch.int16), b.kv.view(torch.int16))
+    some = min(n, 8)
+    check_attend(b, ref_of(b), got[0][:some], got[1][:some], 0, q[:some], range(some), head_dim ** -0.5)
+
+
+@pytest.mark.parametrize("n", [4097, 9000, 20011])
+def test_as_many_slots_as_the_largest_batches_have(n):
+    """plans of many blocks, in a pool that runs out among the last entries"""
+    r = random.Random(n)
+    cache = pg.PagedCache.empty(2 * n, 11 * n // 5, 4, 1, 1, 32, 16, torch.float16)
+    cache = pg.PagedCache(cache.kv.zero_(), torch.full((2 * n, 4), -1, dtype=torch.int32, device="cuda"), cache.lengths, cache.refs)
+    ref = ref_of(cache)
+    order = r.sample(range(n), n)
+    status = torch.full((n,), 99, dtype=torch.uint8, device="cuda")
+    counts = [r.choice([0, 1, 15, 16, 17, 40, 64, 65]) for _ in order]
+    cache.advance(ints(order), ints(counts), status)
+    assert status.tolist() == ref.advance(order, counts)
+    same(cache, ref)
+    src, dst = r.sample(range(n), n), r.sample(range(n, 2 * n), n)
+    said = []
+    for k in range(2):                                       # the second gives up what the first made
+        cache.fork(ints(src), ints(dst), status)
+        assert status.tolist() == ref.fork(src, dst)
+        said += status.tolist()
+        same(cache, ref)
+        cache.advance(ints(dst), 1, status)
+        assert status.tolist() == ref.advance(dst, [1] * n)
+        said += status.tolist()
+        same(cache, ref)
+        src = r.sample(range(n), n)
+    assert {0, 1} <= set(said)
+    gone = r.sample(range(2 * n), n)
+    cache.free(ints(gone))
+    ref.free(gone)
+    used = ints([0])
+    cache.compact(used)
+    assert int(used) == ref.compact()
+    same(cache, ref)
+
+
+def test_a_pool_with_more_pages_than_lds_holds_bits_for():
+    """270000 pages of 2 KB, some of them the caller's own"""
+    pages, slots = 270001, 40
+    r, g = random.Random(5), torch.Generator("cuda").manual_seed(2)
+    cache = pg.PagedCache.empty(slots, pages, 50 * 16, 1, 1, 32, 16, torch.float16)
+    cache.kv.normal_(generator=g)
+    kept = torch.randint(0, pages, (9000,), generator=g, device="cuda")
+    cache.refs[kept] = 1
+    cache.refs[:400] = 1
+    cache.rescan()
+    ref = ref_of(cache)
+    for step in range(6):
+        entries = r.sample(range(slots), 20)
+        counts = [r.choice([0, 1, 16, 100, 300]) for _ in entries]
+        status = torch.full((20,), 99, dtype=torch.uint8, device="cuda")
+        cache.advance(ints(entries), ints(counts), status)
+        assert status.tolist() == ref.advance(entries, counts)
+        src, dst = entries[:10], entries[10:]
+        cache.fork(ints(src), ints(dst))
+        ref.fork(src, dst)
+        same(cache, ref)
+        if step % 2:
+            cache.free(ints(entries[:3]))
+            ref.free(entries[:3])
+            used = ints([0])
+            cache.compact(used)
+            assert int(used) == ref.compact()
+            same(cache, ref)
