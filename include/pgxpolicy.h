@@ -8,7 +8,7 @@
  * Conventions are those of pgxgo.h: pointers named *_dev are device pointers owned by the caller, work is enqueued on
  * the given stream and is asynchronous, every function returns PGXPOLICY_OK or a negative code, nothing throws, aborts,
  * allocates or synchronises.  Nothing is kept between calls.  Rows of inputs may overlap (pitch 0: one row for all games),
- * rows of outputs may not.
+ * rows of outputs may not.  Adjusted logits and gradients may take the place of logits of their type and pitch.
  *
  * Adjusted logits.  For row b (a game) and action a, in 32-bit floating point, every operation rounded by itself:
  *     z = logits[b][a]

@@ -357,6 +357,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Args a) {
       for (int j = 0; j < 8; ++j) z[c][j] = (mask[c][j >> 2] >> (8 * (j & 3)) & 0xFFu) != 0 ? z[c][j] : kNone;
   }
   if (OP == kLogits && !a.normalize) {
+    if (G > 64) __syncthreads();   // out may be the logits: a row's last chunk reads what another wavefront's chunk before it writes
     if (mine) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) store_chunk<F32>((float*)a.out + (int64_t)b * a.out_pitch, Chunk(c * G + lane, A), A, z[c]);

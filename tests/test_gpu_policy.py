@@ -477,3 +477,17 @@ def test_the_sign_of_zero_is_kept(divisor):
         how.update(record=torch.randint(0, 82, (9, 60), generator=g, dtype=torch.int32).cuda(), repetition=1.3)
     want = ref.adjusted(x, dtype=torch.float32, **how)[0]
     assert torch.equal(bits(pg.adjust_logits(x, **how).cpu()), bits(want)) and torch.signbit(want[want == 0]).any()
+
+
+@pytest.mark.parametrize("actions", [5, 82, 362, 383, 513, 1030, 2049, 2561, 2567, 3075, 4099, 8191])
+def test_outputs_in_the_place_of_the_logits(actions):
+    """sizes whose last chunk, moved back, shares actions with one of the same wavefront and of another"""
+    x, how, g = inputs(300, actions, "f32", 8, record=0)
+    moves = torch.randint(0, actions, (300,), generator=g, dtype=torch.int32).cuda()
+    for h in (how, {k: how[k] for k in ("bias", "temperature")}):
+        for normalize in (False, True):
+            want, y = pg.adjust_logits(x, normalize=normalize, **h), x.clone()
+            assert torch.equal(bits(pg.adjust_logits(y, normalize=normalize, out=y, **h)), bits(want))
+        want, y = pg.policy_loss(x, moves, entropy=0.1, **h), x.clone()
+        got = pg.policy_loss(y, moves, entropy=0.1, grad=y, **h)
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want)) and torch.equal(bits(y), bits(want[2]))
