@@ -90,15 +90,16 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
  * last token, [i][head][.], written to the cache by this call where the slot's last pgxcache_advance made room for it (and otherwise
  * ignored), so that a step takes one launch per layer; without them entries may repeat.  A slot without tokens, and an entry that is no slot, gives zeros and -infinity.
  * Scores, sums and the output before its rounding are held in 32 bits; probabilities are multiplied as two numbers of the
- * cache's type that add up to them within 2^-17 (float16: of the sum of 32 tokens' probabilities), however small they are. */
+ * cache's type that add up to them within 2^-17 (float16: of the sum of 32 tokens' probabilities), however small they are.
+ * A key or value that is infinite or NaN makes what it counts for NaN; places behind a slot's last token may hold anything. */
 int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t heads, const void* q_dev, int64_t q_entry_stride,
                     int64_t q_head_stride, const void* k_dev, int64_t k_entry_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride,
                     int64_t v_head_stride, float scale, void* out_dev, int64_t out_entry_stride, int64_t out_head_stride, float* lse_dev);
 
 /* slot[dst_slots_dev[i]] = slot[src_slots_dev[i]], as pgxgo_copy_slots does for states and with its constraints: destinations are pairwise
  * distinct and none is the source of another entry.  Full pages are shared, a partly filled last one is copied to the lowest
- * free page.  What the destination held is given up; pages that come free by it can be taken by later calls, not by this one.  An entry
- * with src == dst does nothing.  On PGXCACHE_NO_PAGES the destination keeps what it had. */
+ * free page.  What the destination held is given up; pages that come free by it can be taken by later calls, not by this one.  Tokens of
+ * the source that have not been written yet are to be written before it is forked.  An entry with src == dst does nothing.  On PGXCACHE_NO_PAGES the destination keeps what it had. */
 int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const int32_t* dst_slots_dev, uint8_t* status_dev);
 
 /* The slots' tokens are given up; pages that no other slot shares come free. */

@@ -10,7 +10,8 @@
  * allocates or synchronises.  Nothing is kept between calls.  Rows of inputs may overlap (pitch 0: one row for all games),
  * rows of outputs may not.  Adjusted logits and gradients may take the place of logits of their type and pitch.
  *
- * Adjusted logits.  For row b (a game) and action a, in 32-bit floating point, every operation rounded by itself:
+ * Adjusted logits.  For row b (a game) and action a, in 32-bit floating point, every operation rounded by itself (a quotient
+ * below 2^-100 may differ in its last bit):
  *     z = logits[b][a]
  *     c = how often a occurs among record[b][t], max(begin[b], 0) <= t < min(end[b], record_len)      (0 without a record)
  *     if c > 0:  z = z > 0 ? z / repetition : z * repetition

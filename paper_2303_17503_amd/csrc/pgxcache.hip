@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(256) scan_refs_kernel(Cache c, uint32_t* arriv
 // ---- giving out pages ----------------------------------------------------------------------------------------------------------------
 // A call takes the lowest free pages, its entries in their order.  Which entry gets which follows from the free pages' bits and the
 // needs of the entries before it, and every block of a planning kernel works both out for itself from memory that no one writes
-// meanwhile; a second kernel then takes the pages out of the bits.  Bound by the round trips to memory that depend on each other (the list, the
+// meanwhile (so a plan of n entries reads n^2 / 2048 of them: 65536 take 78 us); a second kernel then takes the pages out of the bits.  Bound by the round trips to memory that depend on each other (the list, the
 // lengths it names; the bits beside them), so the bits are kept in LDS.  4096 entries of a pool of 143000 pages: one block that took the
 // entries 1024 at a time and looked the bits up in memory took 40 us for a fork's plan; blocks of 1024 entries side by side take 8 to 10.
 constexpr int kBitsInLds = 4096;   // words: pools of up to 262144 pages; beyond, the bits are looked up in memory
@@ -284,8 +284,9 @@ __device__ __forceinline__ void finish(const Cache& c, const Advance& e, bool do
   if (done && e.more > 0) c.lengths[e.slot] = e.length + e.more;
 }
 // PER = 1: a block per kOneBlock entries; one block ends the call itself, more are followed by advance_apply_kernel.  PER > 1: one block, PER
-// neighbouring entries per thread, all their loads under way together, for up to 4096 entries that get one page each at most (of one token
-// more each: 11.9 us, by the two kernels 12.9; 1 to 39 tokens more, 7300 pages: 28.0 by one block, 15.9 by the two kernels, and 22.9 / 15.2 for 2048 entries).
+// neighbouring entries per thread, all their loads under way together, for up to 4096 entries that get one page each at most (a call of 4096 with
+// one token more each: 10.4 us, by the two kernels 12.3, of 2048 8.8 / 11.1; with 0 to 39 tokens more: 32.3 by one block, 16.5 by the two kernels, of
+// 2048 23.0 / 14.4).
 // The pages that the entries get are the free ones of consecutive ranks (an entry that cannot have its pages is followed by others that cannot),
 // so they leave the bits a word at a time (4600 pages, taken out one by one: 52 us, now 12).
 constexpr uint32_t kWanted = 1536;
@@ -421,7 +422,7 @@ __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, co
   uint32_t before = 0, all;
   if (blockIdx.x > 0) {
     uint32_t sum = 0;
-    for (int k0 = 0; k0 < (int)blockIdx.x; k0 += 4)   // four blocks' entries under way together (65536 entries: 85 -> 78 us)
+    for (int k0 = 0; k0 < (int)blockIdx.x; k0 += 4)   // four blocks' entries under way together (65536 entries: 78 us, one block at a time 85)
 #pragma unroll
       for (int k = k0; k < k0 + 4; ++k) {
         const bool need = look(min(k, (int)blockIdx.x - 1) * kOneBlock + (int)threadIdx.x).need;
@@ -444,8 +445,9 @@ __global__ void __launch_bounds__(kOneBlock) fork_plan_kernel(Cache c, int n, co
   free.ranks(before, min(before + all, free.count), [&](int w, uint64_t, uint64_t mask) { atomicOr((unsigned long long*)&c.taken[w], mask); });
 }
 
-// `per` threads for each entry: a wavefront where pages have up to 16 KB (4096 entries whose tails are 8 KB on average: 20.3 us with four
-// wavefronts each, 12.3 us with one, all of which the machine holds at once), more for larger ones.  A page that both slots name keeps
+// `per` threads for each entry: a wavefront where pages have up to 16 KB, two up to 32 KB, four above.  A call of 4096 entries, by one, two and four wavefronts
+// each: pages of 8 KB 15.9, 18.4 and 23.3 us, 16 KB 21.2, 21.6 and 24.4, 32 KB 31.7, 30.8 and 30.8, 64 KB 53.7, 52.5 and 50.0; of 256 entries, 32 KB
+// 11.0, 9.7 and 9.8, 64 KB 14.0, 11.4 and 10.4.  A page that both slots name keeps
 // the source's reference throughout, so none comes free in between.
 __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const ForkEntry* plan, int per) {
   __shared__ Freed freed;
@@ -680,8 +682,7 @@ __device__ __forceinline__ float across_groups_sum(float x) {
 }
 
 // What one block leaves for another of the same launch goes through the dies' L2 caches, which do not know of each other, without
-// writing back or dropping anything else in them: a device-wide fence per block instead cost 20 us each (3 sequences of 110000
-// tokens: 282 -> 250 us).
+// writing back or dropping anything else in them: a device-wide fence per block instead cost 20 us each, 32 us with 3 sequences of 110000 tokens.
 constexpr int kAcrossDies = 16;             // cache policy of a buffer instruction: as an atomic access of the whole device (sc1)
 constexpr int kBufferFlags = 0x00027000;    // raw buffer of 32-bit words
 
@@ -1026,8 +1027,10 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
 
 template <class T, int NT, int W>
 hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t rows, hipStream_t stream) {
-  // A pool beyond the 256 MB memory-side cache is streamed (4096 slots of 1 to 722 tokens, 757 MB: 141 -> 136 us, all of 722: 261 -> 240, 3
-  // sequences of 110000, 1.35 GB: 230 -> 203; 1024 slots of 1 to 722, 189 MB, which stay in that cache from step to step: 34 -> 39).
+  // A pool beyond the 256 MB memory-side cache is streamed (4096 slots of 1 to 722 tokens, 757 MB: 132 us, without the hint 139; all of 722: 241 / 263; 3
+  // sequences of 110000, 1.35 GB: 220 / 243), a smaller one stays in that cache from step to step (1024 slots of 1 to 722, 189 MB: 33 us, with the hint 39;
+  // of 1 to 160 10.3 / 11.8).  The host knows the pool's size and not how much of it slots hold: the same 189 MB in a pool of 1 GB are
+  // streamed, and take 42 us instead of 34.
   const bool streamed = (int64_t)c.pages * c.page_bytes() > (int64_t)256 << 20;
   const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = a.splits > 1 ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
   const dim3 grid((unsigned)(rows * a.splits)), block(64 * W);
@@ -1038,12 +1041,13 @@ hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t rows, h
 template <class T, int NT>
 hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
   // The lengths are known on the device only, so the choice goes by how long a slot can be.
-  //  * Short ones and many rows: a wavefront each (1024 slots of 1 to 160 tokens, 2 key heads of 64: 10.3 us, with four 11.9; 4096 of 1 to 160
-  //    30.5 / 34.2). Longer ones: four (1024 of 1 to 722 tokens 37.8 / 33.3, 4096 147 / 139; one of 722 12.4 / 7.0; eight are slower throughout: 7.5).
-  //  * Few rows that can be longer than 32 tiles are split over blocks, 8 tiles to each if all tiles are there (one sequence of 722
-  //    tokens: 7.0 us in one block, 8.3 split; of 2048: 12.2 in two blocks, 8.5 in eight; of 8192: 12.5 in eight, 9.1 in 32), as long as the machine's 256
-  //    compute units have two blocks each at most (3 x 8 rows of 110000 tokens of 128 elements: 232 us with 504 blocks, 238 with 1008, 252 with 2016).
-  //    Beyond 128 parts the joining costs more than the reading (one of 131072 tokens: 29.3 us in 128 parts, 40.4 in 256).
+  //  * Short ones and many rows: a wavefront each (1 to 160 tokens, 2 key heads; with four in parentheses: 1024 slots, heads of 32 5.7 us (10.1), 64 10.3 (12.1), 128
+  //    17.5 (22.8), 256 31.9 (59.5); 4096 slots, 64 30.8 (34.8), 128 73 (96), 256 170 (280)).  Longer ones: four (heads of 64; with one in parentheses: 1024
+  //    of 1 to 722 tokens 33 us (36), 4096 132 (137), one of 722 7.0 (10.9)).
+  //  * Few rows that can be longer than 32 tiles are split over blocks, 8 tiles to each if all tiles are there (one sequence, 2 key heads of 64, in one block in
+  //    parentheses: 2048 tokens 8.5 us (13.7), 8192 9.0 (44.8)), as long as the machine's 256 compute units have two blocks each at most (3 x 8 rows of
+  //    110000 tokens of 128 elements: 220 us with 504 blocks, 231 with 1008, 234 with 2016). Beyond 128 parts the joining costs more than the
+  //    reading (one of 131072 tokens: 19.8 us in 128 parts, 25.0 in 256; 19.3 in 64).
   const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles, most_tiles = (((int64_t)c.width << c.page_shift) + 31) / 32;
   a.splits = 1;
   if (most_tiles <= 8 && rows >= 1024) return launch_attend_by<T, NT, 1>(c, a, rows, stream);

@@ -5,7 +5,7 @@
 // bytes they move; 16 lanes per row (rather than the wavefront) let a row's reductions run on four rows at once by DPP rotations
 // inside the 16-lane rows, and 3 chunks x 16 lanes x 8 hold the 362 actions of 19x19 with 6 % of the lanes' slots idle.
 //
-// Measured: the loss of 65536 x 362 logits in bfloat16 25.8 us, 4.6 TB/s of what it has to move; 16384 x 122 log-probabilities 5.2 us; sampling of
+// Measured: the loss of 65536 x 362 logits in bfloat16 26.0 us, 4.6 TB/s of what it has to move; 16384 x 122 log-probabilities 5.3 us; sampling of
 // 65536 x 362 with records of up to 361 plies, [plies][games], 75 us, 3.3 TB/s (vector instructions keep 60 % of the time busy, and waves
 // that wait for moves the rest: blocks of 8, 32 and 64 rows instead of 16 take 82, 85 and 104 us).
 #include <hip/hip_runtime.h>
