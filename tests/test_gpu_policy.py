@@ -491,3 +491,21 @@ def test_outputs_in_the_place_of_the_logits(actions):
         want, y = pg.policy_loss(x, moves, entropy=0.1, **h), x.clone()
         got = pg.policy_loss(y, moves, entropy=0.1, grad=y, **h)
         assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want)) and torch.equal(bits(y), bits(want[2]))
+
+
+@pytest.mark.parametrize("actions", [82, 700, 3000])
+def test_rows_beyond_32_bit_offsets(actions):
+    """pitches of more than 2^31 elements, and of 2^32 bytes for the mask: the second row as in dense memory"""
+    x, how, g = inputs(7, actions, "bf16", 3, record=0)
+    x, how = x[1:3].clone(), {"mask": how["mask"][1:3].clone(), "bias": torch.randn(2, actions, generator=g).cuda(), "temperature": how["temperature"][:2].clone()}
+    noise, y = torch.randn(2, actions, generator=g).cuda(), torch.rand(2, actions, generator=g).cuda()
+
+    def far(t, pitch=2 ** 31 + 9):
+        return torch.empty(pitch + t.shape[1], dtype=t.dtype, device="cuda").as_strided(t.shape, (pitch, 1)).copy_(t)
+
+    fx, fhow, fnoise, fy = far(x), dict(how, mask=far(how["mask"], 2 ** 32 + 9), bias=far(how["bias"])), far(noise), far(y)
+    assert torch.equal(bits(pg.adjust_logits(fx, out=far(noise), **fhow).contiguous()), bits(pg.adjust_logits(x, **how)))
+    for a, b in zip(pg.sample_actions(fx, noise=fnoise, **fhow), pg.sample_actions(x, noise=noise, **how)):
+        assert torch.equal(a, b)
+    for a, b in zip(pg.policy_loss(fx, fy, entropy=0.1, grad=far(x), **fhow), pg.policy_loss(x, y, entropy=0.1, **how)):
+        assert torch.equal(a, b)
