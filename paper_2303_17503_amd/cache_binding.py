@@ -1,5 +1,6 @@
 """ctypes binding of the paged cache's entry points of libpgxgo.so; names follow include/pgxcache.h (pgxcache_<name> -> PagedCache.<name>)."""
 import ctypes as C
+import operator
 
 import torch
 
@@ -46,6 +47,17 @@ def _check(rc, what):
     if rc != 0:
         L = lib()
         raise PgxGoError(f"{what}: {L.pgxcache_strerror(rc).decode()} (code {rc}, hip error {L.pgxcache_last_hip_error()})")
+
+
+def _whole(x, name):
+    """a whole number that the entry points' 32 bits hold (ctypes would cut it off)"""
+    try:
+        n = operator.index(x)
+    except TypeError:
+        n = None
+    if n is None or not -2 ** 31 <= n < 2 ** 31:
+        raise PgxGoError(f"{name}: expected a whole number of 32 bits, got {x!r}")
+    return n
 
 
 class PagedCache:
@@ -141,8 +153,8 @@ class PagedCache:
         n, p = self._list(slots)
         each = isinstance(counts, torch.Tensor)
         if each: self._own(counts, torch.int32, (n,), "counts")
-        elif not 0 <= counts < 2 ** 31: raise PgxGoError(f"counts: 0 or more tokens, got {counts}")
-        _check(lib().pgxcache_advance(self._h, n, p, _ptr(counts) if each else None, 0 if each else int(counts), self._status(status, n)), "pgxcache_advance")
+        elif not 0 <= _whole(counts, "counts") < 2 ** 31: raise PgxGoError(f"counts: 0 or more tokens, got {counts}")
+        _check(lib().pgxcache_advance(self._h, n, p, _ptr(counts) if each else None, 0 if each else operator.index(counts), self._status(status, n)), "pgxcache_advance")
 
     def write(self, layer, k, v, slots=None):
         """Keys and values of the tokens that the slots' last advance made room for: [n][kv_heads][head_dim], or [n][tokens][kv_heads][head_dim]
@@ -157,7 +169,7 @@ class PagedCache:
         shape = (n, tokens, self.kv_heads, self.head_dim) if many else (n, self.kv_heads, self.head_dim)
         kp, vp = self._heads(k, shape, "k"), self._heads(v, shape, "v")
         ks, vs = ((t.stride(0), t.stride(1) if many else 0, t.stride(-2)) for t in (k, v))
-        _check(lib().pgxcache_write(self._h, int(layer), n, p, tokens, kp, *ks, vp, *vs), "pgxcache_write")
+        _check(lib().pgxcache_write(self._h, _whole(layer, "layer"), n, p, tokens, kp, *ks, vp, *vs), "pgxcache_write")
 
     def attend(self, layer, q, slots=None, k=None, v=None, scale=None, out=None, lse=False):
         """Attention of one token per slot, q [n][heads][head_dim], over the slot's tokens; heads a multiple of kv_heads; scale: head_dim ** -0.5.
@@ -189,7 +201,7 @@ class PagedCache:
         op = self._heads(out, (n, heads, self.head_dim), "out")
         if lse is True: lse = made
         elif lse is not False: self._own(lse, torch.float32, (n, heads), "lse")
-        _check(lib().pgxcache_attend(self._h, int(layer), n, p, heads, qp, *q.stride()[:2], kp, *ks, vp, *vs, float(scale), op, *out.stride()[:2],
+        _check(lib().pgxcache_attend(self._h, _whole(layer, "layer"), n, p, heads, qp, *q.stride()[:2], kp, *ks, vp, *vs, float(scale), op, *out.stride()[:2],
                                      None if lse is False else lse.data_ptr()), "pgxcache_attend")
         return out if lse is False else (out, lse)
 

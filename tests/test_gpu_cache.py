@@ -727,3 +727,16 @@ def test_a_pool_with_more_pages_than_lds_holds_bits_for():
             cache.compact(used)
             assert int(used) == ref.compact()
             same(cache, ref)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_numbers_of_tokens_and_layers_are_whole(native, monkeypatch):
+    cache, q, k = cache_and_more()
+    if not native:
+        monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    for call in (lambda: cache.advance(counts=1.5), lambda: cache.advance(counts=None), lambda: cache.attend(0.7, q), lambda: cache.write(1.2, k, k), lambda: cache.write("0", k, k), lambda: cache.attend(2 ** 32, q), lambda: cache.write(2 ** 32 + 1, k, k)):
+        with pytest.raises(pg.PgxGoError):
+            call()
+    assert cache.lengths.tolist() == [20, 5]
+    cache.advance(counts=torch.ones(1, dtype=torch.int64).numpy()[0])
+    assert cache.lengths.tolist() == [21, 6]
