@@ -12,11 +12,23 @@
  *   lengths_dev [slots] int32: tokens of the slot
  *   refs_dev    [pages] int32: how many table entries name the page; 0: free
  *   work_dev    pgxcache_work_bytes(): what the calls need between themselves; nothing of it has to be saved
+ *   scales_dev  8 bits only: [pages][layers][2][kv_heads][page_size / 16] float32
  * Only full pages are shared: a partly filled last page belongs to one slot.
  * The calls read table, lengths and refs as they find them; a page number outside the pool is never followed.
  *
  * Conventions are those of pgxgo.h: asynchronous on the stream given at the beginning, no allocation, no synchronisation,
  * negative codes, nothing throws or aborts.  One handle's calls share work_dev and belong on one stream.
+ *
+ * Held in 8 bits (pgxcache_init_e4m3): kv_dev has elements of 8 bits in the same order, e4m3 codes (4 bits of exponent, 3 of fraction, up to
+ * 448, no infinities).  An element is its code times the scale of its block: 16 tokens of a slot, from a multiple of 16 on, in one layer and head, keys or values.
+ * `type` is that of the queries, keys, values and outputs of the calls.  Writing tokens into a block:
+ *     m = the largest finite magnitude among the block's elements that the call writes
+ *     s = the smallest power of two with m <= 448 s, at least 2^-100
+ *     if tokens of the block were there before those that the call writes:  s = max(s, the block's scale), and where that makes the scale larger,
+ *         their codes become  to nearest, ties to even (code * old scale / s)
+ *     code = to nearest, ties to even (x / s);  NaN where x is not finite
+ * so a value is held to 2^-4 of itself, or of 2^-6 s where it is smaller.  A slot's tokens are written in their order: what a block holds behind the
+ * tokens that a call writes is given up.  Scales in memory that the caller fills are finite and above 0; if one is no power of two, x / s may be rounded twice.
  *
  * Lists of slots: slots_dev[n] int32, n <= slots, pairwise distinct; NULL: slots 0 .. n-1.  An entry of -1 is left out (as action
  * -1 in the environments), an entry outside [-1, slots) touches nothing.  status_dev (nullable, uint8 [n]): 0 done (or left out),
@@ -68,6 +80,9 @@ size_t pgxcache_work_bytes(const pgxcache_opts* opts);
  * refs_dev, which leaves all else as it is. */
 int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
                   void* work_dev, size_t work_bytes);
+/* The same for keys and values held in 8 bits; scales_dev 4-byte aligned. */
+int pgxcache_init_e4m3(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, float* scales_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
+                       void* work_dev, size_t work_bytes);
 int pgxcache_destroy(pgxcache_t h); /* frees the host handle only */
 int pgxcache_rescan(pgxcache_t h);
 
@@ -82,6 +97,12 @@ int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const in
 int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t tokens, const void* k_dev, int64_t k_entry_stride,
                    int64_t k_token_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride, int64_t v_token_stride, int64_t v_head_stride);
 
+/* Keys and values as they are held (a copy, or code * scale rounded to `type`): the tokens first_dev[i] (NULL: `first`), ... + tokens - 1 of each slot, in one layer, to
+ * element [i][t][head][.] at i * entry_stride + t * token_stride + head * head_stride, which may not overlap.  Zeros where a slot has no such token, and
+ * for an entry that is no slot.  Entries may repeat. */
+int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, const int32_t* first_dev, int32_t first, int32_t tokens, void* k_dev,
+                  int64_t k_entry_stride, int64_t k_token_stride, int64_t k_head_stride, void* v_dev, int64_t v_entry_stride, int64_t v_token_stride, int64_t v_head_stride);
+
 /* Attention of one token per entry over all tokens of its slot, in one layer:
  *     out[i][h] = sum_t softmax_t(scale * q[i][h] . K[t][h / group]) V[t][h / group],     group = heads / kv_heads
  * q_dev, out_dev: elements of the cache's type, [i][h][.] at i * entry_stride + h * head_stride (those of the output may not
@@ -91,6 +112,7 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
  * ignored), so that a step takes one launch per layer; without them entries may repeat.  A slot without tokens, and an entry that is no slot, gives zeros and -infinity.
  * Scores, sums and the output before its rounding are held in 32 bits; probabilities are multiplied as two numbers of the
  * cache's type that add up to them within 2^-17 (float16: of the sum of 32 tokens' probabilities), however small they are.
+ * With elements of 8 bits the probabilities, times the values' scales, are two bfloat16 numbers whatever `type` is.
  * A key or value that is infinite or NaN makes what it counts for NaN; places behind a slot's last token may hold anything. */
 int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t heads, const void* q_dev, int64_t q_entry_stride,
                     int64_t q_head_stride, const void* k_dev, int64_t k_entry_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride,

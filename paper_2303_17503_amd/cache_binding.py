@@ -8,6 +8,7 @@ from . import binding
 from .binding import PgxGoError, _address, _need, _ptr, lib as _golib
 
 TYPES = {torch.float16: 1, torch.bfloat16: 2}
+E4M3, BLOCK = torch.float8_e4m3fn, 16   # elements held in 8 bits; tokens that share a scale
 HEAD_DIMS = (32, 64, 96, 128, 256)
 NO_PAGES, FULL, BAD_ENTRY = 1, 2, 255
 _ready = False
@@ -27,11 +28,13 @@ def lib():
         L.pgxcache_work_bytes.restype = C.c_size_t
         L.pgxcache_work_bytes.argtypes = [C.POINTER(_Opts)]
         L.pgxcache_init.argtypes = [C.POINTER(vp), C.POINTER(_Opts), vp, vp, vp, vp, vp, C.c_size_t]
+        L.pgxcache_init_e4m3.argtypes = [C.POINTER(vp), C.POINTER(_Opts), vp, vp, vp, vp, vp, vp, C.c_size_t]
         L.pgxcache_destroy.argtypes = [vp]
         L.pgxcache_rescan.argtypes = [vp]
         L.pgxcache_advance.argtypes = [vp, i32, vp, vp, i32, vp]
         L.pgxcache_write.argtypes = [vp, i32, i32, vp, i32, vp, i64, i64, i64, vp, i64, i64, i64]
         L.pgxcache_attend.argtypes = [vp, i32, i32, vp, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, C.c_float, vp, i64, i64, vp]
+        L.pgxcache_read.argtypes = [vp, i32, i32, vp, vp, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64]
         L.pgxcache_fork.argtypes = [vp, i32, vp, vp, vp]
         L.pgxcache_free.argtypes = [vp, i32, vp]
         L.pgxcache_compact.argtypes = [vp, vp]
@@ -66,14 +69,29 @@ class PagedCache:
     The memory is the caller's: kv [pages][layers][2][kv_heads][page_size][head_dim] in float16 or bfloat16, table int32 [slots][width],
     lengths int32 [slots], refs int32 [pages].  The handle takes them as they are (PagedCache.empty makes empty ones), so a cache
     is saved by copying the four and restored by making a handle on them; after writing to refs oneself, call rescan().
+    Held in 8 bits: kv in float8_e4m3fn, with scales, float32 [pages][layers][2][kv_heads][page_size / 16], one for each 16 tokens of a head (copied
+    and saved with kv); dtype, float16 or bfloat16, is then what queries, keys, values and outputs of the calls have.
     All calls run on the stream that was current when the handle was made, and attend's new outputs belong to it, whichever stream is
     current: a program that works on another one has the two wait for each other, as for tensors of any other stream."""
 
-    def __init__(self, kv, table, lengths, refs):
+    def __init__(self, kv, table, lengths, refs, scales=None, dtype=None):
         L = lib()
-        if not isinstance(kv, torch.Tensor) or kv.dtype not in TYPES or kv.dim() != 6 or kv.shape[2] != 2 or not kv.is_cuda or not kv.is_contiguous():
-            raise PgxGoError("kv: expected a contiguous cuda tensor [pages][layers][2][kv_heads][page_size][head_dim] of float16 or bfloat16")
+        if (not isinstance(kv, torch.Tensor) or (kv.dtype not in TYPES and kv.dtype is not E4M3) or kv.dim() != 6 or kv.shape[2] != 2 or not kv.is_cuda
+                or not kv.is_contiguous()):
+            raise PgxGoError("kv: expected a contiguous cuda tensor [pages][layers][2][kv_heads][page_size][head_dim] of float16, bfloat16 or float8_e4m3fn")
         pages, self.layers, _, self.kv_heads, self.page_size, self.head_dim = kv.shape
+        if kv.dtype is E4M3:
+            if dtype not in TYPES:
+                raise PgxGoError(f"dtype: the calls' type beside 8 bits, torch.float16 or torch.bfloat16, got {dtype}")
+            if not isinstance(scales, torch.Tensor):
+                raise PgxGoError("scales: expected float32 [pages][layers][2][kv_heads][page_size / 16] beside elements of 8 bits")
+            _need(scales, torch.float32, (pages, self.layers, 2, self.kv_heads, self.page_size // BLOCK), "scales")
+            if scales.device != kv.device:
+                raise PgxGoError(f"scales have to be on {kv.device}, as kv is")
+        elif scales is not None or dtype not in (None, kv.dtype):
+            raise PgxGoError(f"scales and dtype are about elements of 8 bits: kv has {kv.dtype}")
+        else:
+            dtype = kv.dtype
         if getattr(table, "ndim", 0) != 2:
             raise PgxGoError("table: expected int32 [slots][width]")
         self.slots, self.width = table.shape
@@ -82,17 +100,19 @@ class PagedCache:
         _need(refs, torch.int32, (pages,), "refs")
         if any(t.device != kv.device for t in (table, lengths, refs)):
             raise PgxGoError(f"table, lengths and refs have to be on {kv.device}, as kv is")
-        self.pages, self.dtype, self.device = pages, kv.dtype, kv.device
-        self.kv, self.table, self.lengths, self.refs = kv, table, lengths, refs
+        self.pages, self.dtype, self.device = pages, dtype, kv.device
+        self.kv, self.table, self.lengths, self.refs, self.scales = kv, table, lengths, refs, scales
         with torch.cuda.device(self.device):
             self._stream = torch.cuda.current_stream(self.device)
-            opts = _Opts(self.slots, pages, self.width, self.page_size, self.layers, self.kv_heads, self.head_dim, TYPES[kv.dtype], self._stream.cuda_stream)
+            opts = _Opts(self.slots, pages, self.width, self.page_size, self.layers, self.kv_heads, self.head_dim, TYPES[dtype], self._stream.cuda_stream)
             nbytes = L.pgxcache_work_bytes(C.byref(opts))
             if nbytes == 0:
                 raise PgxGoError(f"cache: pages of a power of two from 16 to 1024 tokens, heads of {HEAD_DIMS} elements; got {self.page_size} and {self.head_dim}")
             self._work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
             h = C.c_void_p()
-            _check(L.pgxcache_init(C.byref(h), C.byref(opts), _ptr(kv), _ptr(table), _ptr(lengths), _ptr(refs), _ptr(self._work), nbytes), "pgxcache_init")
+            rest = _ptr(table), _ptr(lengths), _ptr(refs), _ptr(self._work), nbytes
+            if scales is None: _check(L.pgxcache_init(C.byref(h), C.byref(opts), _ptr(kv), *rest), "pgxcache_init")
+            else: _check(L.pgxcache_init_e4m3(C.byref(h), C.byref(opts), _ptr(kv), _ptr(scales), *rest), "pgxcache_init_e4m3")
         self._h, self._destroy = h, L.pgxcache_destroy
         if _fast is not None:
             self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "attend", "fork", "free")}
@@ -100,12 +120,15 @@ class PagedCache:
         self._scale = self.head_dim ** -0.5
 
     @classmethod
-    def empty(cls, slots, pages, max_length, layers, kv_heads, head_dim, page_size=16, dtype=torch.bfloat16, device="cuda:0"):
-        """An empty cache of slots that hold up to max_length tokens each (rounded up to whole pages)."""
-        kv = torch.empty((pages, layers, 2, kv_heads, page_size, head_dim), dtype=dtype, device=device)
+    def empty(cls, slots, pages, max_length, layers, kv_heads, head_dim, page_size=16, dtype=torch.bfloat16, device="cuda:0", bits=16):
+        """An empty cache of slots that hold up to max_length tokens each (rounded up to whole pages), elements in 16 bits (of dtype) or 8."""
+        if bits not in (8, 16):
+            raise PgxGoError(f"bits: 8 or 16, got {bits}")
+        kv = torch.empty((pages, layers, 2, kv_heads, page_size, head_dim), dtype=dtype if bits == 16 else E4M3, device=device)
+        scales = None if bits == 16 else torch.ones((pages, layers, 2, kv_heads, page_size // BLOCK), dtype=torch.float32, device=device)
         table = torch.full((slots, (max_length + page_size - 1) // page_size), -1, dtype=torch.int32, device=device)
         zeros = lambda n: torch.zeros(n, dtype=torch.int32, device=device)  # noqa: E731
-        return cls(kv, table, zeros(slots), zeros(pages))
+        return cls(kv, table, zeros(slots), zeros(pages), scales, None if bits == 16 else dtype)
 
     def __del__(self):
         h, self._h = getattr(self, "_h", None), None
@@ -170,6 +193,23 @@ class PagedCache:
         kp, vp = self._heads(k, shape, "k"), self._heads(v, shape, "v")
         ks, vs = ((t.stride(0), t.stride(1) if many else 0, t.stride(-2)) for t in (k, v))
         _check(lib().pgxcache_write(self._h, _whole(layer, "layer"), n, p, tokens, kp, *ks, vp, *vs), "pgxcache_write")
+
+    def read(self, layer, tokens, slots=None, first=0, k=None, v=None):
+        """(keys, values) of the slots' tokens first, first + 1, ... (a number, or int32 [n]), `tokens` of them, as they are held, in the calls' type:
+        [n][tokens][kv_heads][head_dim] (new ones belong to the cache's stream).  Zeros where a slot has no such token; entries may repeat."""
+        n, p = self._list(slots)
+        tokens = _whole(tokens, "tokens")
+        each = isinstance(first, torch.Tensor)
+        if each: self._own(first, torch.int32, (n,), "first")
+        elif _whole(first, "first") < 0: raise PgxGoError(f"first: 0 or more, got {first}")
+        if tokens < 0: raise PgxGoError(f"tokens: 0 or more, got {tokens}")
+        shape = (n, tokens, self.kv_heads, self.head_dim)
+        with torch.cuda.stream(self._stream):
+            k, v = (torch.empty(shape, dtype=self.dtype, device=self.device) if t is None else t for t in (k, v))
+        kp, vp = self._heads(k, shape, "k"), self._heads(v, shape, "v")
+        _check(lib().pgxcache_read(self._h, _whole(layer, "layer"), n, p, _ptr(first) if each else None, 0 if each else operator.index(first), tokens,
+                                   kp, *k.stride()[:3], vp, *v.stride()[:3]), "pgxcache_read")
+        return k, v
 
     def attend(self, layer, q, slots=None, k=None, v=None, scale=None, out=None, lse=False):
         """Attention of one token per slot, q [n][heads][head_dim], over the slot's tokens; heads a multiple of kv_heads; scale: head_dim ** -0.5.

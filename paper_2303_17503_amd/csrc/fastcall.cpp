@@ -14,6 +14,7 @@
 
 #include "pgxcache.h"
 #include "pgxpolicy.h"
+#include "pgxrotary.h"
 
 namespace {
 
@@ -485,6 +486,62 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   });
 }
 
+// ---- rotary positions ------------------------------------------------------------------------------------------------------------------
+// a tensor, or a tuple or list of one or two; the number of them, 0: neither
+int take_tensors(PyObject* o, PyObject** items) {
+  if (PyTuple_CheckExact(o) || PyList_CheckExact(o)) {
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    if (n < 1 || n > PGXROTARY_MAX_PARTS) return 0;
+    for (Py_ssize_t k = 0; k < n; ++k)
+      if (!tensor(items[k] = PySequence_Fast_GET_ITEM(o, k))) return 0;
+    return (int)n;
+  }
+  items[0] = o;
+  return tensor(o) ? 1 : 0;
+}
+// (address, x, positions, frequencies, interleaved, magnitude, inverse, out); returns the outputs as a tuple
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded_outputs([&]() -> PyObject* {
+    PyObject *xs[PGXROTARY_MAX_PARTS], *given[PGXROTARY_MAX_PARTS] = {Py_None, Py_None};
+    at::Tensor outs[PGXROTARY_MAX_PARTS];
+    pgxrotary_part parts[PGXROTARY_MAX_PARTS];
+    void* stream;
+    float magnitude;
+    const int n = n_args == 8 ? take_tensors(a[1], xs) : 0;
+    if (n == 0) return nullptr;
+    const at::Tensor &first = *tensor(xs[0]), *p = tensor(a[2]), *f = tensor(a[3]);
+    const auto type = first.scalar_type();
+    const int64_t dim = first.dim();
+    if (!first.is_cuda() || (dim != 3 && dim != 4) || (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) || first.numel() == 0) return nullptr;
+    const int64_t D = first.size(-1), entries = first.size(0), tokens = dim == 4 ? first.size(1) : 1;
+    if (entries * tokens > INT32_MAX || D > PGXROTARY_MAX_HEAD_DIM) return nullptr;
+    if (!p || p->scalar_type() != kInt || p->device() != first.device() || p->dim() != dim - 2 || p->size(0) != entries || (dim == 4 && p->size(1) != tokens)) return nullptr;
+    if (!f || f->scalar_type() != at::kDouble || f->device() != first.device() || f->dim() != 1 || !f->is_contiguous() || f->size(0) < 1 || 2 * f->size(0) > D) return nullptr;
+    if (!number(a[5], &magnitude) || !std::isfinite(magnitude)) return nullptr;
+    const int interleaved = PyObject_IsTrue(a[4]), inverse = PyObject_IsTrue(a[6]);
+    if (interleaved < 0 || inverse < 0) return nullptr;
+    if (a[7] != Py_None && take_tensors(a[7], given) != n) return nullptr;
+    const c10::DeviceGuard guard(first.device());
+    for (int k = 0; k < n; ++k) {
+      const at::Tensor& x = *tensor(xs[k]);
+      if (x.scalar_type() != type || x.device() != first.device() || x.dim() != dim || x.size(0) != entries || (dim == 4 && x.size(1) != tokens) || x.size(-1) != D ||
+          x.size(-2) > 65536 || !dense_rows(x) || !output(given[k], x.sizes(), type, first.device(), &outs[k]))
+        return nullptr;
+      const at::Tensor& o = outs[k];
+      parts[k] = pgxrotary_part{data_or_null(x), x.stride(0), dim == 4 ? x.stride(1) : 0, x.stride(-2), data_or_null(o), o.stride(0), dim == 4 ? o.stride(1) : 0, o.stride(-2),
+                                (int32_t)x.size(-2)};
+    }
+    if (!current_stream(first.device(), &stream)) return nullptr;
+    auto* fn = (decltype(&pgxrotary_turn))pointer(a[0]);
+    const int rc = without_gil([&] {
+      return fn((int32_t)entries, (int32_t)tokens, (int32_t)D, (int32_t)(2 * f->size(0)), type == at::kFloat ? PGXROTARY_F32 : type == at::kHalf ? PGXROTARY_F16 : PGXROTARY_BF16,
+                (const int32_t*)p->data_ptr(), p->stride(0), dim == 4 ? p->stride(1) : 0, (const double*)f->data_ptr(), magnitude, interleaved, inverse, n, parts, stream);
+    });
+    if (n == 1) return outputs(rc, {{given[0], outs[0]}});
+    return outputs(rc, {{given[0], outs[0]}, {given[1], outs[1]}});
+  });
+}
+
 PyMethodDef kMethods[] = {
     {"step", (PyCFunction)(void*)step, METH_FASTCALL, nullptr},
     {"step_sample", (PyCFunction)(void*)step_sample, METH_FASTCALL, nullptr},
@@ -499,6 +556,7 @@ PyMethodDef kMethods[] = {
     {"cache_free", (PyCFunction)(void*)cache_free, METH_FASTCALL, nullptr},
     {"cache_write", (PyCFunction)(void*)cache_write, METH_FASTCALL, nullptr},
     {"cache_attend", (PyCFunction)(void*)cache_attend, METH_FASTCALL, nullptr},
+    {"rotate", (PyCFunction)(void*)rotate, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -11,34 +11,11 @@
 #include <new>
 #include <type_traits>
 
-#include "pgxcache.h"
-
-constexpr int kNoTail = -1, kSkip = -2;
-struct __attribute__((aligned(16))) pgxcache_fork_entry {   // an entry of a fork call as its plan leaves it, so that the copying starts after one look at memory
-  int32_t tail;            // the page for the copy of the last page, kNoTail or kSkip
-  int32_t src, dst, length;
-  int32_t last;            // the source's partly filled last page
-  int32_t old;             // pages of the destination
-  int32_t unused[2];
-};
-
-struct pgxcache_ctx {
-  pgxcache_opts o;
-  void* kv;
-  int32_t *table, *lengths, *refs;
-  uint64_t* free_bits;     // a bit per page: free; 0 behind the last page
-  uint64_t* taken;         // the same shape: pages given out by a plan and still marked free; 0 between calls
-  int32_t* grown;          // [slots] tokens that the slot's last advance made room for
-  int32_t* plan;           // [slots] advance: whether the entry is done
-  pgxcache_fork_entry* forks;   // [slots] what fork does with its entries
-  int32_t* moved_to;       // [pages] compact: where a page at or above `used` goes
-  int2* moves;             // [pages] compact: (from, to)
-  int32_t* counts;         // compact: used, number of moves
-  uint32_t* arrived;       // [kSplitBlocks] attend: blocks of a row that are done, 0 between calls
-  float* partial;          // attend: what they found
-};
+#include "cache_common.hpp"
 
 namespace {
+
+using namespace pgxcache_parts;
 
 thread_local int g_last_hip = 0;
 
@@ -52,30 +29,6 @@ thread_local int g_last_hip = 0;
   } while (0)
 
 constexpr int kOneBlock = 1024;      // threads of the kernels that give out pages
-typedef pgxcache_fork_entry ForkEntry;
-constexpr int kSplitBlocks = 512;    // most blocks of an attend call that splits rows
-constexpr int kMostSplits = 128;     // most blocks of one row
-constexpr int kHeads = 16;           // query heads of a matrix tile
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4_2 __attribute__((aligned(2)));
-
-// what every kernel knows of the cache
-struct Cache {
-  char* kv;
-  int32_t *table, *lengths, *refs;
-  uint64_t *free_bits, *taken;
-  int32_t* grown;
-  int32_t slots, pages, width, page_shift, layers, kv_heads, head_dim;
-
-  __device__ __forceinline__ int pages_of(int tokens) const { return (int)(((int64_t)tokens + (1 << page_shift) - 1) >> page_shift); }
-  __device__ __forceinline__ int capacity() const { return (int)min((int64_t)width << page_shift, (int64_t)0x7FFFFFFF); }
-  __device__ __forceinline__ int length(int slot) const { return min(max(lengths[slot], 0), capacity()); }
-  __device__ __forceinline__ int32_t* row(int slot) const { return table + (int64_t)slot * width; }
-  __device__ __forceinline__ bool is_page(int p) const { return (uint32_t)p < (uint32_t)pages; }
-  __host__ __device__ __forceinline__ int64_t head_bytes() const { return ((int64_t)head_dim << page_shift) * 2; }      // one head's keys or values of a page
-  __host__ __device__ __forceinline__ int64_t page_bytes() const { return head_bytes() * kv_heads * 2 * layers; }
-};
 
 // Pages that come free in a block.  Those of one word of the bits are gathered in LDS, so that a word is written once: pages given out together
 // often come free together, and 64 blocks that each add one to the same word take 4 us.
@@ -485,8 +438,13 @@ __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const ForkEnt
     int now0 = -1, before0 = -1;
     if (tid < most) entry(tid, &now0, &before0);
     constexpr int kAhead = 8;
-    const uint32_t units = (uint32_t)(filled * c.head_dim / 8), all = c.is_page(last) ? (uint32_t)(c.layers * 2 * c.kv_heads) * units : 0;
+    const uint32_t heads = (uint32_t)(c.layers * 2 * c.kv_heads), units = (uint32_t)(filled * c.head_dim * c.element_bytes() / 16), all = c.is_page(last) ? heads * units : 0;
     const uint32_t head = (uint32_t)(c.head_bytes() / 16);
+    // the filled blocks' scales of every head
+    const uint32_t blocks = (uint32_t)(filled + (1 << kBlockShift) - 1) >> kBlockShift, all_scales = c.scales && c.is_page(last) ? heads * blocks : 0;
+    auto scale_at = [&](uint32_t u) { return u / blocks * (uint32_t)c.page_blocks() + u % blocks; };
+    float scale0 = 0.0f;
+    if ((uint32_t)tid < all_scales) scale0 = c.scales[last * c.page_scales() + scale_at((uint32_t)tid)];
     const u32x4* a = (const u32x4*)(c.kv + last * c.page_bytes());
     u32x4* b = (u32x4*)(c.kv + tail * c.page_bytes());
     for (uint32_t u = (uint32_t)tid; u < all; u += (uint32_t)per * kAhead) {   // the filled beginning of every head's keys and values
@@ -502,6 +460,8 @@ __global__ void __launch_bounds__(256) fork_kernel(Cache c, int n, const ForkEnt
       for (int k = 0; k < kAhead; ++k)
         if (u + (uint32_t)(k * per) < all) b[at[k]] = x[k];
     }
+    for (uint32_t u = (uint32_t)tid; u < all_scales; u += (uint32_t)per)
+      c.scales[tail * c.page_scales() + scale_at(u)] = u == (uint32_t)tid ? scale0 : c.scales[last * c.page_scales() + scale_at(u)];
     if (tid < most) exchange(tid, now0, before0);
     for (int k = tid + per; k < most; k += per) {
       int now, before;
@@ -579,13 +539,11 @@ __global__ void __launch_bounds__(256) compact_move_kernel(Cache c, const int2* 
     const u32x4* a = (const u32x4*)(c.kv + move.x * c.page_bytes());
     u32x4* b = (u32x4*)(c.kv + move.y * c.page_bytes());
     for (int64_t u = threadIdx.x; u < units; u += 256) b[u] = a[u];
+    if (c.scales)
+      for (int64_t u = threadIdx.x; u < c.page_scales(); u += 256) c.scales[move.y * c.page_scales() + u] = c.scales[move.x * c.page_scales() + u];
   }
 }
 
-struct Tokens {   // keys or values of new tokens
-  const char* p;
-  int64_t entry, token, head;   // strides in bytes
-};
 
 // A thread per 16 bytes of a head's key or value and four tokens.
 constexpr int kTokensPerThread = 4;
@@ -606,7 +564,7 @@ __global__ void __launch_bounds__(256) write_kernel(Cache c, int layer, int n, c
   const uint32_t head = value ? which - (uint32_t)c.kv_heads : which;
   const Tokens& from = value ? v : k;
   const char* p = from.p + i * from.entry + head * from.head + at;
-  char* to = c.kv + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes() + at;
+  char* to = c.kv + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes(2) + at;
   const int32_t* row = c.row(slot);
   u32x4 data[kTokensPerThread];
   int page[kTokensPerThread];
@@ -619,7 +577,7 @@ __global__ void __launch_bounds__(256) write_kernel(Cache c, int layer, int n, c
 #pragma unroll
   for (int j = 0; j < kTokensPerThread; ++j)
     if (t0 + j < grown && c.is_page(page[j]))
-      *(u32x4*)(to + page[j] * c.page_bytes() + (int64_t)((first + t0 + j) & ((1 << c.page_shift) - 1)) * c.head_dim * 2) = data[j];
+      *(u32x4*)(to + page[j] * c.page_bytes(2) + (int64_t)((first + t0 + j) & ((1 << c.page_shift) - 1)) * c.head_dim * 2) = data[j];
 }
 
 // ---- attention of one token per entry ------------------------------------------------------------------------------------------------
@@ -633,67 +591,11 @@ __global__ void __launch_bounds__(256) write_kernel(Cache c, int layer, int n, c
 // index 8 g + j there means token 4 g + j for j < 4 and 16 + 4 g + j - 4 above.  V is read along its rows, the lane taking elements
 // c D/16 ... of its 8 tokens; a byte permutation per two values turns them into left operands, the m-th of which has row c stand for
 // element c D/16 + m.  The result then has elements (4 g + r) D/16 + m in the lane: D/4 neighbouring ones per lane.
-struct AttendArgs {
-  const char *q, *k, *v;
-  char* out;
-  float* lse;
-  int64_t q_entry, q_head, k_entry, k_head, v_entry, v_head, out_entry, out_head;   // bytes
-  const int32_t* slots;
-  float* partial;
-  uint32_t* arrived;
-  int32_t n, layer, heads, group, head_tiles, splits;
-  float scale;   // times log2 e
-};
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef f32x4 f32x4_4 __attribute__((aligned(4)));
-
-// Probabilities go into the second product as two numbers of the type that add up to them, relative to an exponent that is moved only when a tile
-// requires it, so that most tiles need no exchange between lanes.
-//  * bfloat16 has the range of 32 bits: the sum is within 2^-17 of p whatever its size.  The exponent is the running maximum, raised when a score passes it by 2^8.
-//  * float16 ends at 65504 and at steps of 2^-24: the sum is within 2^-22 of p or within 2^-25.  The exponent goes up and down with the tiles, so that the
-//    largest p of a head in a tile is between 2^-3 and 2^15 (2^11 where it is moved), and the tile's 32 errors add up to 2^-17 of the tile's sum at most.  It goes no further down than 2^60
-//    below the largest score, where nothing counts any more and the sums stay far from the end of 32 bits.  With the running maximum for exponent, p
-//    below 2^-25 of it was lost (721 tokens at e^-15 beside one: 0.7 % of what they add), and the time is the same.
-struct F16 {
-  typedef _Float16 elem;
-  static constexpr bool kNarrow = true;
-  static constexpr float kRoom = 11.0f, kMost = 15.0f, kLeast = -3.0f, kDepth = 60.0f;
-  typedef elem x8 __attribute__((ext_vector_type(8)));
-  static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-};
-struct BF16 {
-  typedef __bf16 elem;
-  static constexpr bool kNarrow = false;
-  static constexpr float kRoom = 0.0f, kMost = 8.0f, kLeast = 0.0f, kDepth = 0.0f;
-  typedef elem x8 __attribute__((ext_vector_type(8)));
-  static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-};
-
-constexpr float kLn2 = 0.69314718055994530942f;
-
-__device__ __forceinline__ float across_groups_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float across_groups_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
-
-// What one block leaves for another of the same launch goes through the dies' L2 caches, which do not know of each other, without
-// writing back or dropping anything else in them: a device-wide fence per block instead cost 20 us each, 32 us with 3 sequences of 110000 tokens.
-constexpr int kAcrossDies = 16;             // cache policy of a buffer instruction: as an atomic access of the whole device (sc1)
-constexpr int kBufferFlags = 0x00027000;    // raw buffer of 32-bit words
-
 template <int NT>
 struct Tile {   // 32 tokens: keys [half][32-element part], values [token][dword]
   u32x4 k[2][NT];
   uint32_t v[8][NT];
 };
-
-template <bool STREAM, class V>
-__device__ __forceinline__ V read_once(const V* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; }
 
 // W wavefronts share a row (an entry and a key head); with four a row may also be split over blocks.  STREAM: keys and values are read with
 // the hint that they are not read again soon.
@@ -701,8 +603,6 @@ template <class T, int NT, int W, bool STREAM>
 __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c, AttendArgs a) {
   typedef typename T::x8 x8;
   constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
-  __shared__ float joined_m[W][kHeads], joined_l[W][kHeads];
-  extern __shared__ float joined_o[];   // [W - 1][kHeads][D]
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   // head tiles and key heads are next to each other in the launch, then the parts of a sequence: what runs together reads neighbouring memory
   const uint32_t place = blockIdx.x, per_part = (uint32_t)(c.kv_heads * a.head_tiles);
@@ -742,7 +642,7 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
   if (split >= active) return;
   const int begin = split * chunk, end = min(tiles, begin + chunk);
 
-  const int64_t page_bytes = c.page_bytes(), head_bytes = c.head_bytes();
+  const int64_t page_bytes = c.page_bytes(2), head_bytes = c.head_bytes(2);
   const char* keys = c.kv + ((int64_t)a.layer * 2 * c.kv_heads + kv_head) * head_bytes;
   const char* values = keys + c.kv_heads * head_bytes;
   const int in_page = (1 << c.page_shift) - 1;
@@ -871,158 +771,7 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
       compute(t0, number, outer);
     }
   }
-  sum = across_groups_sum(sum);
-
-  if (W > 1 && !alone) {   // the wavefronts' parts, into the first's registers
-    if (g == 0) { joined_m[wave][col] = top; joined_l[wave][col] = sum; }
-    __syncthreads();
-    float now = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < W; ++w) now = fmaxf(now, joined_m[w][col]);
-    const float from = now > -INFINITY ? now : 0.0f, factor = __builtin_amdgcn_exp2f(top - from);
-    sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) sum += joined_l[w][col] * __builtin_amdgcn_exp2f(joined_m[w][col] - from);
-    top = now;
-#pragma unroll
-    for (int m = 0; m < 2 * NT; ++m) acc[m] *= factor;
-    if (wave > 0) {
-#pragma unroll
-      for (int m = 0; m < 2 * NT; ++m)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) joined_o[((wave - 1) * 8 * NT + m * 4 + r) * 64 + lane] = acc[m][r];
-    }
-    __syncthreads();
-    if (wave == 0) {
-#pragma unroll
-      for (int w = 0; w < W - 1; ++w)
-#pragma unroll
-        for (int m = 0; m < 2 * NT; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[m][r] += joined_o[(w * 8 * NT + m * 4 + r) * 64 + lane];
-    }
-  }
-
-  if (active == 1) {
-    if (wave > 0) return;
-    if (col >= heads_here) return;
-    const float inverse = 1.0f / sum;
-    char* out = a.out + i * a.out_entry + (head0 + col) * a.out_head + g * kOut * 2;
-#pragma unroll
-    for (int u = 0; u < NT; ++u) {
-      x8 x;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (typename T::elem)(acc[(u * 8 + e) % (2 * NT)][(u * 8 + e) / (2 * NT)] * inverse);
-      *(u32x4_2*)(out + u * 16) = __builtin_bit_cast(u32x4, x);
-    }
-    if (a.lse && g == 0) a.lse[(int64_t)i * a.heads + head0 + col] = (top + __log2f(sum)) * kLn2;
-    return;
-  }
-
-  // The row is split over `active` blocks: each leaves its part in memory, and the one that comes last joins them, in an order of its own.
-  // All its loads are of 16 bytes and under way together: with 4-byte ones, one output each, joining 256 parts of 8 heads of 128 took 40 us.
-  if constexpr (W >= 4) {
-    constexpr int kPart = kHeads * (D + 2), kThreads = 64 * W, kPer = kMostSplits / (4 * W), kJoin = NT < 8 ? 16 : 8;
-    const uint32_t part_bytes = kPart * 4;
-    float* parts = a.partial + (int64_t)unit * a.splits * kPart;
-    const auto memory = __builtin_amdgcn_make_buffer_rsrc(parts, 0, a.splits * part_bytes, kBufferFlags);
-    if (wave == 0 && col < heads_here) {
-      const uint32_t at = (uint32_t)split * part_bytes;
-      if (g == 0) {
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(top), memory, at + col * 4, 0, kAcrossDies);
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), memory, at + (kHeads + col) * 4, 0, kAcrossDies);
-      }
-#pragma unroll
-      for (int u = 0; u < kOut / 4; ++u) {
-        f32x4 x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = acc[(u * 4 + e) % (2 * NT)][(u * 4 + e) / (2 * NT)];
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), memory, at + (2 * kHeads + col * D + g * kOut + u * 4) * 4, 0, kAcrossDies);
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // they are where every die sees them
-    }
-    __shared__ int is_last;
-    __syncthreads();
-    if (threadIdx.x == 0) is_last = atomicAdd(&a.arrived[unit], 1u) == (uint32_t)active - 1u;
-    __syncthreads();
-    if (!is_last) return;
-    if (threadIdx.x == 0) a.arrived[unit] = 0;
-
-    // lane 16 g + c of wavefront w: head c of parts 4 (w + W k) + g
-    float tops[kPer], sums[kPer];
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int s = min(4 * (wave + W * k) + g, active - 1);
-      tops[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(memory, s * part_bytes + col * 4, 0, kAcrossDies));
-      sums[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(memory, s * part_bytes + (kHeads + col) * 4, 0, kAcrossDies));
-    }
-    // an output of four elements per thread; where there are fewer than threads, several share one
-    const int outputs = heads_here * D / 4, sharers = max(1, kThreads / outputs);
-    const int e0 = (int)threadIdx.x % (outputs * sharers) % outputs, sharer = (int)threadIdx.x / outputs;
-    u32x4 next[kJoin];
-    auto fetch = [&](int e, int first) {
-#pragma unroll
-      for (int k = 0; k < kJoin; ++k)
-        next[k] = __builtin_amdgcn_raw_buffer_load_b128(memory, min(first + k * sharers, active - 1) * part_bytes + (2 * kHeads + e * 4) * 4, 0, kAcrossDies);
-    };
-    fetch(e0, sharer);
-    float m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) m = fmaxf(m, tops[k]);
-    m = across_groups_max(m);
-    if (g == 0) joined_m[wave][col] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) m = fmaxf(m, joined_m[w][col]);
-    const float from = m > -INFINITY ? m : 0.0f;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      tops[k] = 4 * (wave + W * k) + g < active ? __builtin_amdgcn_exp2f(tops[k] - from) : 0.0f;
-      l += sums[k] * tops[k];
-    }
-    l = across_groups_sum(l);
-    if (g == 0) joined_l[wave][col] = l;
-    __syncthreads();
-    l = 0.0f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) l += joined_l[w][col];
-    const float inverse = 1.0f / l;
-    float* weights = joined_o;   // [kMostSplits][kHeads]
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) weights[(4 * (wave + W * k) + g) * kHeads + col] = tops[k] * inverse;
-    if (a.lse && wave == 0 && g == 0 && col < heads_here) a.lse[(int64_t)i * a.heads + head0 + col] = (m + __log2f(l)) * kLn2;
-    __syncthreads();
-    f32x4* shared_out = (f32x4*)(joined_o + kMostSplits * kHeads);   // [kThreads]
-    if (sharers == 1 && sharer > 0) return;   // threads left over
-    for (int e = e0; e < outputs; e += kThreads) {
-      const int h = e * 4 / D;
-      f32x4 x = {0, 0, 0, 0};
-      if (sharer < sharers) {
-        for (int s = sharer;;) {
-#pragma unroll
-          for (int k = 0; k < kJoin; ++k) {
-            const int at = s + k * sharers;
-            const float w = at < active ? weights[at * kHeads + h] : 0.0f;
-            x += at < active ? __builtin_bit_cast(f32x4, next[k]) * w : f32x4{0, 0, 0, 0};
-          }
-          s += kJoin * sharers;
-          if (s >= active) break;
-          fetch(e, s);
-        }
-      }
-      if (sharers > 1) {   // (then this loop has one turn)
-        shared_out[threadIdx.x] = x;
-        __syncthreads();
-        if (sharer > 0) return;
-        for (int k = 1; k < sharers; ++k) x += shared_out[threadIdx.x + k * outputs];
-      } else if (e + kThreads < outputs) {
-        fetch(e + kThreads, sharer);
-      }
-      typename T::elem* out = (typename T::elem*)(a.out + i * a.out_entry + (head0 + h) * a.out_head) + e * 4 % D;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) out[k] = (typename T::elem)x[k];
-    }
-  }
+  finish_row<T, NT, W>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
 }
 
 template <class T, int NT, int W>
@@ -1103,10 +852,25 @@ Layout layout(const pgxcache_opts& o) {
 
 Cache cache_of(pgxcache_t h) {
   Cache c;
-  c.kv = (char*)h->kv; c.table = h->table; c.lengths = h->lengths; c.refs = h->refs; c.free_bits = h->free_bits; c.taken = h->taken; c.grown = h->grown;
+  c.kv = (char*)h->kv; c.scales = h->scales; c.table = h->table; c.lengths = h->lengths; c.refs = h->refs; c.free_bits = h->free_bits; c.taken = h->taken; c.grown = h->grown;
   c.slots = h->o.slots; c.pages = h->o.pages; c.width = h->o.width; c.page_shift = __builtin_ctz((unsigned)h->o.page_size);
   c.layers = h->o.layers; c.kv_heads = h->o.kv_heads; c.head_dim = h->o.head_dim;
   return c;
+}
+// rows of `row` elements at these strides do not overlap: in the order of their strides, each dimension steps over what the smaller ones cover
+bool apart(const int64_t (&sizes)[3], const int64_t (&strides)[3], int64_t row) {
+  int64_t covered = row;
+  bool used[3] = {false, false, false};
+  for (int k = 0; k < 3; ++k) {
+    int least = -1;
+    for (int d = 0; d < 3; ++d)
+      if (!used[d] && (least < 0 || llabs(strides[d]) < llabs(strides[least]))) least = d;
+    used[least] = true;
+    if (sizes[least] == 1) continue;
+    if (llabs(strides[least]) < covered) return false;
+    covered += llabs(strides[least]) * (sizes[least] - 1);
+  }
+  return true;
 }
 bool list_ok(pgxcache_t h, int32_t n) { return h && n >= 0 && n <= h->o.slots; }
 int scan(pgxcache_t h, int first) {
@@ -1124,8 +888,8 @@ size_t pgxcache_work_bytes(const pgxcache_opts* opts) { return opts_ok(opts) ? l
 
 int pgxcache_rescan(pgxcache_t h) { return h ? scan(h, 0) : PGXCACHE_EINVAL; }
 
-int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
-                  void* work_dev, size_t work_bytes) {
+static int init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, float* scales_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
+                void* work_dev, size_t work_bytes) {
   if (!out || !opts_ok(opts) || !kv_dev || !table_dev || !lengths_dev || !refs_dev || !work_dev) return PGXCACHE_EINVAL;
   if (((uintptr_t)kv_dev & 15u) != 0 || ((uintptr_t)work_dev & 255u) != 0) return PGXCACHE_EINVAL;
   if ((((uintptr_t)table_dev | (uintptr_t)lengths_dev | (uintptr_t)refs_dev) & 3u) != 0) return PGXCACHE_EINVAL;
@@ -1135,7 +899,7 @@ int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int3
   if (!h) return PGXCACHE_ENOMEM;
   char* w = (char*)work_dev;
   h->o = *opts;
-  h->kv = kv_dev; h->table = table_dev; h->lengths = lengths_dev; h->refs = refs_dev;
+  h->kv = kv_dev; h->scales = scales_dev; h->table = table_dev; h->lengths = lengths_dev; h->refs = refs_dev;
   h->free_bits = (uint64_t*)(w + l.free_bits); h->taken = (uint64_t*)(w + l.taken); h->grown = (int32_t*)(w + l.grown); h->plan = (int32_t*)(w + l.plan); h->forks = (ForkEntry*)(w + l.forks);
   h->moved_to = (int32_t*)(w + l.moved_to); h->moves = (int2*)(w + l.moves); h->counts = (int32_t*)(w + l.counts);
   h->arrived = (uint32_t*)(w + l.arrived); h->partial = (float*)(w + l.partial);
@@ -1143,6 +907,16 @@ int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int3
   if (rc != PGXCACHE_OK) { delete h; return rc; }
   *out = h;
   return PGXCACHE_OK;
+}
+
+int pgxcache_init(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
+                  void* work_dev, size_t work_bytes) {
+  return init(out, opts, kv_dev, nullptr, table_dev, lengths_dev, refs_dev, work_dev, work_bytes);
+}
+int pgxcache_init_e4m3(pgxcache_t* out, const pgxcache_opts* opts, void* kv_dev, float* scales_dev, int32_t* table_dev, int32_t* lengths_dev, int32_t* refs_dev,
+                       void* work_dev, size_t work_bytes) {
+  if (!scales_dev || ((uintptr_t)scales_dev & 3u) != 0) return PGXCACHE_EINVAL;
+  return init(out, opts, kv_dev, scales_dev, table_dev, lengths_dev, refs_dev, work_dev, work_bytes);
 }
 
 int pgxcache_destroy(pgxcache_t h) {
@@ -1176,10 +950,15 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
   if (n == 0 || tokens == 0) return PGXCACHE_OK;
   if (!k_dev || !v_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 1u) != 0) return PGXCACHE_EINVAL;
   const int64_t runs = ((int64_t)tokens + kTokensPerThread - 1) / kTokensPerThread;
-  const int64_t blocks = ((int64_t)n * runs * 2 * h->o.kv_heads * (h->o.head_dim / 8) + 255) / 256;
+  const Cache c = cache_of(h);
+  const int64_t blocks = c.scales ? write8_blocks(c, n, tokens) : ((int64_t)n * runs * 2 * h->o.kv_heads * (h->o.head_dim / 8) + 255) / 256;
   if (blocks > 0x7FFFFFFF) return PGXCACHE_EINVAL;
   const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};
-  hipLaunchKernelGGL(write_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), layer, n, slots_dev, tokens, k, v);
+  if (c.scales) {
+    HIPCHK(write8(c, h->o.type == PGXCACHE_F16, layer, n, slots_dev, tokens, 0, k, v, (hipStream_t)h->o.stream));
+    return PGXCACHE_OK;
+  }
+  hipLaunchKernelGGL(write_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)h->o.stream, c, layer, n, slots_dev, tokens, k, v);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
@@ -1201,7 +980,30 @@ int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots
   a.scale = scale * 1.44269504088896340736f;
   if ((int64_t)n * h->o.kv_heads * a.head_tiles > 0x7FFFFFFF) return PGXCACHE_EINVAL;
   const Cache c = cache_of(h);
+  if (c.scales) {
+    if (a.k && a.head_tiles > 1) {   // several blocks read the new token's block: it is written before, since rounding a block again is not the same twice
+      const Tokens k = {a.k, a.k_entry, 0, a.k_head}, v = {a.v, a.v_entry, 0, a.v_head};
+      HIPCHK(write8(c, h->o.type == PGXCACHE_F16, layer, n, slots_dev, 1, 1, k, v, (hipStream_t)h->o.stream));
+      a.k = a.v = nullptr;
+    }
+    HIPCHK(attend8(c, h->o.type == PGXCACHE_F16, a, (hipStream_t)h->o.stream));
+    return PGXCACHE_OK;
+  }
   HIPCHK(h->o.type == PGXCACHE_F16 ? launch_attend_for<F16>(c, a, (hipStream_t)h->o.stream) : launch_attend_for<BF16>(c, a, (hipStream_t)h->o.stream));
+  return PGXCACHE_OK;
+}
+
+int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, const int32_t* first_dev, int32_t first, int32_t tokens, void* k_dev,
+                  int64_t k_entry_stride, int64_t k_token_stride, int64_t k_head_stride, void* v_dev, int64_t v_entry_stride, int64_t v_token_stride, int64_t v_head_stride) {
+  if (!list_ok(h, n) || layer < 0 || layer >= h->o.layers || tokens < 0 || (!first_dev && first < 0)) return PGXCACHE_EINVAL;
+  if (n == 0 || tokens == 0) return PGXCACHE_OK;
+  if (!k_dev || !v_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 1u) != 0) return PGXCACHE_EINVAL;
+  const int64_t sizes[3] = {n, tokens, h->o.kv_heads}, ks[3] = {k_entry_stride, k_token_stride, k_head_stride}, vs[3] = {v_entry_stride, v_token_stride, v_head_stride};
+  if (!apart(sizes, ks, h->o.head_dim) || !apart(sizes, vs, h->o.head_dim)) return PGXCACHE_EINVAL;
+  const Cache c = cache_of(h);
+  if (read_blocks(c, n, tokens) > 0x7FFFFFFF) return PGXCACHE_EINVAL;
+  const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};
+  HIPCHK(read_back(c, h->o.type == PGXCACHE_F16, layer, n, slots_dev, first_dev, first, tokens, k, v, (hipStream_t)h->o.stream));
   return PGXCACHE_OK;
 }
 
@@ -1211,7 +1013,7 @@ int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const i
   if (!src_slots_dev || !dst_slots_dev) return PGXCACHE_EINVAL;
   hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->forks, status_dev);
   HIPCHK(hipGetLastError());
-  const size_t page = (size_t)h->o.layers * 2 * h->o.kv_heads * h->o.page_size * h->o.head_dim * 2;
+  const size_t page = (size_t)cache_of(h).page_bytes();
   const int per = page <= 16384 ? 64 : page <= 32768 ? 128 : 256, entries = 256 / per, words = (h->o.pages + 63) / 64;
   hipLaunchKernelGGL(fork_kernel, dim3((unsigned)((n + entries - 1) / entries + (words + 255) / 256)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, h->forks, per);
   HIPCHK(hipGetLastError());

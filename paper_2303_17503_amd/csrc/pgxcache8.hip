@@ -1,0 +1,503 @@
+// pgxcache8.hip -- keys and values held in 8 bits (include/pgxcache.h): rounding them as they are written, attention over them, reading them back, gfx950.
+//
+// An element is an e4m3 number times the scale of its block: 16 tokens of a slot (beginning with a multiple of 16) in one layer and head, keys or
+// values.  A head's block is one run of 16 head_dim bytes, half the rows of a matrix tile of attention, so that a wavefront knows its scale as one number.
+#include "cache_common.hpp"
+
+namespace pgxcache_parts {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kBlock = 1 << kBlockShift;   // tokens of a block
+
+__device__ __forceinline__ int64_t scale_index(const Cache& c, int64_t page, int layer, int which) {   // which: keys of all heads, then values
+  return page * c.page_scales() + ((int64_t)layer * 2 * c.kv_heads + which) * c.page_blocks();
+}
+
+// The scale for a largest magnitude m: the smallest power of two with m <= 448 of it (1.75 2^8), no smaller than 2^-100.
+__device__ __forceinline__ float scale_for(float m) {
+  const int e = (int)((__float_as_uint(m) + 0x1FFFFFu) >> 23) - 8;   // one up where the fraction is above 1.75
+  return __uint_as_float((uint32_t)max(e, 27) << 23);
+}
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 0x1.fffffep127f; }
+
+template <class T>
+__device__ __forceinline__ void unpack(const u32x4& w, float* x) {
+  const typename T::x8 h = __builtin_bit_cast(typename T::x8, w);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = (float)h[j];
+}
+// eight e4m3 codes, to nearest, ties to even; what is not finite becomes NaN
+__device__ __forceinline__ u32x2 encode(const float* x, float inverse) {
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = finite(x[j]) ? x[j] * inverse : __builtin_nanf("");
+  u32x2 w;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * j], y[4 * j + 1], 0, false);
+    w[j] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * j + 2], y[4 * j + 3], v, true);
+  }
+  return w;
+}
+__device__ __forceinline__ void decode(const u32x2& w, float* x) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
+    x[4 * j] = a[0]; x[4 * j + 1] = a[1]; x[4 * j + 2] = b[0]; x[4 * j + 3] = b[1];
+  }
+}
+__device__ __forceinline__ float largest(const float* x, float m) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = fmaxf(m, finite(x[j]) ? fabsf(x[j]) : 0.0f);
+  return m;
+}
+template <int ROT>
+__device__ __forceinline__ float rotated(float x) {   // within each 16 lanes
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + ROT, 0xF, 0xF, false));
+}
+// over the 32 lanes of a half of the wavefront
+__device__ __forceinline__ float half_max(float x) {
+  x = fmaxf(x, rotated<8>(x));
+  x = fmaxf(x, rotated<4>(x));
+  x = fmaxf(x, rotated<2>(x));
+  x = fmaxf(x, rotated<1>(x));
+  return fmaxf(x, __shfl_xor(x, 16));
+}
+
+// A block's earlier tokens, `count` of them, are rounded once more for a larger scale; 8 elements of one each per lane.
+__device__ __forceinline__ void round_again(char* block, int units, int lane, int lanes, float ratio) {
+  for (int u = lane; u < units; u += lanes) {
+    float x[8];
+    decode(*(const u32x2*)(block + u * 8), x);
+    *(u32x2*)(block + u * 8) = encode(x, ratio);
+  }
+}
+
+// ---- writing: a wavefront for each block of tokens, head and keys or values --------------------------------------------------------------
+template <class T, int NT>
+__global__ void __launch_bounds__(256) write8_kernel(Cache c, int layer, int n, const int32_t* slots, int tokens, int blocks, int last_only, Tokens k, Tokens v) {
+  constexpr int D = NT * 32, kUnits = D / 8;   // units of 8 elements of a token
+  const int lane = (int)threadIdx.x & 63, heads = 2 * c.kv_heads;
+  const int64_t piece = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int64_t entry_block = piece / heads;
+  const int which = (int)(piece - entry_block * heads), i = (int)(entry_block / blocks), b = (int)(entry_block - (int64_t)i * blocks);
+  if (i >= n) return;
+  const int slot = slots ? slots[i] : i;
+  if ((uint32_t)slot >= (uint32_t)c.slots) return;
+  const int grown = c.grown[slot], length = c.length(slot), first = length - (last_only ? 1 : grown), end = last_only ? length : first + min(grown, tokens);
+  const int block = (first >> kBlockShift) + b, t0 = block << kBlockShift;
+  if (grown <= 0 || first < 0 || t0 >= end) return;
+  const int page = c.row(slot)[t0 >> c.page_shift];
+  if (!c.is_page(page)) return;
+  const bool value = which >= c.kv_heads;
+  const Tokens& from = value ? v : k;
+  const char* p = from.p + (int64_t)i * from.entry + (value ? which - c.kv_heads : which) * from.head;
+  char* to = c.kv + page * c.page_bytes(1) + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes(1) + (int64_t)(t0 & ((1 << c.page_shift) - 1)) * D;
+  float* scale = c.scales + scale_index(c, page, layer, which) + (block & (c.page_blocks() - 1));
+  const bool had = first > t0;
+  const float was = had ? *scale : 0.0f;
+  float x[NT][8], m = 0.0f;
+#pragma unroll
+  for (int r = 0; r < NT; ++r) {
+    const int u = lane + 64 * r, t = t0 + u / kUnits;
+    const bool there = t >= first && t < end;
+    u32x4 w = {0, 0, 0, 0};
+    if (there) w = *(const u32x4_2*)(p + (int64_t)(t - first) * from.token + u % kUnits * 16);
+    unpack<T>(w, x[r]);
+    m = largest(x[r], m);
+  }
+  m = half_max(m);
+  m = fmaxf(m, __shfl_xor(m, 32));
+  const float own = scale_for(m), now = had && was >= own ? was : own, inverse = 1.0f / now;
+#pragma unroll
+  for (int r = 0; r < NT; ++r) {
+    const int u = lane + 64 * r, t = t0 + u / kUnits;
+    if (t >= first && t < end) *(u32x2*)(to + u * 8) = encode(x[r], inverse);
+  }
+  if (had && now != was) round_again(to, (first - t0) * kUnits, lane, 64, was / now);
+  if (lane == 0 && now != was) *scale = now;
+}
+
+// ---- reading back: a thread per 8 elements of a head's key or value and four tokens; both ways of holding them ----------------------------
+constexpr int kTokensPerThread = 4;
+template <class T, bool EIGHT>
+__global__ void __launch_bounds__(256) read_kernel(Cache c, int layer, int n, const int32_t* slots, const int32_t* firsts, int first_of_all, int tokens, Tokens k, Tokens v) {
+  const uint32_t units = (uint32_t)c.head_dim / 8, per_entry = 2u * (uint32_t)c.kv_heads * units;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t runs = (uint32_t)(tokens + kTokensPerThread - 1) / kTokensPerThread;
+  const int64_t token_run = x / per_entry;
+  const uint32_t u = (uint32_t)(x - token_run * per_entry);
+  if (token_run >= (int64_t)n * runs) return;
+  const int i = (int)(token_run / runs), j0 = (int)(token_run - (int64_t)i * runs) * kTokensPerThread;
+  const int slot = slots ? slots[i] : i;
+  const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
+  const int length = is_slot ? c.length(slot) : 0;
+  const int64_t first = firsts ? firsts[i] : first_of_all;
+  const uint32_t which = u / units, at = u % units * 8;   // which: keys of all heads, then values
+  const bool value = which >= (uint32_t)c.kv_heads;
+  const uint32_t head = value ? which - (uint32_t)c.kv_heads : which;
+  const Tokens& to = value ? v : k;
+  char* p = (char*)to.p + i * to.entry + head * to.head + at * 2;
+  const int32_t* row = c.row(is_slot ? slot : 0);
+  const char* from = c.kv + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes(EIGHT ? 1 : 2) + at * (EIGHT ? 1 : 2);
+  int page[kTokensPerThread];
+#pragma unroll
+  for (int j = 0; j < kTokensPerThread; ++j) {
+    const int64_t t = first + j0 + j;
+    page[j] = t >= 0 && t < length ? row[t >> c.page_shift] : -1;
+  }
+  u32x4 data[kTokensPerThread];
+  float scale[kTokensPerThread];
+#pragma unroll
+  for (int j = 0; j < kTokensPerThread; ++j) {
+    const int t = (int)(first + j0 + j);
+    data[j] = u32x4{0, 0, 0, 0};
+    scale[j] = 0.0f;
+    if (!c.is_page(page[j])) continue;
+    const char* source = from + page[j] * c.page_bytes(EIGHT ? 1 : 2) + (int64_t)(t & ((1 << c.page_shift) - 1)) * c.head_dim * (EIGHT ? 1 : 2);
+    if (EIGHT) {
+      const u32x2 w = *(const u32x2*)source;
+      data[j][0] = w[0];
+      data[j][1] = w[1];
+      scale[j] = c.scales[scale_index(c, page[j], layer, (int)which) + (t >> kBlockShift & (c.page_blocks() - 1))];
+    } else {
+      data[j] = *(const u32x4*)source;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kTokensPerThread; ++j) {
+    if (j0 + j >= tokens) break;
+    if (EIGHT) {
+      float y[8];
+      decode(u32x2{data[j][0], data[j][1]}, y);
+      typename T::x8 h;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = (typename T::elem)(y[e] * scale[j]);
+      data[j] = __builtin_bit_cast(u32x4, h);
+    }
+    *(u32x4_2*)(p + (int64_t)(j0 + j) * to.token) = data[j];
+  }
+}
+
+// ---- attention of one token per entry ----------------------------------------------------------------------------------------------------
+// The products of attention over 16 bits (pgxcache.hip) on codes that are turned into 16-bit numbers, exactly, on their way into the matrix instructions:
+// keys into the type of the queries, values into bfloat16, whose range holds probabilities times any scale.  Scores are multiplied by their block's scale,
+// probabilities by that of the values.  A tile is 32 tokens, two blocks.  The contraction of the first product may run over the elements in any order that both
+// operands share: a lane takes 16 neighbouring elements of its key at once, for two matrix instructions.
+template <int NT>
+struct Tile8 {
+  uint32_t k[2][2 * NT], v[8][(NT + 1) / 2];
+};
+template <class T>
+struct Decoded;
+template <>
+struct Decoded<BF16> {
+  static __device__ __forceinline__ uint32_t low(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)); }
+  static __device__ __forceinline__ uint32_t high(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)); }
+};
+template <>
+struct Decoded<F16> {
+  static __device__ __forceinline__ uint32_t low(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)); }
+  static __device__ __forceinline__ uint32_t high(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)); }
+};
+
+// where the 8 elements begin that group g of the m-th instruction of the first product takes
+template <int NT>
+__device__ __forceinline__ constexpr int key_element(int m, int g) { return (NT & 1) && m == NT - 1 ? m * 32 + g * 8 : m / 2 * 64 + g * 16 + (m & 1) * 8; }
+
+template <class T, int NT, int W, bool STREAM>
+__global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c, AttendArgs a) {
+  typedef typename T::x8 x8;
+  typedef typename BF16::x8 v8;
+  constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const uint32_t place = blockIdx.x, per_part = (uint32_t)(c.kv_heads * a.head_tiles);
+  const uint32_t part = place / per_part, in_part = place - part * per_part;
+  const int i = (int)(part / (uint32_t)a.splits), split = (int)(part - (uint32_t)i * (uint32_t)a.splits);
+  const int kv_head = (int)(in_part / (uint32_t)a.head_tiles), head_tile = (int)(in_part - (uint32_t)(kv_head * a.head_tiles));
+  const uint32_t unit = (uint32_t)i * per_part + in_part;
+  const int slot = a.slots ? a.slots[i] : i;
+  const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
+  const int first_head = head_tile * kHeads, heads_here = min(kHeads, a.group - first_head), head0 = kv_head * a.group + first_head;
+
+  // what depends on the entry only is asked for first, beside the slot's length
+  u32x4 query[NT], fresh = {0, 0, 0, 0};
+#pragma unroll
+  for (int m = 0; m < NT; ++m) query[m] = *(const u32x4_2*)(a.q + i * a.q_entry + (head0 + min(col, heads_here - 1)) * a.q_head + key_element<NT>(m, g) * 2);
+  const bool writes = (lane & 31) < D / 8;   // the new token: its key in the lower lanes, its value in the upper ones
+  if (a.k && writes) fresh = *(const u32x4_2*)((lane < 32 ? a.k + i * a.k_entry + kv_head * a.k_head : a.v + i * a.v_entry + kv_head * a.v_head) + (lane & 31) * 16);
+  const int32_t* row = c.row(is_slot ? slot : 0);
+  // page of half-tile lane & 1 of the wavefront's tile number (a multiple of 32) + lane / 2; the first ones are asked for before the length is known
+  int ids = 0;
+  if (a.splits == 1) ids = row[min((((wave + (lane >> 1) * W) * 2 + (lane & 1)) << 4) >> c.page_shift, c.width - 1)];
+  const int length = is_slot ? c.length(slot) : 0, grown = a.k && is_slot ? c.grown[slot] : 0;
+
+  if (length == 0) {   // nothing to attend to
+    if (split == 0 && wave == 0 && col < heads_here) {
+      char* out = a.out + i * a.out_entry + (head0 + col) * a.out_head + g * kOut * 2;
+#pragma unroll
+      for (int u = 0; u < NT; ++u) *(u32x4_2*)(out + u * 16) = u32x4{0, 0, 0, 0};
+      if (a.lse && g == 0) a.lse[(int64_t)i * a.heads + head0 + col] = -INFINITY;
+    }
+    return;
+  }
+  const int tiles = (int)(((int64_t)length + 31) >> 5);
+  const int chunk = ((tiles + a.splits - 1) / a.splits + W - 1) / W * W, active = (tiles + chunk - 1) / chunk;
+  if (split >= active) return;
+  const int begin = split * chunk, end = min(tiles, begin + chunk);
+
+  const int64_t page_bytes = c.page_bytes(1), head_bytes = c.head_bytes(1), page_scales = c.page_scales();
+  const char* keys = c.kv + ((int64_t)a.layer * 2 * c.kv_heads + kv_head) * head_bytes;
+  const char* values = keys + c.kv_heads * head_bytes;
+  float* key_scales = c.scales + ((int64_t)a.layer * 2 * c.kv_heads + kv_head) * c.page_blocks();
+  float* value_scales = key_scales + c.kv_heads * c.page_blocks();
+  const int in_page = (1 << c.page_shift) - 1, in_blocks = c.page_blocks() - 1;
+
+  const bool alone = W > 1 && tiles <= 1;   // nothing to share: the first wavefront goes on by itself
+  if (alone && wave > 0) return;
+
+  // The new token goes into the cache first, by the wavefront that reads the last tile (nobody else reads its block, and a wavefront's own memory
+  // operations are in order).
+  if (grown > 0 && end == tiles && wave == (tiles - 1 - begin) % W) {
+    const int at = length - 1, page = row[at >> c.page_shift], before = at & (kBlock - 1);
+    if (c.is_page(page)) {
+      float* scale = (lane < 32 ? key_scales : value_scales) + page * page_scales + (at >> kBlockShift & in_blocks);
+      char* block = (char*)(lane < 32 ? keys : values) + page * page_bytes + (int64_t)(at & in_page & ~(kBlock - 1)) * D;
+      const float was = before > 0 ? *scale : 0.0f;
+      float x[8];
+      unpack<T>(fresh, x);
+      const float own = scale_for(half_max(largest(x, 0.0f))), now = before > 0 && was >= own ? was : own;
+      if (writes) *(u32x2*)(block + before * D + (lane & 31) * 8) = encode(x, 1.0f / now);
+      if (now != was) {
+        round_again(block, before * (D / 8), lane & 31, 32, was / now);
+        if ((lane & 31) == 0) *scale = now;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+
+  x8 q[NT];
+#pragma unroll
+  for (int m = 0; m < NT; ++m) q[m] = __builtin_bit_cast(x8, col < heads_here ? query[m] : u32x4{0, 0, 0, 0});
+
+  float top = -INFINITY, sum = 0.0f;   // of the lane's head: the exponent that all four groups use, and this group's sum
+  f32x4 acc[2 * NT];
+#pragma unroll
+  for (int m = 0; m < 2 * NT; ++m) acc[m] = f32x4{0, 0, 0, 0};
+
+  if (!c.is_page(ids)) ids = 0;   // (behind the sequence: what is read there does not count)
+  const int last_half = (length - 1) >> 4;
+  // scales of the half-tiles whose pages are in ids, and of those that are computed: pages are changed with the load of a tile, one tile ahead
+  float next_key_scale = 0.0f, next_value_scale = 0.0f, key_scale = 0.0f, value_scale = 0.0f;
+  auto load = [&](Tile8<NT>& t, int number) {   // the wavefront's tile of that number
+    const int tile = begin + wave + number * W;
+    if ((number & 31) == 0) {
+      const int half = (tile + (lane >> 1) * W) * 2 + (lane & 1);
+      if (number > 0 || a.splits > 1) {
+        const int p = row[(min(half, last_half) << 4) >> c.page_shift];
+        ids = c.is_page(p) ? p : 0;
+      }
+      const int64_t at = ids * page_scales + (half & in_blocks);
+      next_key_scale = key_scales[at] * a.scale;
+      next_value_scale = half <= last_half ? value_scales[at] : 0.0f;   // (a block behind the last token may have any scale)
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t page = (int64_t)__builtin_amdgcn_readlane(ids, (number & 31) * 2 + h) * page_bytes + (int64_t)((tile * 32 + h * 16) & in_page) * D;
+      const char* k = keys + page + col * D;
+#pragma unroll
+      for (int m = 0; m < NT / 2; ++m) {
+        const u32x4 w = read_once<STREAM>((const u32x4*)(k + m * 64 + g * 16));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t.k[h][m * 4 + e] = w[e];
+      }
+      if (NT & 1) {
+        const u32x2 w = read_once<STREAM>((const u32x2*)(k + (NT - 1) * 32 + g * 8));
+        t.k[h][2 * NT - 2] = w[0];
+        t.k[h][2 * NT - 1] = w[1];
+      }
+      const char* v = values + page + (g * 4 * D + col * NT * 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t* to = t.v[h * 4 + j];
+        if constexpr (NT == 8) {
+          const u32x4 w = read_once<STREAM>((const u32x4*)(v + j * D));
+          to[0] = w[0]; to[1] = w[1]; to[2] = w[2]; to[3] = w[3];
+        } else if constexpr (NT == 4) {
+          const u32x2 w = read_once<STREAM>((const u32x2*)(v + j * D));
+          to[0] = w[0]; to[1] = w[1];
+        } else if constexpr (NT == 3) {   // (6 bytes from an even address)
+          const uint16_t* w = (const uint16_t*)(v + j * D);
+          to[0] = read_once<STREAM>(w) | (uint32_t)read_once<STREAM>(w + 1) << 16;
+          to[1] = read_once<STREAM>(w + 2);
+        } else if constexpr (NT == 2) {
+          to[0] = read_once<STREAM>((const uint32_t*)(v + j * D));
+        } else {
+          to[0] = read_once<STREAM>((const uint16_t*)(v + j * D));
+        }
+      }
+    }
+  };
+  auto compute = [&](Tile8<NT>& t, int number, auto last) {
+    if ((number & 31) == 0) {
+      key_scale = next_key_scale;
+      value_scale = next_value_scale;
+    }
+    f32x4 s[2];
+    float value_scales_here[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = (number & 31) * 2 + h;
+      s[h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int m = 0; m < NT; ++m) {
+        const uint32_t w0 = t.k[h][2 * m], w1 = t.k[h][2 * m + 1];
+        s[h] = T::mfma(__builtin_bit_cast(x8, u32x4{Decoded<T>::low(w0), Decoded<T>::high(w0), Decoded<T>::low(w1), Decoded<T>::high(w1)}), q[m], s[h]);
+      }
+      s[h] *= __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(key_scale), at));
+      value_scales_here[h] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(value_scale), at));
+    }
+    if (last.value) {   // tokens behind the sequence's last: no score, and their values may hold anything
+      const int first = (begin + wave + number * W) * 32 + g * 4;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool there = first + h * 16 + r < length;
+          s[h][r] = there ? s[h][r] : -INFINITY;
+#pragma unroll
+          for (int w = 0; w < (NT + 1) / 2; ++w) t.v[h * 4 + r][w] = there ? t.v[h * 4 + r][w] : 0;
+        }
+    }
+    const float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    if (__any(most > top + BF16::kMost)) {
+      const float now = across_groups_max(fmaxf(most, top));
+      const float factor = now > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 1.0f;
+      top = now;
+      sum *= factor;
+#pragma unroll
+      for (int m = 0; m < 2 * NT; ++m) acc[m] *= factor;
+    }
+    const float from = top > -INFINITY ? top : 0.0f;
+    v8 high, low;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float p = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - from);
+      sum += p;
+      p *= value_scales_here[j >> 2];
+      high[j] = (__bf16)p;
+      low[j] = (__bf16)(p - (float)high[j]);
+    }
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {   // elements 2 m and 2 m + 1 of the lane's 2 NT
+      u32x4 x, y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w = __builtin_amdgcn_perm(t.v[2 * j + 1][m / 2], t.v[2 * j][m / 2], m & 1 ? 0x07030602u : 0x05010400u);
+        x[j] = Decoded<BF16>::low(w);
+        y[j] = Decoded<BF16>::high(w);
+      }
+      acc[2 * m] = BF16::mfma(__builtin_bit_cast(v8, x), high, acc[2 * m]);
+      acc[2 * m] = BF16::mfma(__builtin_bit_cast(v8, x), low, acc[2 * m]);
+      acc[2 * m + 1] = BF16::mfma(__builtin_bit_cast(v8, y), high, acc[2 * m + 1]);
+      acc[2 * m + 1] = BF16::mfma(__builtin_bit_cast(v8, y), low, acc[2 * m + 1]);
+    }
+  };
+  const int mine = (end - begin - wave + W - 1) / W;   // this wavefront's tiles
+  if (mine > 0) {   // the next tile is under way while one is computed
+    constexpr std::false_type inner{};
+    constexpr std::true_type outer{};
+    Tile8<NT> t0, t1;
+    load(t0, 0);
+    int number = 0;
+    for (; number + 2 < mine; number += 2) {
+      load(t1, number + 1);
+      compute(t0, number, inner);
+      load(t0, number + 2);
+      compute(t1, number + 1, inner);
+    }
+    if (number + 1 < mine) {
+      load(t1, number + 1);
+      compute(t0, number, inner);
+      compute(t1, number + 1, outer);
+    } else {
+      compute(t0, number, outer);
+    }
+  }
+  finish_row<T, NT, W>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
+}
+
+template <class T, int NT, int W>
+hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t rows, hipStream_t stream) {
+  const bool streamed = (int64_t)c.pages * c.page_bytes(1) > (int64_t)256 << 20;   // (as over 16 bits)
+  const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = a.splits > 1 ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
+  const dim3 grid((unsigned)(rows * a.splits)), block(64 * W);
+  if (streamed) hipLaunchKernelGGL((attend8_kernel<T, NT, W, true>), grid, block, join > weights ? join : weights, stream, c, a);
+  else hipLaunchKernelGGL((attend8_kernel<T, NT, W, false>), grid, block, join > weights ? join : weights, stream, c, a);
+  return hipGetLastError();
+}
+template <class T, int NT>
+hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles, most_tiles = (((int64_t)c.width << c.page_shift) + 31) / 32;
+  a.splits = 1;
+  if (most_tiles <= 8 && rows >= 1024) return launch_attend_by<T, NT, 1>(c, a, rows, stream);
+  if (most_tiles > 32) {
+    const int64_t spread = kSplitBlocks / rows, useful = (most_tiles + 7) / 8;
+    const int64_t splits = spread < useful ? spread : useful;
+    a.splits = (int32_t)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
+  }
+  return launch_attend_by<T, NT, 4>(c, a, rows, stream);
+}
+
+template <class T>
+hipError_t attend8_for(const Cache& c, const AttendArgs& a, hipStream_t stream) {
+  switch (c.head_dim) {
+    case 32: return launch_attend<T, 1>(c, a, stream);
+    case 64: return launch_attend<T, 2>(c, a, stream);
+    case 96: return launch_attend<T, 3>(c, a, stream);
+    case 128: return launch_attend<T, 4>(c, a, stream);
+    default: return launch_attend<T, 8>(c, a, stream);
+  }
+}
+template <class T>
+hipError_t write8_for(const Cache& c, int layer, int n, const int32_t* slots, int tokens, int blocks, int last_only, const Tokens& k, const Tokens& v, unsigned grid, hipStream_t stream) {
+  switch (c.head_dim) {
+    case 32: hipLaunchKernelGGL((write8_kernel<T, 1>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
+    case 64: hipLaunchKernelGGL((write8_kernel<T, 2>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
+    case 96: hipLaunchKernelGGL((write8_kernel<T, 3>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
+    case 128: hipLaunchKernelGGL((write8_kernel<T, 4>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
+    default: hipLaunchKernelGGL((write8_kernel<T, 8>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t write8_blocks(const Cache& c, int n, int tokens) {   // of the launch
+  const int64_t blocks = ((int64_t)tokens + kBlock - 2) / kBlock + 1;   // that `tokens` tokens can lie in
+  return ((int64_t)n * blocks * 2 * c.kv_heads + 3) / 4;
+}
+hipError_t write8(const Cache& c, bool f16, int layer, int n, const int32_t* slots, int tokens, int last_only, const Tokens& k, const Tokens& v, hipStream_t stream) {
+  const int blocks = (int)(((int64_t)tokens + kBlock - 2) / kBlock + 1);
+  const unsigned grid = (unsigned)write8_blocks(c, n, tokens);
+  return f16 ? write8_for<F16>(c, layer, n, slots, tokens, blocks, last_only, k, v, grid, stream) : write8_for<BF16>(c, layer, n, slots, tokens, blocks, last_only, k, v, grid, stream);
+}
+
+hipError_t attend8(const Cache& c, bool f16, const AttendArgs& a, hipStream_t stream) { return f16 ? attend8_for<F16>(c, a, stream) : attend8_for<BF16>(c, a, stream); }
+
+int64_t read_blocks(const Cache& c, int n, int tokens) {
+  const int64_t runs = ((int64_t)tokens + kTokensPerThread - 1) / kTokensPerThread;
+  return ((int64_t)n * runs * 2 * c.kv_heads * (c.head_dim / 8) + 255) / 256;
+}
+hipError_t read_back(const Cache& c, bool f16, int layer, int n, const int32_t* slots, const int32_t* firsts, int first, int tokens, const Tokens& k, const Tokens& v, hipStream_t stream) {
+  const dim3 grid((unsigned)read_blocks(c, n, tokens)), block(256);
+  if (!c.scales) hipLaunchKernelGGL((read_kernel<BF16, false>), grid, block, 0, stream, c, layer, n, slots, firsts, first, tokens, k, v);   // (copies either type)
+  else if (f16) hipLaunchKernelGGL((read_kernel<F16, true>), grid, block, 0, stream, c, layer, n, slots, firsts, first, tokens, k, v);
+  else hipLaunchKernelGGL((read_kernel<BF16, true>), grid, block, 0, stream, c, layer, n, slots, firsts, first, tokens, k, v);
+  return hipGetLastError();
+}
+
+}  // namespace pgxcache_parts

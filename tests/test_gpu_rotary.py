@@ -1,0 +1,239 @@
+"""pg.rotate against the plain 64-bit form.
+
+Tolerance.  u = 2^-24.  The part of a circle is exact to |p| 2^-53 times the frequency and then rounded to 32 bits: the angle is off by at most
+pi u + 2 pi 2^31 2^-53 < 4 u, cosine and sine (of sincospi, 2 units in the last place) by at most 4 u + 2 u and with the magnitude's product 7 u of the magnitude; a result x c - y s, of a
+rounded product and a fused one, by 9 u (|x| + |y|) times the magnitude, and the rounding to the type, half a step: eps / 2 of the result, and half of the smallest subnormal."""
+import random
+
+import pytest
+import torch
+
+import paper_2303_17503_amd as pg
+from rotary_ref import turned
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TINY = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133}
+
+
+def check(got, x, positions, f, interleaved, magnitude, inverse):
+    want = turned(x, positions, f, interleaved, magnitude, inverse)
+    R, size = 2 * f.numel(), x.detach().cpu().double().abs()
+    both = size.clone()
+    pairs = size[..., :R].unflatten(-1, (R // 2, 2) if interleaved else (2, R // 2)).sum(-1 if interleaved else -2)
+    both[..., :R] = pairs.repeat_interleave(2, -1) if interleaved else torch.cat((pairs, pairs), -1)
+    assert got.dtype is x.dtype and got.shape == x.shape
+    assert torch.equal(got[..., R:].cpu(), x[..., R:].cpu())
+    err = (got.cpu().double() - want).abs()[..., :R]
+    assert (err <= (9 * U * abs(magnitude) * both + torch.finfo(x.dtype).eps / 2 * 1.001 * want.abs() + TINY[x.dtype])[..., :R]).all(), float(err.max())
+
+
+def whole(g, lo, hi, *shape):
+    return torch.randint(lo, hi, shape, generator=g, device="cuda", dtype=torch.int32)
+
+
+SHAPES = [(1, None, 1, 1, 2, 2), (3, None, 2, 1, 3, 2), (5, None, 8, 2, 64, 64), (7, None, 3, 3, 96, 96), (2, 9, 4, 1, 128, 32), (3, 4, 5, 2, 80, 20), (2, 3, 2, 1, 33, 18),
+          (300, None, 8, 2, 64, 64), (2, 700, 6, 2, 32, 32), (1, 3, 1, 1, 1024, 1024), (1, 2, 2, 1, 1023, 514), (2, 3, 3, 2, 256, 16), (4, 500, 1, 1, 17, 14), (2, 1, 40, 8, 256, 250)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("n,T,heads,kv_heads,D,R", SHAPES)
+def test_shapes_and_types(n, T, heads, kv_heads, D, R, interleaved, dtype):
+    g = torch.Generator("cuda").manual_seed(D)
+    lead = (n,) if T is None else (n, T)
+    q, k = (torch.randn(*lead, h, D, generator=g, device="cuda").to(dtype) for h in (heads, kv_heads))
+    f = pg.rotary_frequencies(R)
+    positions = whole(g, 0, 5000, *lead)
+    for inverse, magnitude in ((False, 1.0), (True, 1.25)):
+        a, b = pg.rotate((q, k), positions, f, interleaved=interleaved, magnitude=magnitude, inverse=inverse)
+        check(a, q, positions, f, interleaved, magnitude, inverse)
+        check(b, k, positions, f, interleaved, magnitude, inverse)
+        alone = pg.rotate(q, positions, f, interleaved=interleaved, magnitude=magnitude, inverse=inverse)
+        assert isinstance(alone, torch.Tensor) and torch.equal(alone, a)
+        into = [q.clone(), k.clone()]
+        got = pg.rotate(into, positions, f, interleaved=interleaved, magnitude=magnitude, inverse=inverse, out=into)
+        assert got[0] is into[0] and torch.equal(into[0], a) and torch.equal(into[1], b)       # in place
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_far_positions(interleaved, dtype):
+    """up to the ends of 32 bits, both signs, with frequencies of every scaling; the angles are those of 64 bits"""
+    g = torch.Generator("cuda").manual_seed(1)
+    positions = torch.tensor([0, 1, -1, 2, 131071, 2 ** 24 + 1, 2 ** 30 + 12345, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    x = torch.randn(9, 3, 64, generator=g, device="cuda").to(dtype)
+    for how in (dict(), dict(scaling="linear", factor=16.0), dict(scaling="base", factor=8.0), dict(scaling="parts", factor=32.0, original=8192), dict(base=500000.0)):
+        f = pg.rotary_frequencies(48, **how)
+        check(pg.rotate(x, positions, f, interleaved=interleaved), x, positions, f, interleaved, 1.0, False)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_strides(interleaved, dtype):
+    """queries and keys as views into one product, heads before tokens, rows at odd addresses; positions that all rows share, and strided ones"""
+    g = torch.Generator("cuda").manual_seed(2)
+    n, T, H, KV, D, R = 3, 11, 4, 2, 40, 36
+    product = torch.randn(n, T, (H + 2 * KV) * D + 1, generator=g, device="cuda").to(dtype)
+    q, k = product[..., 1:1 + H * D].unflatten(-1, (H, D)), product[..., 1 + H * D:1 + (H + KV) * D].unflatten(-1, (KV, D))
+    f = pg.rotary_frequencies(R)
+    for positions in (torch.arange(T, device="cuda", dtype=torch.int32).expand(n, T), whole(g, 0, 9999, T, n).t(), whole(g, 0, 9, n, 1).expand(n, T)):
+        a, b = pg.rotate((q, k), positions, f, interleaved=interleaved)
+        check(a, q, positions, f, interleaved, 1.0, False)
+        check(b, k, positions, f, interleaved, 1.0, False)
+    wide = torch.full((n, H, T, D + 3), 7.0, dtype=dtype, device="cuda")
+    into = wide[..., 2:-1].transpose(1, 2)
+    assert torch.equal(pg.rotate(q, positions, f, interleaved=interleaved, out=into), a) and (wide[..., :2] == 7).all() and (wide[..., -1] == 7).all()
+    before = product.clone()
+    pg.rotate((q, k), positions, f, interleaved=interleaved, out=(q, k))             # in place, in the product
+    assert torch.equal(q, a) and torch.equal(k, b) and torch.equal(product[..., 1 + (H + KV) * D:], before[..., 1 + (H + KV) * D:]) and torch.equal(product[..., 0], before[..., 0])
+    repeated = q[:1, :, :1].expand(2, T, 3, D)                                        # an input's rows may overlap
+    check(pg.rotate(repeated, positions[:2], f, interleaved=interleaved), repeated, positions[:2], f, interleaved, 1.0, False)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_the_gradient_against_differences(interleaved):
+    """of sum w . rotate(x): linear in x, so a difference over a step of 1 is the derivative itself, off by what two results are"""
+    g = torch.Generator("cuda").manual_seed(3)
+    D, R = 12, 10
+    x, w = torch.randn(4, 2, D, generator=g, device="cuda"), torch.randn(4, 2, D, generator=g, device="cuda")
+    positions, f = whole(g, 0, 100000, 4), pg.rotary_frequencies(R)
+    run = lambda t: pg.rotate(t, positions, f, interleaved=interleaved, magnitude=1.5).double()  # noqa: E731
+    grad = pg.rotate(w, positions, f, interleaved=interleaved, magnitude=1.5, inverse=True).double()
+    check(grad.float(), w, positions, f, interleaved, 1.5, True)
+    for e in range(D):
+        step = x.clone()
+        step[..., e] += 1
+        slope = ((run(step) - run(x)) * w.double()).sum(-1) / (step.double() - x.double())[..., e]
+        most = (x.abs().max() + 1) * 2 * 1.5
+        assert ((slope - grad[..., e]).abs() <= 2 * (9 + 1) * U * 2 * most * w.abs().double().sum(-1) + 10 * U * 4 * 1.5 * w.abs().max()).all()
+
+
+def test_values_that_are_not_finite_stay_in_their_pair():
+    x = torch.randn(2, 2, 16, device="cuda")
+    x[0, 0, 3], x[1, 1, 12], x[0, 1, 15] = float("nan"), float("inf"), float("nan")
+    f = pg.rotary_frequencies(12)
+    got = pg.rotate(x, torch.tensor([5, 6], dtype=torch.int32, device="cuda"), f)
+    bad = ~torch.isfinite(got)
+    assert bad[0, 0].nonzero()[:, 0].tolist() == [3, 9] and bad[1, 1].nonzero()[:, 0].tolist() == [12] and bad[0, 1].nonzero()[:, 0].tolist() == [15] and not bad[1, 0].any()
+
+
+def test_nothing_to_do():
+    f = pg.rotary_frequencies(8)
+    assert pg.rotate(torch.zeros(0, 2, 8, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"), f).shape == (0, 2, 8)
+    a, b = pg.rotate((torch.ones(3, 0, 8, device="cuda"), torch.ones(3, 1, 8, device="cuda")), torch.zeros(3, dtype=torch.int32, device="cuda"), f)
+    assert a.shape == (3, 0, 8) and (b == 1).all()
+    a, b = pg.rotate((torch.ones(3, 1, 8, device="cuda"), torch.ones(3, 0, 8, device="cuda")), torch.zeros(3, dtype=torch.int32, device="cuda"), f)
+    assert b.shape == (3, 0, 8) and (a == 1).all()
+
+
+def test_offsets_beyond_32_bits():
+    """tokens more than 2^31 elements apart"""
+    n, D = 3, 64
+    memory = torch.empty(2 ** 32 + 64, dtype=torch.bfloat16, device="cuda")
+    x = memory.as_strided((n, 1, D), (2 ** 31, D, 1))
+    x.copy_(torch.randn(n, 1, D, device="cuda"))
+    positions, f = torch.tensor([3, 500, 70000], dtype=torch.int32, device="cuda"), pg.rotary_frequencies(D)
+    want = pg.rotate(x.contiguous(), positions, f)
+    assert torch.equal(pg.rotate(x, positions, f), want)
+    pg.rotate(x, positions, f, out=x)
+    assert torch.equal(x, want)
+
+
+def test_on_another_stream_and_captured():
+    g = torch.Generator("cuda").manual_seed(4)
+    q, k = torch.randn(50, 8, 64, generator=g, device="cuda").bfloat16(), torch.randn(50, 2, 64, generator=g, device="cuda").bfloat16()
+    positions, f = whole(g, 0, 999, 50), pg.rotary_frequencies(64)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    into = [torch.empty_like(q), torch.empty_like(k)]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        pg.rotate((q, k), positions, f, out=into)
+    for _ in range(4):
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = pg.rotate((q, k), positions, f)
+        assert torch.equal(a, into[0]) and torch.equal(b, into[1])
+        positions.add_(17)
+        q.mul_(-1)
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.default_stream())
+        c = pg.rotate(q, positions, f)
+        at = c.data_ptr()
+        assert [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]] == [side.cuda_stream]
+    side.synchronize()
+    check(c, q, positions, f, False, 1.0, False)
+
+
+def call(**k):
+    a = dict(x=torch.zeros(4, 2, 16, device="cuda"), positions=torch.zeros(4, dtype=torch.int32, device="cuda"), frequencies=torch.ones(8, dtype=torch.float64, device="cuda"))
+    a.update({n: v() if callable(v) else v for n, v in k.items()})
+    return pg.rotate(**a)
+
+
+def zeros(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype, device="cuda")
+
+
+REFUSED = [
+    ("x on the host", dict(x=lambda: zeros(4, 2, 16).cpu())), ("x of double", dict(x=lambda: zeros(4, 2, 16).double())), ("x of two dimensions", dict(x=lambda: zeros(4, 16))),
+    ("x of five", dict(x=lambda: zeros(4, 1, 1, 2, 16))), ("x strided inside", dict(x=lambda: zeros(4, 2, 32)[..., ::2])), ("three tensors", dict(x=lambda: [zeros(4, 2, 16)] * 3)), ("none", dict(x=lambda: [])),
+    ("a pair of two types", dict(x=lambda: (zeros(4, 2, 16), zeros(4, 2, 16).half()))), ("a pair of two sizes", dict(x=lambda: (zeros(4, 2, 16), zeros(4, 2, 18)))),
+    ("a pair of two lengths", dict(x=lambda: (zeros(4, 2, 16), zeros(3, 2, 16)))), ("no tensor", dict(x=3)),
+    ("positions of long", dict(positions=lambda: zeros(4, dtype=torch.int64))), ("positions of other size", dict(positions=lambda: zeros(3, dtype=torch.int32))),
+    ("positions of two dimensions", dict(positions=lambda: zeros(4, 1, dtype=torch.int32))), ("positions on the host", dict(positions=lambda: zeros(4, dtype=torch.int32).cpu())), ("positions a list", dict(positions=[0] * 4)),
+    ("frequencies of float", dict(frequencies=lambda: zeros(8))), ("more frequencies than pairs", dict(frequencies=lambda: zeros(9, dtype=torch.float64))), ("no frequencies", dict(frequencies=lambda: zeros(0, dtype=torch.float64))),
+    ("frequencies on the host", dict(frequencies=lambda: zeros(8, dtype=torch.float64).cpu())), ("frequencies strided", dict(frequencies=lambda: zeros(16, dtype=torch.float64)[::2])),
+    ("magnitude", dict(magnitude=float("nan"))), ("out of another type", dict(out=lambda: zeros(4, 2, 16).half())), ("out of another size", dict(out=lambda: zeros(4, 3, 16))),
+    ("out strided inside", dict(out=lambda: zeros(4, 2, 32)[..., ::2])), ("out for a pair", dict(out=lambda: (zeros(4, 2, 16), zeros(4, 2, 16)))), ("out that overlaps", dict(out=lambda: zeros(4, 1, 16).expand(4, 2, 16))),
+    ("out with shared entries", dict(out=lambda: zeros(1, 2, 16).expand(4, 2, 16))), ("out with rows that overlap", dict(out=lambda: zeros(900).as_strided((4, 2, 16), (40, 15, 1)))),
+    ("a head of 1025", dict(x=lambda: zeros(4, 2, 1026))),
+]
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("what", [n for n, _ in REFUSED])
+def test_refusals(what, native, monkeypatch):
+    call()
+    if not native:
+        monkeypatch.setattr(pg.rotary_binding, "_fast", None)
+    with pytest.raises(pg.PgxGoError):
+        call(**dict(REFUSED)[what])
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_the_same_tensor_twice(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(pg.rotary_binding, "_fast", None)
+    x = torch.randn(4, 2, 16, device="cuda")
+    a, b = call(x=(x, x))
+    assert torch.equal(a, b)
+    for out in ((x, x), (a, a)):
+        with pytest.raises(pg.PgxGoError):
+            call(x=(x, x), out=out)
+
+
+def test_native_and_python_checks_make_the_same_calls(monkeypatch):
+    def history():
+        g, r = torch.Generator("cuda").manual_seed(1), random.Random(1)
+        out = []
+        for _ in range(40):
+            lead = (r.randint(0, 4),) if r.random() < 0.5 else (r.randint(1, 4), r.randint(1, 5))
+            D = r.randint(2, 70)
+            R = 2 * r.randint(1, D // 2)
+            x = [torch.randn(*lead, r.randint(1, 3), D, generator=g, device="cuda").to(r.choice([torch.float32, torch.bfloat16]) if i == 0 else x0) for i, x0 in ((0, None),)]
+            if r.random() < 0.5: x.append(torch.randn(*lead, 2, D, generator=g, device="cuda").to(x[0].dtype))
+            into = [torch.zeros_like(t) for t in x] if r.random() < 0.3 else None
+            got = pg.rotate(x, whole(g, 0, 99, *lead), pg.rotary_frequencies(R), interleaved=r.random() < 0.5, magnitude=r.choice([1, 0.5]), inverse=r.random() < 0.5, out=into)
+            out += list(got)
+        return out
+
+    assert pg.rotary_binding.lib() is not None and pg.rotary_binding._fast is not None
+    native = history()
+    monkeypatch.setattr(pg.rotary_binding, "_fast", None)
+    for a, b in zip(native, history()):
+        assert torch.equal(a, b)
