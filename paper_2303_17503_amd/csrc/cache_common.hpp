@@ -87,6 +87,7 @@ struct AttendArgs {
   uint32_t* arrived;
   int32_t n, layer, heads, group, head_tiles, splits;
   float scale;   // times log2 e
+  int32_t by_die;   // 8 bits: whether heads of one part are launched eight blocks apart
 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -144,7 +145,7 @@ struct Spot {
 
 // The end of a row: the parts of W wavefronts, and of `active` blocks, are joined and written.  Lane 16 g + c has elements (4 g + r) D/16 + m of head c in
 // acc[m][r], relative to the exponent `top` (of powers of two), and the sum of its group's probabilities.
-template <class T, int NT, int W>
+template <class T, int NT, int W, bool SPLIT>
 __device__ __forceinline__ void finish_row(const AttendArgs& a, const Spot& at_spot, float top, float sum, f32x4 (&acc)[2 * NT]) {
   typedef typename T::x8 x8;
   constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
@@ -186,7 +187,7 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, const Spot& at_s
     }
   }
 
-  if (active == 1) {
+  if (!SPLIT || active == 1) {
     if (wave > 0) return;
     if (col >= heads_here) return;
     const float inverse = 1.0f / sum;
@@ -204,7 +205,7 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, const Spot& at_s
 
   // The row is split over `active` blocks: each leaves its part in memory, and the one that comes last joins them, in an order of its own.
   // All its loads are of 16 bytes and under way together: with 4-byte ones, one output each, joining 256 parts of 8 heads of 128 took 40 us.
-  if constexpr (W >= 4) {
+  if constexpr (SPLIT) {
     constexpr int kPart = kHeads * (D + 2), kThreads = 64 * W, kPer = kMostSplits / (4 * W), kJoin = NT < 8 ? 16 : 8;
     const uint32_t part_bytes = kPart * 4;
     float* parts = a.partial + (int64_t)unit * a.splits * kPart;

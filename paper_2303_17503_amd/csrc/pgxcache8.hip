@@ -11,6 +11,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 1 << kBlockShift;   // tokens of a block
+int blocks_of(int tokens) { return (int)(((int64_t)tokens + kBlock - 2) / kBlock + 1); }   // that so many tokens can lie in
 
 __device__ __forceinline__ int64_t scale_index(const Cache& c, int64_t page, int layer, int which) {   // which: keys of all heads, then values
   return page * c.page_scales() + ((int64_t)layer * 2 * c.kv_heads + which) * c.page_blocks();
@@ -54,71 +55,132 @@ __device__ __forceinline__ float largest(const float* x, float m) {
   for (int j = 0; j < 8; ++j) m = fmaxf(m, finite(x[j]) ? fabsf(x[j]) : 0.0f);
   return m;
 }
-template <int ROT>
-__device__ __forceinline__ float rotated(float x) {   // within each 16 lanes
-  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + ROT, 0xF, 0xF, false));
+template <int DPP>
+__device__ __forceinline__ float moved(float x) {   // lanes exchanged within each 16
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), DPP, 0xF, 0xF, false));
 }
-// over the 32 lanes of a half of the wavefront
+// over the 32 lanes of a half of the wavefront: rotations within 16, then the other 16
 __device__ __forceinline__ float half_max(float x) {
-  x = fmaxf(x, rotated<8>(x));
-  x = fmaxf(x, rotated<4>(x));
-  x = fmaxf(x, rotated<2>(x));
-  x = fmaxf(x, rotated<1>(x));
+  x = fmaxf(x, moved<0x128>(x));
+  x = fmaxf(x, moved<0x124>(x));
+  x = fmaxf(x, moved<0x122>(x));
+  x = fmaxf(x, moved<0x121>(x));
   return fmaxf(x, __shfl_xor(x, 16));
 }
 
-// A block's earlier tokens, `count` of them, are rounded once more for a larger scale; 8 elements of one each per lane.
+// A block's earlier tokens are rounded once more for a larger scale: `units` runs of 8 elements, `lanes` lanes, N at most for each, four under way together.
+template <int N>
 __device__ __forceinline__ void round_again(char* block, int units, int lane, int lanes, float ratio) {
-  for (int u = lane; u < units; u += lanes) {
-    float x[8];
-    decode(*(const u32x2*)(block + u * 8), x);
-    *(u32x2*)(block + u * 8) = encode(x, ratio);
+  constexpr int kAhead = N < 4 ? N : 4;
+  for (int u0 = lane; u0 < units; u0 += lanes * kAhead) {
+    u32x2 w[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) w[k] = *(const u32x2*)(block + min(u0 + k * lanes, units - 1) * 8);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      float x[8];
+      decode(w[k], x);
+      if (u0 + k * lanes < units) *(u32x2*)(block + (u0 + k * lanes) * 8) = encode(x, ratio);
+    }
   }
 }
 
-// ---- writing: a wavefront for each block of tokens, head and keys or values --------------------------------------------------------------
+// ---- writing -----------------------------------------------------------------------------------------------------------------------------
+// Several tokens: a wavefront for the keys and values of each block of tokens and head, with the loads of both under way beside the look at the table.
 template <class T, int NT>
-__global__ void __launch_bounds__(256) write8_kernel(Cache c, int layer, int n, const int32_t* slots, int tokens, int blocks, int last_only, Tokens k, Tokens v) {
+__global__ void __launch_bounds__(256) write8_kernel(Cache c, int layer, int n, const int32_t* slots, int tokens, int blocks, Tokens k, Tokens v) {
   constexpr int D = NT * 32, kUnits = D / 8;   // units of 8 elements of a token
-  const int lane = (int)threadIdx.x & 63, heads = 2 * c.kv_heads;
+  const int lane = (int)threadIdx.x & 63;
   const int64_t piece = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int64_t entry_block = piece / heads;
-  const int which = (int)(piece - entry_block * heads), i = (int)(entry_block / blocks), b = (int)(entry_block - (int64_t)i * blocks);
+  const int64_t entry_block = piece / c.kv_heads;
+  const int head = (int)(piece - entry_block * c.kv_heads), i = (int)(entry_block / blocks), b = (int)(entry_block - (int64_t)i * blocks);
   if (i >= n) return;
   const int slot = slots ? slots[i] : i;
   if ((uint32_t)slot >= (uint32_t)c.slots) return;
-  const int grown = c.grown[slot], length = c.length(slot), first = length - (last_only ? 1 : grown), end = last_only ? length : first + min(grown, tokens);
+  const int grown = c.grown[slot], first = c.length(slot) - grown, end = first + min(grown, tokens);
   const int block = (first >> kBlockShift) + b, t0 = block << kBlockShift;
   if (grown <= 0 || first < 0 || t0 >= end) return;
+  u32x4 raw[2][NT];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const Tokens& from = w ? v : k;
+    const char* p = from.p + (int64_t)i * from.entry + head * from.head;
+#pragma unroll
+    for (int r = 0; r < NT; ++r) {
+      const int u = lane + 64 * r, t = t0 + u / kUnits;
+      raw[w][r] = u32x4{0, 0, 0, 0};
+      if (t >= first && t < end) raw[w][r] = *(const u32x4_2*)(p + (int64_t)(t - first) * from.token + u % kUnits * 16);
+    }
+  }
   const int page = c.row(slot)[t0 >> c.page_shift];
   if (!c.is_page(page)) return;
+  const bool had = first > t0;
+  float* scale[2];
+  float was[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    scale[w] = c.scales + scale_index(c, page, layer, head + w * c.kv_heads) + (block & (c.page_blocks() - 1));
+    was[w] = had ? *scale[w] : 0.0f;
+  }
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    float x[NT][8], m = 0.0f;
+#pragma unroll
+    for (int r = 0; r < NT; ++r) {
+      unpack<T>(raw[w][r], x[r]);
+      m = largest(x[r], m);
+    }
+    m = half_max(m);
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float own = scale_for(m), now = had && was[w] >= own ? was[w] : own, inverse = 1.0f / now;
+    char* to = c.kv + page * c.page_bytes(1) + ((int64_t)layer * 2 * c.kv_heads + head + w * c.kv_heads) * c.head_bytes(1) + (int64_t)(t0 & ((1 << c.page_shift) - 1)) * D;
+#pragma unroll
+    for (int r = 0; r < NT; ++r) {
+      const int u = lane + 64 * r, t = t0 + u / kUnits;
+      if (t >= first && t < end) *(u32x2*)(to + u * 8) = encode(x[r], inverse);
+    }
+    if (had && now != was[w]) round_again<NT>(to, (first - t0) * kUnits, lane, 64, was[w] / now);
+    if (lane == 0 && now != was[w]) *scale[w] = now;
+  }
+}
+
+// One token: as many lanes as it has runs of 8 elements, or the next power of two, for each entry, head and keys or values; its elements are on their way while its place is
+// looked up.
+template <class T, int NT>
+__global__ void __launch_bounds__(256) write8_one_kernel(Cache c, int layer, int n, const int32_t* slots, int last, Tokens k, Tokens v) {
+  constexpr int D = NT * 32, kUnits = D / 8, kGroup = kUnits <= 4 ? 4 : kUnits <= 8 ? 8 : kUnits <= 16 ? 16 : 32;
+  const int u = (int)threadIdx.x % kGroup, heads = 2 * c.kv_heads;
+  const int64_t piece = (int64_t)blockIdx.x * (256 / kGroup) + (int)threadIdx.x / kGroup;
+  const int entry = (int)(piece / heads), which = (int)(piece - (int64_t)entry * heads), i = min(entry, n - 1);
   const bool value = which >= c.kv_heads;
   const Tokens& from = value ? v : k;
-  const char* p = from.p + (int64_t)i * from.entry + (value ? which - c.kv_heads : which) * from.head;
-  char* to = c.kv + page * c.page_bytes(1) + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes(1) + (int64_t)(t0 & ((1 << c.page_shift) - 1)) * D;
-  float* scale = c.scales + scale_index(c, page, layer, which) + (block & (c.page_blocks() - 1));
-  const bool had = first > t0;
-  const float was = had ? *scale : 0.0f;
-  float x[NT][8], m = 0.0f;
-#pragma unroll
-  for (int r = 0; r < NT; ++r) {
-    const int u = lane + 64 * r, t = t0 + u / kUnits;
-    const bool there = t >= first && t < end;
-    u32x4 w = {0, 0, 0, 0};
-    if (there) w = *(const u32x4_2*)(p + (int64_t)(t - first) * from.token + u % kUnits * 16);
-    unpack<T>(w, x[r]);
-    m = largest(x[r], m);
+  u32x4 raw = {0, 0, 0, 0};
+  if (u < kUnits) raw = *(const u32x4_2*)(from.p + (int64_t)i * from.entry + (value ? which - c.kv_heads : which) * from.head + u * 16);
+  const int slot = slots ? slots[i] : i;
+  const bool is_slot = entry < n && (uint32_t)slot < (uint32_t)c.slots;
+  const int at_slot = is_slot ? slot : 0, length = c.length(at_slot), grown = c.grown[at_slot], t = length - (last ? 1 : grown);
+  const bool there = is_slot && grown > 0 && t >= 0;
+  const int page = c.row(at_slot)[there ? t >> c.page_shift : 0];
+  const bool writes = there && c.is_page(page);
+  float* scale = c.scales + scale_index(c, writes ? page : 0, layer, which) + (t >> kBlockShift & (c.page_blocks() - 1));
+  const int before = t & (kBlock - 1);
+  const float was = writes && before > 0 ? *scale : 0.0f;
+  float x[8];
+  unpack<T>(raw, x);
+  float m = largest(x, 0.0f);   // (over the group: neighbours first, then mirrored, when halves are alike)
+  m = fmaxf(m, moved<0xB1>(m));
+  m = fmaxf(m, moved<0x4E>(m));
+  if (kGroup >= 8) m = fmaxf(m, moved<0x141>(m));
+  if (kGroup >= 16) m = fmaxf(m, moved<0x140>(m));
+  if (kGroup >= 32) m = fmaxf(m, __shfl_xor(m, 16));
+  if (!writes) return;
+  const float own = scale_for(m), now = before > 0 && was >= own ? was : own;
+  char* to = c.kv + page * c.page_bytes(1) + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes(1) + (int64_t)(t & ((1 << c.page_shift) - 1) & ~(kBlock - 1)) * D;
+  if (u < kUnits) *(u32x2*)(to + before * D + u * 8) = encode(x, 1.0f / now);
+  if (before == 0 || now != was) {
+    if (before > 0) round_again<15>(to, before * kUnits, u, kGroup, was / now);
+    if (u == 0) *scale = now;
   }
-  m = half_max(m);
-  m = fmaxf(m, __shfl_xor(m, 32));
-  const float own = scale_for(m), now = had && was >= own ? was : own, inverse = 1.0f / now;
-#pragma unroll
-  for (int r = 0; r < NT; ++r) {
-    const int u = lane + 64 * r, t = t0 + u / kUnits;
-    if (t >= first && t < end) *(u32x2*)(to + u * 8) = encode(x[r], inverse);
-  }
-  if (had && now != was) round_again(to, (first - t0) * kUnits, lane, 64, was / now);
-  if (lane == 0 && now != was) *scale = now;
 }
 
 // ---- reading back: a thread per 8 elements of a head's key or value and four tokens; both ways of holding them ----------------------------
@@ -208,20 +270,34 @@ struct Decoded<F16> {
 template <int NT>
 __device__ __forceinline__ constexpr int key_element(int m, int g) { return (NT & 1) && m == NT - 1 ? m * 32 + g * 8 : m / 2 * 64 + g * 16 + (m & 1) * 8; }
 
-template <class T, int NT, int W, bool STREAM>
-__global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c, AttendArgs a) {
+// W wavefronts share a row: an entry, a key head and a tile of 16 query heads.  SPLIT: a row may be split over blocks.  STREAM: keys and values are read with the hint
+// that they are not read again soon.
+template <class T, int NT, int W, int BUF, bool SPLIT, bool STREAM>
+__global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : W == 16 ? 4 : 2) attend8_kernel(Cache c, AttendArgs a) {
   typedef typename T::x8 x8;
   typedef typename BF16::x8 v8;
   constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = (int)threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const uint32_t place = blockIdx.x, per_part = (uint32_t)(c.kv_heads * a.head_tiles);
-  const uint32_t part = place / per_part, in_part = place - part * per_part;
-  const int i = (int)(part / (uint32_t)a.splits), split = (int)(part - (uint32_t)i * (uint32_t)a.splits);
+  // What runs together reads neighbouring memory: heads are next to each other in the launch, then the parts of a sequence.  Blocks go to the eight dies in turn, so with
+  // by_die the heads of a part are eight blocks apart: the tiles of query heads of one key head find its keys and values in one die's L2 (201 slots of up to 4001 tokens, 20 heads of
+  // 256 on one key head: 217 MB read from memory and not twice that), and the key heads the lines that hold their scales.
+  const uint32_t per_part = (uint32_t)(c.kv_heads * a.head_tiles);
+  uint32_t part, in_part;
+  if (a.by_die) {
+    const uint32_t eight = blockIdx.x / (8u * per_part), inside = blockIdx.x - eight * 8u * per_part;
+    in_part = inside >> 3;
+    part = eight * 8 + (inside & 7);
+    if (part >= (uint32_t)(a.n * a.splits)) return;
+  } else {
+    part = blockIdx.x / per_part;
+    in_part = blockIdx.x - part * per_part;
+  }
+  const int i = SPLIT ? (int)(part / (uint32_t)a.splits) : (int)part, split = SPLIT ? (int)(part - (uint32_t)i * (uint32_t)a.splits) : 0;
   const int kv_head = (int)(in_part / (uint32_t)a.head_tiles), head_tile = (int)(in_part - (uint32_t)(kv_head * a.head_tiles));
-  const uint32_t unit = (uint32_t)i * per_part + in_part;
+  const uint32_t unit = ((uint32_t)i * (uint32_t)c.kv_heads + (uint32_t)kv_head) * (uint32_t)a.head_tiles + (uint32_t)head_tile;
   const int slot = a.slots ? a.slots[i] : i;
   const bool is_slot = (uint32_t)slot < (uint32_t)c.slots;
-  const int first_head = head_tile * kHeads, heads_here = min(kHeads, a.group - first_head), head0 = kv_head * a.group + first_head;
+  const int heads_here = min(kHeads, a.group - head_tile * kHeads), head0 = kv_head * a.group + head_tile * kHeads;
 
   // what depends on the entry only is asked for first, beside the slot's length
   u32x4 query[NT], fresh = {0, 0, 0, 0};
@@ -232,7 +308,7 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c
   const int32_t* row = c.row(is_slot ? slot : 0);
   // page of half-tile lane & 1 of the wavefront's tile number (a multiple of 32) + lane / 2; the first ones are asked for before the length is known
   int ids = 0;
-  if (a.splits == 1) ids = row[min((((wave + (lane >> 1) * W) * 2 + (lane & 1)) << 4) >> c.page_shift, c.width - 1)];
+  if (!SPLIT || a.splits == 1) ids = row[min((((wave + (lane >> 1) * W) * 2 + (lane & 1)) << 4) >> c.page_shift, c.width - 1)];
   const int length = is_slot ? c.length(slot) : 0, grown = a.k && is_slot ? c.grown[slot] : 0;
 
   if (length == 0) {   // nothing to attend to
@@ -245,8 +321,8 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c
     return;
   }
   const int tiles = (int)(((int64_t)length + 31) >> 5);
-  const int chunk = ((tiles + a.splits - 1) / a.splits + W - 1) / W * W, active = (tiles + chunk - 1) / chunk;
-  if (split >= active) return;
+  const int chunk = SPLIT ? ((tiles + a.splits - 1) / a.splits + W - 1) / W * W : tiles, active = SPLIT ? (tiles + chunk - 1) / chunk : 1;
+  if (SPLIT && split >= active) return;
   const int begin = split * chunk, end = min(tiles, begin + chunk);
 
   const int64_t page_bytes = c.page_bytes(1), head_bytes = c.head_bytes(1), page_scales = c.page_scales();
@@ -259,26 +335,6 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c
   const bool alone = W > 1 && tiles <= 1;   // nothing to share: the first wavefront goes on by itself
   if (alone && wave > 0) return;
 
-  // The new token goes into the cache first, by the wavefront that reads the last tile (nobody else reads its block, and a wavefront's own memory
-  // operations are in order).
-  if (grown > 0 && end == tiles && wave == (tiles - 1 - begin) % W) {
-    const int at = length - 1, page = row[at >> c.page_shift], before = at & (kBlock - 1);
-    if (c.is_page(page)) {
-      float* scale = (lane < 32 ? key_scales : value_scales) + page * page_scales + (at >> kBlockShift & in_blocks);
-      char* block = (char*)(lane < 32 ? keys : values) + page * page_bytes + (int64_t)(at & in_page & ~(kBlock - 1)) * D;
-      const float was = before > 0 ? *scale : 0.0f;
-      float x[8];
-      unpack<T>(fresh, x);
-      const float own = scale_for(half_max(largest(x, 0.0f))), now = before > 0 && was >= own ? was : own;
-      if (writes) *(u32x2*)(block + before * D + (lane & 31) * 8) = encode(x, 1.0f / now);
-      if (now != was) {
-        round_again(block, before * (D / 8), lane & 31, 32, was / now);
-        if ((lane & 31) == 0) *scale = now;
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
-
   x8 q[NT];
 #pragma unroll
   for (int m = 0; m < NT; ++m) q[m] = __builtin_bit_cast(x8, col < heads_here ? query[m] : u32x4{0, 0, 0, 0});
@@ -288,26 +344,59 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c
 #pragma unroll
   for (int m = 0; m < 2 * NT; ++m) acc[m] = f32x4{0, 0, 0, 0};
 
-  if (!c.is_page(ids)) ids = 0;   // (behind the sequence: what is read there does not count)
+  const int mine = (end - begin - wave + W - 1) / W;   // this wavefront's tiles
   const int last_half = (length - 1) >> 4;
-  // scales of the half-tiles whose pages are in ids, and of those that are computed: pages are changed with the load of a tile, one tile ahead
-  float next_key_scale = 0.0f, next_value_scale = 0.0f, key_scale = 0.0f, value_scale = 0.0f;
-  auto load = [&](Tile8<NT>& t, int number) {   // the wavefront's tile of that number
-    const int tile = begin + wave + number * W;
-    if ((number & 31) == 0) {
-      const int half = (tile + (lane >> 1) * W) * 2 + (lane & 1);
-      if (number > 0 || a.splits > 1) {
-        const int p = row[(min(half, last_half) << 4) >> c.page_shift];
-        ids = c.is_page(p) ? p : 0;
-      }
-      const int64_t at = ids * page_scales + (half & in_blocks);
-      next_key_scale = key_scales[at] * a.scale;
-      next_value_scale = half <= last_half ? value_scales[at] : 0.0f;   // (a block behind the last token may have any scale)
+  uint64_t pages_there = 0;   // which of the pages in ids are pages (behind the sequence, and where the table is wrong: what is read there is page 0's and does not count)
+  auto take_pages = [&](int p) {
+    pages_there = __ballot(c.is_page(p));
+    ids = c.is_page(p) ? p : 0;
+  };
+  take_pages(ids);
+  // Scales of the half-tiles whose pages are in ids.  They are asked for ahead of the tile's keys and values and taken over behind them: a register that a load may
+  // still be on its way to would have every tile wait for all loads.
+  float asked_key_scale = 0.0f, asked_value_scale = 0.0f, key_scale = 0.0f, value_scale = 0.0f;
+  auto lane_of = [](float x, int at) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), at)); };
+  auto look_up = [&](int number) {   // pages and scales of the wavefront's tiles number to number + 31
+    const int half = (begin + wave + (number + (lane >> 1)) * W) * 2 + (lane & 1);
+    if (number > 0 || (SPLIT && a.splits > 1)) take_pages(row[(min(half, last_half) << 4) >> c.page_shift]);
+    const int64_t at = ids * page_scales + (half & in_blocks);
+    asked_key_scale = key_scales[at];
+    asked_value_scale = value_scales[at];
+  };
+  auto take_over = [&](int number) {
+    const int half = (begin + wave + (number + (lane >> 1)) * W) * 2 + (lane & 1);
+    key_scale = asked_key_scale * a.scale;
+    value_scale = half <= last_half ? asked_value_scale : 0.0f;   // (a block behind the last token may have any scale)
+  };
+  // The new token goes into the cache ahead of the loads of the last tile, by the wavefront that reads that (nobody else reads its block, and a
+  // wavefront's own memory operations are in order), beside its first tile's on their way.
+  const bool renews = grown > 0 && mine > 0 && end == tiles && wave == (tiles - 1 - begin) % W;
+  auto renew = [&]() {
+    const int at = length - 1, before = at & (kBlock - 1), half = (mine - 1) * 2 + (at >> kBlockShift & 1);   // (of the first 32 tiles: a lane's)
+    const bool near = half < 64;
+    const int page = near ? (pages_there >> half & 1 ? __builtin_amdgcn_readlane(ids, half) : -1) : row[at >> c.page_shift];
+    if (!c.is_page(page)) return;
+    const int64_t scale_at = page * page_scales + (at >> kBlockShift & in_blocks);
+    char* block = (char*)(lane < 32 ? keys : values) + page * page_bytes + (int64_t)(at & in_page & ~(kBlock - 1)) * D;
+    const float was = near ? (lane < 32 ? lane_of(asked_key_scale, half) : lane_of(asked_value_scale, half)) : (lane < 32 ? key_scales : value_scales)[scale_at];
+    float x[8];
+    unpack<T>(fresh, x);
+    const float own = scale_for(half_max(largest(x, 0.0f))), now = before > 0 && was >= own ? was : own;
+    if (writes) *(u32x2*)(block + before * D + (lane & 31) * 8) = encode(x, 1.0f / now);
+    if (before == 0 || now != was) {
+      if (before > 0) round_again<2 * NT>(block, before * (D / 8), lane & 31, 32, was / now);
+      if ((lane & 31) == 0) (lane < 32 ? key_scales : value_scales)[scale_at] = now;
     }
+    const float key_now = lane_of(now, 0), value_now = lane_of(now, 32);
+    key_scale = lane == half ? key_now * a.scale : key_scale;
+    value_scale = lane == half ? value_now : value_scale;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  auto load_half = [&](int number, int h) { return (int64_t)__builtin_amdgcn_readlane(ids, (number & 31) * 2 + h) * page_bytes + (int64_t)(((begin + wave + number * W) * 32 + h * 16) & in_page) * D; };
+  auto load_keys = [&](Tile8<NT>& t, int number) {   // of the wavefront's tile of that number
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t page = (int64_t)__builtin_amdgcn_readlane(ids, (number & 31) * 2 + h) * page_bytes + (int64_t)((tile * 32 + h * 16) & in_page) * D;
-      const char* k = keys + page + col * D;
+      const char* k = keys + load_half(number, h) + col * D;
 #pragma unroll
       for (int m = 0; m < NT / 2; ++m) {
         const u32x4 w = read_once<STREAM>((const u32x4*)(k + m * 64 + g * 16));
@@ -319,7 +408,12 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c
         t.k[h][2 * NT - 2] = w[0];
         t.k[h][2 * NT - 1] = w[1];
       }
-      const char* v = values + page + (g * 4 * D + col * NT * 2);
+    }
+  };
+  auto load_values = [&](Tile8<NT>& t, int number) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char* v = values + load_half(number, h) + (g * 4 * D + col * NT * 2);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t* to = t.v[h * 4 + j];
@@ -341,24 +435,40 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c
       }
     }
   };
-  auto compute = [&](Tile8<NT>& t, int number, auto last) {
-    if ((number & 31) == 0) {
-      key_scale = next_key_scale;
-      value_scale = next_value_scale;
-    }
+  // BUF = 2: the next tile is under way while one is computed.  BUF = 1: its keys take the place of the present ones as soon as the scores are there, its values when
+  // the present ones are added up.
+  auto compute = [&](Tile8<NT>& t, Tile8<NT>& next, int number, auto last) {
     f32x4 s[2];
-    float value_scales_here[2];
+    float key_scales_here[2], value_scales_here[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int at = (number & 31) * 2 + h;
+      key_scales_here[h] = lane_of(key_scale, (number & 31) * 2 + h);
+      value_scales_here[h] = lane_of(value_scale, (number & 31) * 2 + h);
+    }
+    auto turn = [&]() {
+      if (((number + 1) & 31) == 0) {
+        look_up(number + 1);
+        take_over(number + 1);
+      }
+    };
+    if (BUF == 2 && !last.value) {
+      turn();
+      load_keys(next, number + 1);
+      load_values(next, number + 1);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
       s[h] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int m = 0; m < NT; ++m) {
         const uint32_t w0 = t.k[h][2 * m], w1 = t.k[h][2 * m + 1];
         s[h] = T::mfma(__builtin_bit_cast(x8, u32x4{Decoded<T>::low(w0), Decoded<T>::high(w0), Decoded<T>::low(w1), Decoded<T>::high(w1)}), q[m], s[h]);
       }
-      s[h] *= __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(key_scale), at));
-      value_scales_here[h] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(value_scale), at));
+      s[h] *= key_scales_here[h];
+    }
+    if (BUF == 1 && !last.value) {
+      turn();
+      load_keys(t, number + 1);
     }
     if (last.value) {   // tokens behind the sequence's last: no score, and their values may hold anything
       const int first = (begin + wave + number * W) * 32 + g * 4;
@@ -404,52 +514,72 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend8_kernel(Cache c
       acc[2 * m] = BF16::mfma(__builtin_bit_cast(v8, x), low, acc[2 * m]);
       acc[2 * m + 1] = BF16::mfma(__builtin_bit_cast(v8, y), high, acc[2 * m + 1]);
       acc[2 * m + 1] = BF16::mfma(__builtin_bit_cast(v8, y), low, acc[2 * m + 1]);
+      if (NT == 8) __builtin_amdgcn_sched_barrier(0);
     }
+    if (BUF == 1 && !last.value) load_values(t, number + 1);
   };
-  const int mine = (end - begin - wave + W - 1) / W;   // this wavefront's tiles
-  if (mine > 0) {   // the next tile is under way while one is computed
+  if (mine > 0) {
     constexpr std::false_type inner{};
     constexpr std::true_type outer{};
     Tile8<NT> t0, t1;
-    load(t0, 0);
-    int number = 0;
-    for (; number + 2 < mine; number += 2) {
-      load(t1, number + 1);
-      compute(t0, number, inner);
-      load(t0, number + 2);
-      compute(t1, number + 1, inner);
+    look_up(0);
+    if (!renews || mine > 1) {
+      load_keys(t0, 0);
+      load_values(t0, 0);
     }
-    if (number + 1 < mine) {
-      load(t1, number + 1);
-      compute(t0, number, inner);
-      compute(t1, number + 1, outer);
+    take_over(0);
+    if (renews) {
+      renew();
+      if (mine == 1) {
+        load_keys(t0, 0);
+        load_values(t0, 0);
+      }
+    }
+    int number = 0;
+    if constexpr (BUF == 1) {
+      for (; number + 1 < mine; ++number) compute(t0, t0, number, inner);
+      compute(t0, t0, number, outer);
     } else {
-      compute(t0, number, outer);
+      for (; number + 2 < mine; number += 2) {
+        compute(t0, t1, number, inner);
+        compute(t1, t0, number + 1, inner);
+      }
+      if (number + 1 < mine) {
+        compute(t0, t1, number, inner);
+        compute(t1, t0, number + 1, outer);
+      } else {
+        compute(t0, t1, number, outer);
+      }
     }
   }
-  finish_row<T, NT, W>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
+  finish_row<T, NT, W, SPLIT>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
 }
 
-template <class T, int NT, int W>
-hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t rows, hipStream_t stream) {
+template <class T, int NT, int W, int BUF, bool SPLIT>
+hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, hipStream_t stream) {
   const bool streamed = (int64_t)c.pages * c.page_bytes(1) > (int64_t)256 << 20;   // (as over 16 bits)
-  const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = a.splits > 1 ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
-  const dim3 grid((unsigned)(rows * a.splits)), block(64 * W);
-  if (streamed) hipLaunchKernelGGL((attend8_kernel<T, NT, W, true>), grid, block, join > weights ? join : weights, stream, c, a);
-  else hipLaunchKernelGGL((attend8_kernel<T, NT, W, false>), grid, block, join > weights ? join : weights, stream, c, a);
+  const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = SPLIT ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
+  const int64_t parts = (int64_t)a.n * a.splits, heads = (int64_t)c.kv_heads * a.head_tiles;
+  const dim3 grid((unsigned)(a.by_die ? (parts + 7) / 8 * 8 * heads : parts * heads)), block(64 * W);
+  if (streamed) hipLaunchKernelGGL((attend8_kernel<T, NT, W, BUF, SPLIT, true>), grid, block, join > weights ? join : weights, stream, c, a);
+  else hipLaunchKernelGGL((attend8_kernel<T, NT, W, BUF, SPLIT, false>), grid, block, join > weights ? join : weights, stream, c, a);
   return hipGetLastError();
 }
 template <class T, int NT>
 hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
+  // As over 16 bits (pgxcache.hip), by how long a slot can be: a wavefront for each of many short rows, four for longer ones, and few rows that can be longer than 32
+  // tiles are split over blocks, two for each compute unit at most.  @@
   const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles, most_tiles = (((int64_t)c.width << c.page_shift) + 31) / 32;
   a.splits = 1;
-  if (most_tiles <= 8 && rows >= 1024) return launch_attend_by<T, NT, 1>(c, a, rows, stream);
   if (most_tiles > 32) {
     const int64_t spread = kSplitBlocks / rows, useful = (most_tiles + 7) / 8;
     const int64_t splits = spread < useful ? spread : useful;
     a.splits = (int32_t)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
   }
-  return launch_attend_by<T, NT, 4>(c, a, rows, stream);
+  a.by_die = a.head_tiles > 1 || (int64_t)a.n * a.splits >= 64;
+  if (a.splits > 1) return launch_attend_by<T, NT, 4, NT < 8 ? 2 : 1, true>(c, a, stream);
+  if (most_tiles <= 8 && rows >= 1024) return launch_attend_by<T, NT, 1, 2, false>(c, a, stream);
+  return launch_attend_by<T, NT, 4, 2, false>(c, a, stream);
 }
 
 template <class T>
@@ -462,28 +592,33 @@ hipError_t attend8_for(const Cache& c, const AttendArgs& a, hipStream_t stream) 
     default: return launch_attend<T, 8>(c, a, stream);
   }
 }
-template <class T>
-hipError_t write8_for(const Cache& c, int layer, int n, const int32_t* slots, int tokens, int blocks, int last_only, const Tokens& k, const Tokens& v, unsigned grid, hipStream_t stream) {
-  switch (c.head_dim) {
-    case 32: hipLaunchKernelGGL((write8_kernel<T, 1>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
-    case 64: hipLaunchKernelGGL((write8_kernel<T, 2>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
-    case 96: hipLaunchKernelGGL((write8_kernel<T, 3>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
-    case 128: hipLaunchKernelGGL((write8_kernel<T, 4>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
-    default: hipLaunchKernelGGL((write8_kernel<T, 8>), dim3(grid), dim3(256), 0, stream, c, layer, n, slots, tokens, blocks, last_only, k, v); break;
-  }
+template <class T, int NT>
+hipError_t launch_write(const Cache& c, int layer, int n, const int32_t* slots, int tokens, int last_only, const Tokens& k, const Tokens& v, hipStream_t stream) {
+  const dim3 grid((unsigned)write8_blocks(c, n, tokens)), block(256);
+  if (tokens == 1) hipLaunchKernelGGL((write8_one_kernel<T, NT>), grid, block, 0, stream, c, layer, n, slots, last_only, k, v);
+  else hipLaunchKernelGGL((write8_kernel<T, NT>), grid, block, 0, stream, c, layer, n, slots, tokens, blocks_of(tokens), k, v);
   return hipGetLastError();
+}
+template <class T>
+hipError_t write8_for(const Cache& c, int layer, int n, const int32_t* slots, int tokens, int last_only, const Tokens& k, const Tokens& v, hipStream_t stream) {
+  switch (c.head_dim) {
+    case 32: return launch_write<T, 1>(c, layer, n, slots, tokens, last_only, k, v, stream);
+    case 64: return launch_write<T, 2>(c, layer, n, slots, tokens, last_only, k, v, stream);
+    case 96: return launch_write<T, 3>(c, layer, n, slots, tokens, last_only, k, v, stream);
+    case 128: return launch_write<T, 4>(c, layer, n, slots, tokens, last_only, k, v, stream);
+    default: return launch_write<T, 8>(c, layer, n, slots, tokens, last_only, k, v, stream);
+  }
 }
 
 }  // namespace
 
 int64_t write8_blocks(const Cache& c, int n, int tokens) {   // of the launch
-  const int64_t blocks = ((int64_t)tokens + kBlock - 2) / kBlock + 1;   // that `tokens` tokens can lie in
-  return ((int64_t)n * blocks * 2 * c.kv_heads + 3) / 4;
+  if (tokens > 1) return ((int64_t)n * blocks_of(tokens) * c.kv_heads + 3) / 4;
+  const int group = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
+  return ((int64_t)n * 2 * c.kv_heads * group + 255) / 256;
 }
 hipError_t write8(const Cache& c, bool f16, int layer, int n, const int32_t* slots, int tokens, int last_only, const Tokens& k, const Tokens& v, hipStream_t stream) {
-  const int blocks = (int)(((int64_t)tokens + kBlock - 2) / kBlock + 1);
-  const unsigned grid = (unsigned)write8_blocks(c, n, tokens);
-  return f16 ? write8_for<F16>(c, layer, n, slots, tokens, blocks, last_only, k, v, grid, stream) : write8_for<BF16>(c, layer, n, slots, tokens, blocks, last_only, k, v, grid, stream);
+  return f16 ? write8_for<F16>(c, layer, n, slots, tokens, last_only, k, v, stream) : write8_for<BF16>(c, layer, n, slots, tokens, last_only, k, v, stream);
 }
 
 hipError_t attend8(const Cache& c, bool f16, const AttendArgs& a, hipStream_t stream) { return f16 ? attend8_for<F16>(c, a, stream) : attend8_for<BF16>(c, a, stream); }
