@@ -115,7 +115,7 @@ class PagedCache:
             else: _check(L.pgxcache_init_e4m3(C.byref(h), C.byref(opts), _ptr(kv), _ptr(scales), *rest), "pgxcache_init_e4m3")
         self._h, self._destroy = h, L.pgxcache_destroy
         if _fast is not None:
-            self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "attend", "fork", "free")}
+            self._calls = {n: _address(getattr(L, "pgxcache_" + n)) for n in ("advance", "write", "read", "attend", "fork", "free")}
             self._shape = (self.slots, self.kv_heads, self.head_dim, TYPES[self.dtype], self.device.index, self._stream.stream_id)
         self._scale = self.head_dim ** -0.5
 
@@ -197,6 +197,10 @@ class PagedCache:
     def read(self, layer, tokens, slots=None, first=0, k=None, v=None):
         """(keys, values) of the slots' tokens first, first + 1, ... (a number, or int32 [n]), `tokens` of them, as they are held, in the calls' type:
         [n][tokens][kv_heads][head_dim] (new ones belong to the cache's stream).  Zeros where a slot has no such token; entries may repeat."""
+        if _fast is not None:
+            got = _fast.cache_read(self._calls["read"], self._h.value, self._shape, layer, tokens, slots, first, k, v)
+            if type(got) is tuple: return got
+            if got is not None: _check(got, "pgxcache_read")
         n, p = self._list(slots)
         tokens = _whole(tokens, "tokens")
         each = isinstance(first, torch.Tensor)

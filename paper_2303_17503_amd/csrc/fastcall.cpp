@@ -451,6 +451,45 @@ PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   });
 }
 
+// (address, handle, shape, layer, tokens, slots, first, k, v)
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  return guarded_outputs([&]() -> PyObject* {
+    CacheShape s{0, 0, 0, kFloat, c10::Device(c10::kCPU), 0};
+    int64_t n, first = 0, got;
+    void *slots, *firsts = nullptr, *at[2];
+    int64_t entry[2], token[2], head[2];
+    at::Tensor out[2];
+    if (n_args != 9 || !take_shape(a[2], &s) || !take_list(a[5], s, &n, &slots) || !PyLong_CheckExact(a[4])) return nullptr;
+    const int64_t tokens = PyLong_AsLongLong(a[4]);
+    const long layer = PyLong_AsLong(a[3]);
+    if (PyErr_Occurred() || layer < 0 || layer > INT32_MAX || tokens < 0 || tokens > INT32_MAX) return nullptr;
+    if (PyLong_CheckExact(a[6])) {
+      first = PyLong_AsLongLong(a[6]);
+      if (PyErr_Occurred() || first < 0 || first > INT32_MAX) return nullptr;
+    } else if (!take_entries(a[6], s, kInt, n, &firsts)) {
+      return nullptr;
+    }
+    const c10::StreamGuard guard(c10::Stream(c10::Stream::UNSAFE, s.device, s.stream));   // new outputs belong to the stream that writes them
+    for (int i = 0; i < 2; ++i) {
+      if (a[7 + i] == Py_None) {
+        out[i] = fresh({n, tokens, s.kv_heads, s.head_dim}, s.type, s.device);
+        at[i] = data_or_null(out[i]);
+        entry[i] = out[i].stride(0); token[i] = out[i].stride(1); head[i] = out[i].stride(2);
+      } else {
+        if (!tensor(a[7 + i]) || tensor(a[7 + i])->dim() != 4 || !take_tokens(a[7 + i], s, n, &got, &at[i], &entry[i], &token[i], &head[i]) || got != tokens) return nullptr;
+        out[i] = *tensor(a[7 + i]);
+      }
+    }
+    auto* fn = (decltype(&pgxcache_read))pointer(a[0]);
+    void* h = pointer(a[1]);
+    const int rc = without_gil([&] {
+      return fn((pgxcache_t)h, (int32_t)layer, (int32_t)n, (const int32_t*)slots, (const int32_t*)firsts, (int32_t)first, (int32_t)tokens, at[0], entry[0], token[0], head[0], at[1],
+                entry[1], token[1], head[1]);
+    });
+    return outputs(rc, {{a[7], out[0]}, {a[8], out[1]}});
+  });
+}
+
 // (address, handle, shape, layer, q, slots, k, v, scale, out, lse)
 PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded_outputs([&]() -> PyObject* {
@@ -555,6 +594,7 @@ PyMethodDef kMethods[] = {
     {"cache_fork", (PyCFunction)(void*)cache_fork, METH_FASTCALL, nullptr},
     {"cache_free", (PyCFunction)(void*)cache_free, METH_FASTCALL, nullptr},
     {"cache_write", (PyCFunction)(void*)cache_write, METH_FASTCALL, nullptr},
+    {"cache_read", (PyCFunction)(void*)cache_read, METH_FASTCALL, nullptr},
     {"cache_attend", (PyCFunction)(void*)cache_attend, METH_FASTCALL, nullptr},
     {"rotate", (PyCFunction)(void*)rotate, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -12,6 +12,14 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 1 << kBlockShift;   // tokens of a block
 int blocks_of(int tokens) { return (int)(((int64_t)tokens + kBlock - 2) / kBlock + 1); }   // that so many tokens can lie in
+// Blocks that a wavefront of a write takes one after the other: all of an entry's where these are up to four and there are more than the machine's 8192 wavefronts hold at once, since
+// most of them have no token (4096 entries of 8 to 16 tokens, 2 heads of 64: 11.9 us, by a wavefront for each block 19.5; 2048 of 20 to 40 14.8 / 20.8), otherwise one (256 of 60 to 500
+// tokens 17.0 us, by runs of four blocks 20.7).
+int blocks_per_run(const Cache& c, int n, int tokens) {
+  const int64_t blocks = (int64_t)n * blocks_of(tokens) * 2 * c.kv_heads;
+  return blocks >= 16384 && blocks_of(tokens) <= 4 ? blocks_of(tokens) : 1;
+}
+int runs_of(const Cache& c, int n, int tokens) { return (blocks_of(tokens) + blocks_per_run(c, n, tokens) - 1) / blocks_per_run(c, n, tokens); }
 
 __device__ __forceinline__ int64_t scale_index(const Cache& c, int64_t page, int layer, int which) {   // which: keys of all heads, then values
   return page * c.page_scales() + ((int64_t)layer * 2 * c.kv_heads + which) * c.page_blocks();
@@ -86,61 +94,74 @@ __device__ __forceinline__ void round_again(char* block, int units, int lane, in
 }
 
 // ---- writing -----------------------------------------------------------------------------------------------------------------------------
-// Several tokens: a wavefront for the keys and values of each block of tokens and head, with the loads of both under way beside the look at the table.
-template <class T, int NT>
-__global__ void __launch_bounds__(256) write8_kernel(Cache c, int layer, int n, const int32_t* slots, int tokens, int blocks, Tokens k, Tokens v) {
+// Several tokens: a wavefront for each head, keys or values, and block of tokens, or with MANY for `per` blocks one after the other, the next one's elements and page on their way.
+template <class T, int NT, bool MANY>
+__global__ void __launch_bounds__(256) write8_kernel(Cache c, int layer, int n, const int32_t* slots, int tokens, int runs, int per, Tokens k, Tokens v) {
   constexpr int D = NT * 32, kUnits = D / 8;   // units of 8 elements of a token
-  const int lane = (int)threadIdx.x & 63;
+  const int lane = (int)threadIdx.x & 63, heads = 2 * c.kv_heads;
   const int64_t piece = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int64_t entry_block = piece / c.kv_heads;
-  const int head = (int)(piece - entry_block * c.kv_heads), i = (int)(entry_block / blocks), b = (int)(entry_block - (int64_t)i * blocks);
+  const int64_t entry_run = piece / heads;
+  const int which = (int)(piece - entry_run * heads), i = (int)(entry_run / runs), run = (int)(entry_run - (int64_t)i * runs);
   if (i >= n) return;
   const int slot = slots ? slots[i] : i;
   if ((uint32_t)slot >= (uint32_t)c.slots) return;
   const int grown = c.grown[slot], first = c.length(slot) - grown, end = first + min(grown, tokens);
-  const int block = (first >> kBlockShift) + b, t0 = block << kBlockShift;
-  if (grown <= 0 || first < 0 || t0 >= end) return;
-  u32x4 raw[2][NT];
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const Tokens& from = w ? v : k;
-    const char* p = from.p + (int64_t)i * from.entry + head * from.head;
+  if (grown <= 0 || first < 0) return;
+  const int block0 = (first >> kBlockShift) + run * per, block_end = min(block0 + per, (end + kBlock - 1) >> kBlockShift);
+  if (block0 >= block_end) return;
+  const bool value = which >= c.kv_heads;
+  const Tokens& from = value ? v : k;
+  const char* p = from.p + (int64_t)i * from.entry + (value ? which - c.kv_heads : which) * from.head;
+  const int32_t* row = c.row(slot);
+  auto load = [&](int block, u32x4 (&raw)[NT], int& page) {
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
-      const int u = lane + 64 * r, t = t0 + u / kUnits;
-      raw[w][r] = u32x4{0, 0, 0, 0};
-      if (t >= first && t < end) raw[w][r] = *(const u32x4_2*)(p + (int64_t)(t - first) * from.token + u % kUnits * 16);
+      const int u = lane + 64 * r, t = (block << kBlockShift) + u / kUnits;
+      raw[r] = u32x4{0, 0, 0, 0};
+      if (t >= first && t < end) raw[r] = *(const u32x4_2*)(p + (int64_t)(t - first) * from.token + u % kUnits * 16);
     }
-  }
-  const int page = c.row(slot)[t0 >> c.page_shift];
-  if (!c.is_page(page)) return;
-  const bool had = first > t0;
-  float* scale[2];
-  float was[2];
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    scale[w] = c.scales + scale_index(c, page, layer, head + w * c.kv_heads) + (block & (c.page_blocks() - 1));
-    was[w] = had ? *scale[w] : 0.0f;
-  }
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
+    page = row[block >> (c.page_shift - kBlockShift)];
+  };
+  auto write = [&](int block, const u32x4 (&raw)[NT], int page) {
+    if (!c.is_page(page)) return;
+    const int t0 = block << kBlockShift;
+    char* to = c.kv + page * c.page_bytes(1) + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes(1) + (int64_t)(t0 & ((1 << c.page_shift) - 1)) * D;
+    float* scale = c.scales + scale_index(c, page, layer, which) + (block & (c.page_blocks() - 1));
+    const bool had = first > t0;
+    const float was = had ? *scale : 0.0f;
     float x[NT][8], m = 0.0f;
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
-      unpack<T>(raw[w][r], x[r]);
+      unpack<T>(raw[r], x[r]);
       m = largest(x[r], m);
     }
     m = half_max(m);
     m = fmaxf(m, __shfl_xor(m, 32));
-    const float own = scale_for(m), now = had && was[w] >= own ? was[w] : own, inverse = 1.0f / now;
-    char* to = c.kv + page * c.page_bytes(1) + ((int64_t)layer * 2 * c.kv_heads + head + w * c.kv_heads) * c.head_bytes(1) + (int64_t)(t0 & ((1 << c.page_shift) - 1)) * D;
+    const float own = scale_for(m), now = had && was >= own ? was : own, inverse = 1.0f / now;
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
       const int u = lane + 64 * r, t = t0 + u / kUnits;
       if (t >= first && t < end) *(u32x2*)(to + u * 8) = encode(x[r], inverse);
     }
-    if (had && now != was[w]) round_again<NT>(to, (first - t0) * kUnits, lane, 64, was[w] / now);
-    if (lane == 0 && now != was[w]) *scale[w] = now;
+    if (had && now != was) round_again<NT>(to, (first - t0) * kUnits, lane, 64, was / now);
+    if (lane == 0 && !(had && now == was)) *scale = now;
+  };
+  u32x4 raw[2][NT];
+  int page[2];
+  load(block0, raw[0], page[0]);
+  if (!MANY) {
+    write(block0, raw[0], page[0]);
+    return;
+  }
+  for (int block = block0;; block += 2) {
+    const bool second = block + 1 < block_end;
+    if (second) load(block + 1, raw[1], page[1]);
+    write(block, raw[0], page[0]);
+    if (!second) break;
+    const bool third = block + 2 < block_end;
+    if (third) load(block + 2, raw[0], page[0]);
+    write(block + 1, raw[1], page[1]);
+    if (!third) break;
   }
 }
 
@@ -596,7 +617,8 @@ template <class T, int NT>
 hipError_t launch_write(const Cache& c, int layer, int n, const int32_t* slots, int tokens, int last_only, const Tokens& k, const Tokens& v, hipStream_t stream) {
   const dim3 grid((unsigned)write8_blocks(c, n, tokens)), block(256);
   if (tokens == 1) hipLaunchKernelGGL((write8_one_kernel<T, NT>), grid, block, 0, stream, c, layer, n, slots, last_only, k, v);
-  else hipLaunchKernelGGL((write8_kernel<T, NT>), grid, block, 0, stream, c, layer, n, slots, tokens, blocks_of(tokens), k, v);
+  else if (blocks_per_run(c, n, tokens) > 1) hipLaunchKernelGGL((write8_kernel<T, NT, true>), grid, block, 0, stream, c, layer, n, slots, tokens, 1, blocks_of(tokens), k, v);
+  else hipLaunchKernelGGL((write8_kernel<T, NT, false>), grid, block, 0, stream, c, layer, n, slots, tokens, blocks_of(tokens), 1, k, v);
   return hipGetLastError();
 }
 template <class T>
@@ -613,7 +635,7 @@ hipError_t write8_for(const Cache& c, int layer, int n, const int32_t* slots, in
 }  // namespace
 
 int64_t write8_blocks(const Cache& c, int n, int tokens) {   // of the launch
-  if (tokens > 1) return ((int64_t)n * blocks_of(tokens) * c.kv_heads + 3) / 4;
+  if (tokens > 1) return ((int64_t)n * runs_of(c, n, tokens) * 2 * c.kv_heads + 3) / 4;
   const int group = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
   return ((int64_t)n * 2 * c.kv_heads * group + 255) / 256;
 }
