@@ -7,6 +7,7 @@
   search      one expansion per game in a pool of state slots: the environment's state and the cache's slot are copied together,
               the new states' move probabilities are the children's priors
 
+A move's place in its game is learned as a table of vectors or, with --rotary, turned into queries and keys; with --bits 8 the cache holds keys and values in half the memory.
 The network is small and its weights are random: what is shown is how the calls fit together.  `python examples/sequence_policy.py`
 """
 import argparse
@@ -22,7 +23,8 @@ import paper_2303_17503_amd as pg  # noqa: E402
 class SequencePolicy:
     """A small transformer over move tokens: 0 .. N*N the moves, N*N + 1 the beginning of a game."""
 
-    def __init__(self, actions, max_plies, layers=2, heads=8, kv_heads=2, head_dim=64, dim=128, seed=0, dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, actions, max_plies, layers=2, heads=8, kv_heads=2, head_dim=64, dim=128, seed=0, dtype=torch.bfloat16, device="cuda",
+                 rotary=False, bits=16):
         g = torch.Generator(device).manual_seed(seed)
         new = lambda *s: (torch.randn(*s, generator=g, device=device) * s[0] ** -0.5).to(dtype)  # noqa: E731
         self.actions, self.start, self.layers, self.heads, self.kv_heads, self.head_dim = actions, actions, layers, heads, kv_heads, head_dim
@@ -32,6 +34,8 @@ class SequencePolicy:
         self.back = [new(heads * head_dim, dim) for _ in range(layers)]
         self.up, self.down = [new(dim, 4 * dim) for _ in range(layers)], [new(4 * dim, dim) for _ in range(layers)]
         self.out = new(dim, actions)
+        self.frequencies = pg.rotary_frequencies(head_dim, device=device) if rotary else None
+        self.bits = bits
 
     def split(self, layer, x):
         """query, key and value heads of one product, as views into it"""
@@ -44,7 +48,8 @@ class SequencePolicy:
         return (x.float() * torch.rsqrt(x.float().square().mean(1, keepdim=True) + 1e-6)).to(x.dtype)
 
     def embed(self, tokens, plies):
-        return self.move[tokens.long()] + self.ply[plies.long()]
+        x = self.move[tokens.long()]
+        return x if self.frequencies is not None else x + self.ply[plies.long()]
 
     def finish(self, layer, x, attended):
         x = x + attended.flatten(1) @ self.back[layer]
@@ -54,9 +59,12 @@ class SequencePolicy:
         """The newest token of each slot, [n][dim], with its keys and values written to the cache: one launch per layer beside the products."""
         cache.advance(slots)
         lengths = cache.lengths if slots is None else cache.lengths[slots.clamp(min=0).long()]
-        x = self.embed(tokens, lengths - 1)
+        plies = lengths - 1
+        x = self.embed(tokens, plies)
         for i in range(self.layers):
             q, k, v = self.split(i, x)
+            if self.frequencies is not None:
+                q, k = pg.rotate((q, k), plies, self.frequencies)
             x = self.finish(i, x, cache.attend(i, q, slots, k=k, v=v))
         return self.norm(x)
 
@@ -64,7 +72,7 @@ class SequencePolicy:
         return features @ self.out
 
     def new_cache(self, slots, pages, max_plies, page_size=16):
-        return pg.PagedCache.empty(slots, pages, max_plies + 1, self.layers, self.kv_heads, self.head_dim, page_size, self.out.dtype)
+        return pg.PagedCache.empty(slots, pages, max_plies + 1, self.layers, self.kv_heads, self.head_dim, page_size, self.out.dtype, bits=self.bits)
 
 
 def gumbel(shape, g):
@@ -137,8 +145,10 @@ def main():
     ap.add_argument("--games", type=int, default=256)
     ap.add_argument("--size", type=int, default=9, choices=(9, 19))
     ap.add_argument("--plies", type=int, default=200)
+    ap.add_argument("--rotary", action="store_true")
+    ap.add_argument("--bits", type=int, default=16, choices=(8, 16))
     a = ap.parse_args()
-    policy = SequencePolicy(a.size * a.size + 1, 2 * a.size * a.size)
+    policy = SequencePolicy(a.size * a.size + 1, 2 * a.size * a.size, rotary=a.rotary, bits=a.bits)
     batch = self_play(policy, a.games, a.size, a.plies)
     print(f"self-play: {a.games} games, {a.plies} plies, {int((batch['result'] != 0).sum())} moves of finished games, "
           f"mean log-probability {float(batch['logp'].mean()):.3f}, {int((batch['cache'].refs > 0).sum())} pages in use")
