@@ -588,8 +588,13 @@ hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, hipStream_t str
 }
 template <class T, int NT>
 hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
-  // As over 16 bits (pgxcache.hip), by how long a slot can be: a wavefront for each of many short rows, four for longer ones, and few rows that can be longer than 32
-  // tiles are split over blocks, two for each compute unit at most.  @@
+  // The lengths are known on the device only, so the choice goes by how long a slot can be and by the rows (2 key heads here, lengths from 1 up, us).
+  //  * From 1024 rows on a wavefront each up to 10 tiles of 32 tokens (with 1, 2, 4 wavefronts: 1024 slots of up to 160 tokens, heads of 32 6.9 7.3 8.7, 64 7.4 8.1 10.2, 128 12.6 14.6 22.1,
+  //    256 22 34 59; 4096 of up to 320, 64 33.9 31.4 38.6), two up to 32 (4096 of up to 722, 64 76.6 73.8 76.2; 1024, 128 39.0 36.0 36.4, 256 81 82 105), then four (1024 of up to
+  //    1500, 64 41.9 41.1 36.0; of 4000 126 122 102), or two for heads of 256, whose four have a compute unit to themselves (1024 of 1500: 157 149 167).
+  //  * Fewer rows: four (200 slots of up to 722, 64 13.7 11.4 8.2; 64, 128 16.4 10.9 8.4), or for heads of 256 up to 32 tiles and from 256 rows on two (200 of up to 722 27.9 20.7 24.7).
+  //  * Few rows that can be longer than 32 tiles are split over blocks, two for each compute unit at most (16 slots of 20000 tokens 20.8, with twice the blocks 27; 512
+  //    slots of 2000 tokens in two blocks each 30.6, in one 23).
   const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles, most_tiles = (((int64_t)c.width << c.page_shift) + 31) / 32;
   a.splits = 1;
   if (most_tiles > 32) {
@@ -598,8 +603,9 @@ hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
     a.splits = (int32_t)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
   }
   a.by_die = a.head_tiles > 1 || (int64_t)a.n * a.splits >= 64;
-  if (a.splits > 1) return launch_attend_by<T, NT, 4, NT < 8 ? 2 : 1, true>(c, a, stream);
-  if (most_tiles <= 8 && rows >= 1024) return launch_attend_by<T, NT, 1, 2, false>(c, a, stream);
+  if (a.splits > 1) return launch_attend_by<T, NT, 4, NT < 8 ? 2 : 1, true>(c, a, stream);   // (heads of 256: 201 slots of 2000 tokens 45.5 us, with the next tile beside the present 54)
+  if (rows >= 1024 && most_tiles <= 10) return launch_attend_by<T, NT, 1, 2, false>(c, a, stream);
+  if ((rows >= 1024 && (most_tiles <= 32 || NT == 8)) || (NT == 8 && rows >= 256 && most_tiles <= 32)) return launch_attend_by<T, NT, 2, 2, false>(c, a, stream);
   return launch_attend_by<T, NT, 4, 2, false>(c, a, stream);
 }
 
