@@ -50,7 +50,9 @@ struct Args {
   int64_t positions_entry, positions_token;
   int32_t tokens, head_dim, pairs, heads, block_tokens, entry_blocks, pair_chunks, chunks;   // heads: of all parts; chunks: of a row, those with pairs first
   float magnitude;
-  int32_t inverse;
+  int32_t per_wave, lanes, t_step, h_step;          // rows that a wavefront, and the block, look at together; these as tokens and heads
+  uint32_t chunks_inverse, heads_inverse, pairs_inverse;   // rounded up: over 2^16, quotients of threads; over 2^32, of angles
+  int32_t entries, inverse, back;   // back: a run of pairs or elements that is not full begins earlier instead, so that it is, and shares some with the one before it
 };
 
 struct Row {   // where a row begins
@@ -63,10 +65,14 @@ __global__ void __launch_bounds__(256) turn_kernel(Args a) {
   typedef typename T::type E;
   extern __shared__ float2 turns[];   // [block_tokens][pairs]: cosine, sine
   const int threads = (int)blockDim.x, tid = (int)threadIdx.x, A = a.pairs;
-  const int entry = (int)(blockIdx.x / (uint32_t)a.entry_blocks), token0 = (int)(blockIdx.x - (uint32_t)entry * (uint32_t)a.entry_blocks) * a.block_tokens;
+  const int entry = a.entries == 1 ? 0 : (int)(blockIdx.x / (uint32_t)a.entry_blocks), token0 = (int)(blockIdx.x - (uint32_t)entry * (uint32_t)a.entry_blocks) * a.block_tokens;
   const int here = min(a.block_tokens, a.tokens - token0), rows = here * a.heads;
-  const int lanes = threads / a.chunks, chunk = tid % a.chunks, row0 = tid / a.chunks;   // rows that the block looks at together
-  const bool busy = row0 < lanes;
+  // Rows that the block looks at together.  A row's chunks are in one wavefront where that holds them: it has loaded all of a row before it stores any, so chunks that share
+  // elements may be turned in place.
+  const bool whole = a.chunks <= 64;
+  const int part = whole ? tid & 63 : tid, in_part = (int)((uint32_t)part * a.chunks_inverse >> 16), chunk = part - in_part * a.chunks;
+  const int row0 = whole ? tid / 64 * a.per_wave + in_part : in_part, lanes = a.lanes;
+  const bool busy = in_part < (whole ? a.per_wave : lanes);
 
   // both parts' addresses of the block's first token, and a row's from them
   const E *in0 = (const E*)a.part[0].in_dev + entry * a.part[0].in_entry_stride + token0 * a.part[0].in_token_stride;
@@ -82,8 +88,9 @@ __global__ void __launch_bounds__(256) turn_kernel(Args a) {
     return Row{(const char*)((second ? in1 : in0) + t * in_token + head * in_head), (char*)((second ? out1 : out0) + t * out_token + head * out_head)};
   };
   const bool turned = chunk < a.pair_chunks;
-  const int at = turned ? chunk * 8 : 2 * A + (chunk - a.pair_chunks) * 8;              // first pair, or first element that is copied
-  const int many = min(8, turned ? A - at : a.head_dim - at);                           // pairs or elements
+  const int low = turned ? 0 : 2 * A, high = turned ? A : a.head_dim, begin = low + (turned ? chunk : chunk - a.pair_chunks) * 8;
+  const int at = a.back && high - low >= 8 ? min(begin, high - 8) : begin;              // first pair, or first element that is copied
+  const int many = min(8, high - at);                                                   // pairs or elements
   const int u0 = !turned ? at : INTERLEAVED ? 2 * at : at, w0 = INTERLEAVED ? u0 + 8 : at + A;   // the two runs of elements; of a copied chunk the first
   struct Chunk {
     f32x8 x, y;   // the two runs
@@ -106,14 +113,13 @@ __global__ void __launch_bounds__(256) turn_kernel(Args a) {
   };
   Chunk now_chunk = {};
   Row now{nullptr, nullptr};
-  const int t_step = lanes / a.heads, h_step = lanes - t_step * a.heads;
-  int t = row0 / a.heads, h = row0 - t * a.heads;
+  int t = (int)((uint32_t)row0 * a.heads_inverse >> 16), h = row0 - t * a.heads;
   if (busy && row0 < rows) {   // the first row is on its way while the angles are worked out
     now = row(t, h);
     now_chunk = load(now.in);
   }
   for (int k = tid; k < here * A; k += threads) {
-    const int t = k / A, j = k - t * A;
+    const int t = A == 1 ? k : (int)__umulhi((uint32_t)k, a.pairs_inverse), j = k - t * A;
     const int32_t position = a.positions[entry * a.positions_entry + (int64_t)(token0 + t) * a.positions_token];
     const double turn = (double)position * (a.frequencies[j] * 0.15915494309189533577), part = turn - rint(turn);   // of a whole circle, to -1/2 .. 1/2
     float s, c;
@@ -126,8 +132,8 @@ __global__ void __launch_bounds__(256) turn_kernel(Args a) {
     Chunk next_chunk = {};
     Row next{nullptr, nullptr};
     const float2* turn = turns + t * A + at;
-    t += t_step;
-    h += h_step;
+    t += a.t_step;
+    h += a.h_step;
     if (h >= a.heads) {
       h -= a.heads;
       ++t;
@@ -179,6 +185,14 @@ hipError_t launch(Args& a, int32_t entries, bool interleaved, hipStream_t stream
   a.block_tokens = (a.tokens + a.entry_blocks - 1) / a.entry_blocks;
   if ((int64_t)entries * a.entry_blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   const int threads = a.chunks <= 64 && a.block_tokens * per_token <= 128 ? 64 : 256;
+  a.entries = entries;
+  a.per_wave = a.chunks <= 64 ? 64 / a.chunks : 0;
+  a.lanes = a.chunks <= 64 ? threads / 64 * a.per_wave : threads / a.chunks;
+  a.t_step = a.lanes / a.heads; a.h_step = a.lanes % a.heads;
+  // (exact: thread * (what rounding up adds) is below the power of two for up to 256 threads and divisors, 4096 angles of up to 512 pairs; quotients by more heads are 0)
+  a.chunks_inverse = (65536u + (uint32_t)a.chunks - 1) / (uint32_t)a.chunks;
+  a.heads_inverse = (65536u + (uint32_t)a.heads - 1) / (uint32_t)a.heads;
+  a.pairs_inverse = a.pairs == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + (uint64_t)a.pairs - 1) / (uint64_t)a.pairs);
   const dim3 grid((unsigned)(entries * a.entry_blocks)), block((unsigned)threads);
   const size_t lds = ((size_t)a.block_tokens * a.pairs + 8) * sizeof(float2);
   if (interleaved) hipLaunchKernelGGL((turn_kernel<T, true>), grid, block, lds, stream, a);
@@ -214,7 +228,7 @@ int pgxrotary_turn(int32_t entries, int32_t tokens, int32_t head_dim, int32_t ro
   const int64_t total = (int64_t)entries * tokens;
   if (total > 0x7FFFFFFF) return PGXROTARY_EINVAL;
   Args a = {};
-  bool in_place = true;
+  bool in_place = true, any_in_place = false;
   for (int k = 0; k < parts; ++k) {
     const pgxrotary_part& p = part[k];
     if (p.heads < 0 || p.heads > 65536) return PGXROTARY_EINVAL;
@@ -228,6 +242,7 @@ int pgxrotary_turn(int32_t entries, int32_t tokens, int32_t head_dim, int32_t ro
                       (p.heads == 1 || p.in_head_stride == p.out_head_stride);
     if (p.in_dev == p.out_dev && !same) return PGXROTARY_EINVAL;
     in_place = in_place && same;
+    any_in_place = any_in_place || same;
   }
   if (total == 0 || a.heads == 0) return PGXROTARY_OK;
   if (parts == 2 && part[0].heads > 0 && part[1].heads > 0 && part[0].out_dev == part[1].out_dev) return PGXROTARY_EINVAL;   // one tensor given twice
@@ -237,6 +252,7 @@ int pgxrotary_turn(int32_t entries, int32_t tokens, int32_t head_dim, int32_t ro
   a.tokens = tokens; a.head_dim = head_dim; a.pairs = rotary_dim / 2;
   a.pair_chunks = (a.pairs + 7) / 8;
   a.chunks = a.pair_chunks + (in_place ? 0 : (head_dim - rotary_dim + 7) / 8);
+  a.back = a.chunks <= 64 || !any_in_place;
   // entries whose tokens follow each other's in every tensor are one long entry, and so are entries of one token
   bool follow = true;
   auto next = [&](int64_t& entry, int64_t& token) {

@@ -34,7 +34,8 @@ def whole(g, lo, hi, *shape):
 
 
 SHAPES = [(1, None, 1, 1, 2, 2), (3, None, 2, 1, 3, 2), (5, None, 8, 2, 64, 64), (7, None, 3, 3, 96, 96), (2, 9, 4, 1, 128, 32), (3, 4, 5, 2, 80, 20), (2, 3, 2, 1, 33, 18),
-          (300, None, 8, 2, 64, 64), (2, 700, 6, 2, 32, 32), (1, 3, 1, 1, 1024, 1024), (1, 2, 2, 1, 1023, 514), (2, 3, 3, 2, 256, 16), (4, 500, 1, 1, 17, 14), (2, 1, 40, 8, 256, 250)]
+          (300, None, 8, 2, 64, 64), (2, 700, 6, 2, 32, 32), (1, 3, 1, 1, 1024, 1024), (1, 2, 2, 1, 1023, 514), (2, 3, 3, 2, 256, 16), (4, 500, 1, 1, 17, 14), (2, 1, 40, 8, 256, 250), (3, 5, 300, 1, 16, 16), (1000, None, 1, 1, 512, 512),
+          (5, 77, 7, 3, 130, 130), (2, 3, 2, 1, 1024, 2), (600, 3, 1, 2, 30, 30)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
@@ -90,6 +91,21 @@ def test_strides(interleaved, dtype):
     assert torch.equal(q, a) and torch.equal(k, b) and torch.equal(product[..., 1 + (H + KV) * D:], before[..., 1 + (H + KV) * D:]) and torch.equal(product[..., 0], before[..., 0])
     repeated = q[:1, :, :1].expand(2, T, 3, D)                                        # an input's rows may overlap
     check(pg.rotate(repeated, positions[:2], f, interleaved=interleaved), repeated, positions[:2], f, interleaved, 1.0, False)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,R", [(64, 64), (66, 50), (1024, 514), (1023, 1006), (18, 18), (17, 2)])
+def test_one_of_a_pair_in_place(D, R, interleaved):
+    g = torch.Generator("cuda").manual_seed(D)
+    q, k = torch.randn(90, 3, D, generator=g, device="cuda").bfloat16(), torch.randn(90, 2, D, generator=g, device="cuda").bfloat16()
+    positions, f = whole(g, 0, 5000, 90), pg.rotary_frequencies(R)
+    want = pg.rotate((q, k), positions, f, interleaved=interleaved)
+    check(want[0], q, positions, f, interleaved, 1.0, False)
+    first, second = q.clone(), k.clone()
+    a, b = pg.rotate((first, k), positions, f, interleaved=interleaved, out=(first, torch.empty_like(k)))
+    assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+    a, b = pg.rotate((q, second), positions, f, interleaved=interleaved, out=(torch.empty_like(q), second))
+    assert torch.equal(a, want[0]) and torch.equal(b, want[1])
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
