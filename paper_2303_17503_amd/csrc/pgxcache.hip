@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "cache_common.hpp"
+#include "rows_apart.hpp"
 
 namespace {
 
@@ -857,21 +858,6 @@ Cache cache_of(pgxcache_t h) {
   c.layers = h->o.layers; c.kv_heads = h->o.kv_heads; c.head_dim = h->o.head_dim;
   return c;
 }
-// rows of `row` elements at these strides do not overlap: in the order of their strides, each dimension steps over what the smaller ones cover
-bool apart(const int64_t (&sizes)[3], const int64_t (&strides)[3], int64_t row) {
-  int64_t covered = row;
-  bool used[3] = {false, false, false};
-  for (int k = 0; k < 3; ++k) {
-    int least = -1;
-    for (int d = 0; d < 3; ++d)
-      if (!used[d] && (least < 0 || llabs(strides[d]) < llabs(strides[least]))) least = d;
-    used[least] = true;
-    if (sizes[least] == 1) continue;
-    if (llabs(strides[least]) < covered) return false;
-    covered += llabs(strides[least]) * (sizes[least] - 1);
-  }
-  return true;
-}
 bool list_ok(pgxcache_t h, int32_t n) { return h && n >= 0 && n <= h->o.slots; }
 int scan(pgxcache_t h, int first) {
   const int64_t most = h->o.pages > h->o.slots ? h->o.pages : h->o.slots, threads = most > kSplitBlocks ? most : kSplitBlocks;
@@ -999,7 +985,7 @@ int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_d
   if (n == 0 || tokens == 0) return PGXCACHE_OK;
   if (!k_dev || !v_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 1u) != 0) return PGXCACHE_EINVAL;
   const int64_t sizes[3] = {n, tokens, h->o.kv_heads}, ks[3] = {k_entry_stride, k_token_stride, k_head_stride}, vs[3] = {v_entry_stride, v_token_stride, v_head_stride};
-  if (!apart(sizes, ks, h->o.head_dim) || !apart(sizes, vs, h->o.head_dim)) return PGXCACHE_EINVAL;
+  if (k_dev == v_dev || !rows_apart(sizes, ks, h->o.head_dim) || !rows_apart(sizes, vs, h->o.head_dim)) return PGXCACHE_EINVAL;
   const Cache c = cache_of(h);
   if (read_blocks(c, n, tokens) > 0x7FFFFFFF) return PGXCACHE_EINVAL;
   const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};

@@ -76,10 +76,10 @@ __device__ __forceinline__ float half_max(float x) {
   return fmaxf(x, __shfl_xor(x, 16));
 }
 
-// A block's earlier tokens are rounded once more for a larger scale: `units` runs of 8 elements, `lanes` lanes, N at most for each, four under way together.
+// A block's earlier tokens are rounded once more for a larger scale: `units` runs of 8 elements, `lanes` lanes, N at most for each, eight under way together.
 template <int N>
 __device__ __forceinline__ void round_again(char* block, int units, int lane, int lanes, float ratio) {
-  constexpr int kAhead = N < 4 ? N : 4;
+  constexpr int kAhead = N < 8 ? N : 8;
   for (int u0 = lane; u0 < units; u0 += lanes * kAhead) {
     u32x2 w[kAhead];
 #pragma unroll
@@ -294,7 +294,7 @@ __device__ __forceinline__ constexpr int key_element(int m, int g) { return (NT 
 // W wavefronts share a row: an entry, a key head and a tile of 16 query heads.  SPLIT: a row may be split over blocks.  STREAM: keys and values are read with the hint
 // that they are not read again soon.
 template <class T, int NT, int W, int BUF, bool SPLIT, bool STREAM>
-__global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : W == 16 ? 4 : 2) attend8_kernel(Cache c, AttendArgs a) {
+__global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_kernel(Cache c, AttendArgs a) {
   typedef typename T::x8 x8;
   typedef typename BF16::x8 v8;
   constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane

@@ -8,6 +8,7 @@
 #include <stdlib.h>
 
 #include "pgxrotary.h"
+#include "rows_apart.hpp"
 
 namespace {
 
@@ -200,22 +201,6 @@ hipError_t launch(Args& a, int32_t entries, bool interleaved, hipStream_t stream
   return hipGetLastError();
 }
 
-// rows of `row` elements at these strides do not overlap: in the order of their strides, each dimension steps over what the smaller ones cover
-bool apart(const int64_t (&sizes)[3], const int64_t (&strides)[3], int64_t row) {
-  int64_t covered = row;
-  bool used[3] = {false, false, false};
-  for (int k = 0; k < 3; ++k) {
-    int least = -1;
-    for (int d = 0; d < 3; ++d)
-      if (!used[d] && (least < 0 || llabs(strides[d]) < llabs(strides[least]))) least = d;
-    used[least] = true;
-    if (sizes[least] == 1) continue;
-    if (llabs(strides[least]) < covered) return false;
-    covered += llabs(strides[least]) * (sizes[least] - 1);
-  }
-  return true;
-}
-
 }  // namespace
 
 extern "C" {
@@ -237,7 +222,7 @@ int pgxrotary_turn(int32_t entries, int32_t tokens, int32_t head_dim, int32_t ro
     if (p.heads == 0 || total == 0) continue;
     const uintptr_t either = (uintptr_t)p.in_dev | (uintptr_t)p.out_dev;
     const int64_t sizes[3] = {entries, tokens, p.heads}, out[3] = {p.out_entry_stride, p.out_token_stride, p.out_head_stride};
-    if (!p.in_dev || !p.out_dev || (either & (type == PGXROTARY_F32 ? 3u : 1u)) != 0 || !apart(sizes, out, head_dim)) return PGXROTARY_EINVAL;
+    if (!p.in_dev || !p.out_dev || (either & (type == PGXROTARY_F32 ? 3u : 1u)) != 0 || !rows_apart(sizes, out, head_dim)) return PGXROTARY_EINVAL;
     const bool same = p.in_dev == p.out_dev && (entries == 1 || p.in_entry_stride == p.out_entry_stride) && (tokens == 1 || p.in_token_stride == p.out_token_stride) &&
                       (p.heads == 1 || p.in_head_stride == p.out_head_stride);
     if (p.in_dev == p.out_dev && !same) return PGXROTARY_EINVAL;

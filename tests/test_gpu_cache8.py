@@ -554,6 +554,7 @@ REFUSED = [
     ("read: k of another type", lambda c, q, k: c.read(0, 1, k=torch.zeros(2, 1, 2, 64, dtype=torch.float16, device="cuda"))),
     ("read: k that overlaps", lambda c, q, k: c.read(0, 3, k=torch.zeros(2, 1, 2, 64, dtype=torch.bfloat16, device="cuda").expand(2, 3, 2, 64))),
     ("read: v that overlaps", lambda c, q, k: c.read(0, 3, v=torch.zeros(4000, dtype=torch.bfloat16, device="cuda").as_strided((2, 3, 2, 64), (384, 128, 63, 1)))),
+    ("read: keys and values into one tensor", lambda c, q, k: (lambda t: c.read(0, 3, k=t, v=t))(torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16, device="cuda"))),
     ("read: entries that overlap", lambda c, q, k: c.read(0, 3, v=torch.zeros(4000, dtype=torch.bfloat16, device="cuda").as_strided((2, 3, 2, 64), (256, 128, 64, 1)))),
 ]
 
