@@ -477,16 +477,16 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
       load_keys(next, number + 1);
       load_values(next, number + 1);
     }
+    s[0] = s[1] = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      s[h] = f32x4{0, 0, 0, 0};
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
-      for (int m = 0; m < NT; ++m) {
+      for (int h = 0; h < 2; ++h) {   // (two chains of products that do not wait for each other)
         const uint32_t w0 = t.k[h][2 * m], w1 = t.k[h][2 * m + 1];
         s[h] = T::mfma(__builtin_bit_cast(x8, u32x4{Decoded<T>::low(w0), Decoded<T>::high(w0), Decoded<T>::low(w1), Decoded<T>::high(w1)}), q[m], s[h]);
       }
-      s[h] *= key_scales_here[h];
-    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) s[h] *= key_scales_here[h];
     if (BUF == 1 && !last.value) {
       turn();
       load_keys(t, number + 1);
@@ -532,10 +532,10 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
         y[j] = Decoded<BF16>::high(w);
       }
       acc[2 * m] = BF16::mfma(__builtin_bit_cast(v8, x), high, acc[2 * m]);
-      acc[2 * m] = BF16::mfma(__builtin_bit_cast(v8, x), low, acc[2 * m]);
       acc[2 * m + 1] = BF16::mfma(__builtin_bit_cast(v8, y), high, acc[2 * m + 1]);
+      acc[2 * m] = BF16::mfma(__builtin_bit_cast(v8, x), low, acc[2 * m]);
       acc[2 * m + 1] = BF16::mfma(__builtin_bit_cast(v8, y), low, acc[2 * m + 1]);
-      if (NT == 8) __builtin_amdgcn_sched_barrier(0);
+      if (NT == 8 && m % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (decoding far ahead of the products takes registers that are not there)
     }
     if (BUF == 1 && !last.value) load_values(t, number + 1);
   };
@@ -589,10 +589,12 @@ hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, hipStream_t str
 template <class T, int NT>
 hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
   // The lengths are known on the device only, so the choice goes by how long a slot can be and by the rows (2 key heads here, lengths from 1 up, us).
-  //  * From 1024 rows on a wavefront each up to 10 tiles of 32 tokens (with 1, 2, 4 wavefronts: 1024 slots of up to 160 tokens, heads of 32 6.9 7.3 8.7, 64 7.4 8.1 10.2, 128 12.6 14.6 22.1,
-  //    256 22 34 59; 4096 of up to 320, 64 33.9 31.4 38.6), two up to 32 (4096 of up to 722, 64 76.6 73.8 76.2; 1024, 128 39.0 36.0 36.4, 256 81 82 105), then four (1024 of up to
-  //    1500, 64 41.9 41.1 36.0; of 4000 126 122 102), or two for heads of 256, whose four have a compute unit to themselves (1024 of 1500: 157 149 167).
-  //  * Fewer rows: four (200 slots of up to 722, 64 13.7 11.4 8.2; 64, 128 16.4 10.9 8.4), or for heads of 256 up to 32 tiles and from 256 rows on two (200 of up to 722 27.9 20.7 24.7).
+  //  * Up to 10 tiles of 32 tokens and from 1024 rows on a wavefront each (with 1, 2, 4 wavefronts: 1024 slots of up to 160 tokens, heads of 32 6.9 7.3 8.7, 64 7.4 8.1 10.2, 128 12.6 14.6
+  //    22.1, 256 22 34 59; of up to 320, 64 11.8 12.5 13.4; 4096 of up to 320, 64 33.9 31.4 38.6, 128 75 77 100).
+  //  * Up to 32 tiles and from 4096 rows on two (4096 of up to 722, 64 76.6 73.8 76.2; 1024 22.3 22.2 20.2).  Heads of 256, whose four have a compute unit to
+  //    themselves: from 256 rows on (200 of up to 722 27.9 20.7 24.7, 1024 81 82 105), and from 1024 on however long (1024 of up to 1500 157 149 167).
+  //  * Otherwise four (200 slots of up to 722, 64 13.7 11.4 8.2; 64, 128 16.4 10.9 8.4; 1024 of up to 1500, 64 41.9 41.1 36.0, of 4000 126 122 102); eight take as long with few rows and
+  //    longer with many (one of 722 6.8 / 6.9, 256 9.3 / 8.3, 1024 26 / 21).
   //  * Few rows that can be longer than 32 tiles are split over blocks, two for each compute unit at most (16 slots of 20000 tokens 20.8, with twice the blocks 27; 512
   //    slots of 2000 tokens in two blocks each 30.6, in one 23).
   const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles, most_tiles = (((int64_t)c.width << c.page_shift) + 31) / 32;
@@ -605,7 +607,7 @@ hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
   a.by_die = a.head_tiles > 1 || (int64_t)a.n * a.splits >= 64;
   if (a.splits > 1) return launch_attend_by<T, NT, 4, NT < 8 ? 2 : 1, true>(c, a, stream);   // (heads of 256: 201 slots of 2000 tokens 45.5 us, with the next tile beside the present 54)
   if (rows >= 1024 && most_tiles <= 10) return launch_attend_by<T, NT, 1, 2, false>(c, a, stream);
-  if ((rows >= 1024 && (most_tiles <= 32 || NT == 8)) || (NT == 8 && rows >= 256 && most_tiles <= 32)) return launch_attend_by<T, NT, 2, 2, false>(c, a, stream);
+  if (NT == 8 ? rows >= 1024 || (rows >= 256 && most_tiles <= 32) : rows >= 4096 && most_tiles <= 32) return launch_attend_by<T, NT, 2, 2, false>(c, a, stream);
   return launch_attend_by<T, NT, 4, 2, false>(c, a, stream);
 }
 

@@ -236,7 +236,7 @@ def test_long_sequences(head_dim, kv_heads, group, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("head_dim", [32, 64, 96, 128, 256])
-@pytest.mark.parametrize("tiles,n", [(8, 20), (10, 520), (11, 520), (32, 512), (9, 20), (32, 300), (33, 5), (40, 512), (80, 20), (80, 300), (600, 2), (200, 300), (1200, 12)])
+@pytest.mark.parametrize("tiles,n", [(8, 20), (10, 520), (11, 520), (32, 512), (12, 2050), (9, 20), (32, 300), (33, 5), (40, 512), (80, 20), (80, 300), (600, 2), (200, 300), (1200, 12)])
 def test_attention_in_each_way_that_rows_are_spread(tiles, n, head_dim, dtype):
     """one wavefront to a row, four, four in each of several blocks; and more than 32 tiles for a wavefront, which looks its pages up 32 tiles at a time"""
     some = min(n, 12 if tiles > 100 else 16)
