@@ -1,7 +1,11 @@
 // pgxrotary.hip -- queries and keys turned by their positions (include/pgxrotary.h), gfx950.
 //
 // A block has some tokens.  The cosines and sines of their positions are worked out once, in LDS, for all heads of both tensors (an angle takes 64-bit
-// arithmetic and some 40 instructions, a pair of elements 4); then threads take the rows, 8 pairs each, so that neighbouring threads read neighbouring memory.
+// arithmetic and some 100 instructions, a pair of elements 4); then threads take the rows, 8 pairs each, so that neighbouring threads read neighbouring memory, with the next
+// row on its way while one is turned.
+//
+// Bound by the bytes: 185000 tokens of 10 heads of 64 in bfloat16 96.8 us, 4.9 TB/s (vector instructions keep half of the time busy); 40001 of 16 heads of 128 in float32, half of each turned, 137 us,
+// 4.8 TB/s.  One ply of 256 games 3.3 us: a launch, one round trip to memory and an angle.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -175,10 +179,12 @@ __global__ void __launch_bounds__(256) turn_kernel(Args a) {
 
 template <class T>
 hipError_t launch(Args& a, int32_t entries, bool interleaved, hipStream_t stream) {
-  // Tokens of a block: as many as give each of 256 threads four chunks, fewer where that would leave the machine's 256 compute units without four blocks each;
-  // an entry's tokens in equal shares.
+  // Tokens of a block: as many as give each of 256 threads three chunks, two of 32-bit elements (185000 tokens of 10 heads of 64 in bfloat16: 96.8 us, with two 96.6, four 98.3, eight 104; 192000 of 3
+  // heads of 256 126.5, 137.8, 130.4, 150; 40001 of 16 heads of 128 in float32 with one 134.6, two 137, three 139, four 143; 160000 of 10 of 130 389, 386, 398, 411), fewer where that would
+  // leave the machine's 256 compute units without four blocks each (16384 tokens of one ply: 9.7 us, with half and twice the blocks 11.0 and 9.8); an entry's tokens in equal shares.
+  constexpr int kChunks = sizeof(typename T::type) == 4 ? 2 : 3;
   const int64_t per_token = (int64_t)a.heads * a.chunks, spread = ((int64_t)entries * a.tokens + 1023) / 1024, room = 4096 / a.pairs;
-  int64_t tokens = (4 * 256 + per_token - 1) / per_token;
+  int64_t tokens = (kChunks * 256 + per_token - 1) / per_token;
   tokens = tokens < spread ? tokens : spread;
   tokens = tokens < room ? tokens : room;
   if (tokens < 1) tokens = 1;
