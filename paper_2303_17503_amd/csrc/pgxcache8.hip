@@ -32,6 +32,8 @@ __device__ __forceinline__ float scale_for(float m) {
 }
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 0x1.fffffep127f; }
 
+__device__ __forceinline__ float reciprocal(float scale) { return __builtin_amdgcn_rcpf(scale); }   // exact for powers of two
+
 template <class T>
 __device__ __forceinline__ void unpack(const u32x4& w, float* x) {
   const typename T::x8 h = __builtin_bit_cast(typename T::x8, w);
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(256) write8_kernel(Cache c, int layer, int n, 
     }
     m = half_max(m);
     m = fmaxf(m, __shfl_xor(m, 32));
-    const float own = scale_for(m), now = had && was >= own ? was : own, inverse = 1.0f / now;
+    const float own = scale_for(m), now = had && was >= own ? was : own, inverse = reciprocal(now);
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
       const int u = lane + 64 * r, t = t0 + u / kUnits;
@@ -197,7 +199,7 @@ __global__ void __launch_bounds__(256) write8_one_kernel(Cache c, int layer, int
   if (!writes) return;
   const float own = scale_for(m), now = before > 0 && was >= own ? was : own;
   char* to = c.kv + page * c.page_bytes(1) + ((int64_t)layer * 2 * c.kv_heads + which) * c.head_bytes(1) + (int64_t)(t & ((1 << c.page_shift) - 1) & ~(kBlock - 1)) * D;
-  if (u < kUnits) *(u32x2*)(to + before * D + u * 8) = encode(x, 1.0f / now);
+  if (u < kUnits) *(u32x2*)(to + before * D + u * 8) = encode(x, reciprocal(now));
   if (before == 0 || now != was) {
     if (before > 0) round_again<15>(to, before * kUnits, u, kGroup, was / now);
     if (u == 0) *scale = now;
@@ -392,7 +394,7 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
   // The new token goes into the cache ahead of the loads of the last tile, by the wavefront that reads that (nobody else reads its block, and a
   // wavefront's own memory operations are in order), beside its first tile's on their way.
   const bool renews = grown > 0 && mine > 0 && end == tiles && wave == (tiles - 1 - begin) % W;
-  auto renew = [&]() {
+  auto renew = [&](const float* x, float own) {   // the elements, and the scale that they ask for
     const int at = length - 1, before = at & (kBlock - 1), half = (mine - 1) * 2 + (at >> kBlockShift & 1);   // (of the first 32 tiles: a lane's)
     const bool near = half < 64;
     const int page = near ? (pages_there >> half & 1 ? __builtin_amdgcn_readlane(ids, half) : -1) : row[at >> c.page_shift];
@@ -400,10 +402,8 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
     const int64_t scale_at = page * page_scales + (at >> kBlockShift & in_blocks);
     char* block = (char*)(lane < 32 ? keys : values) + page * page_bytes + (int64_t)(at & in_page & ~(kBlock - 1)) * D;
     const float was = near ? (lane < 32 ? lane_of(asked_key_scale, half) : lane_of(asked_value_scale, half)) : (lane < 32 ? key_scales : value_scales)[scale_at];
-    float x[8];
-    unpack<T>(fresh, x);
-    const float own = scale_for(half_max(largest(x, 0.0f))), now = before > 0 && was >= own ? was : own;
-    if (writes) *(u32x2*)(block + before * D + (lane & 31) * 8) = encode(x, 1.0f / now);
+    const float now = before > 0 && was >= own ? was : own;
+    if (writes) *(u32x2*)(block + before * D + (lane & 31) * 8) = encode(x, reciprocal(now));
     if (before == 0 || now != was) {
       if (before > 0) round_again<2 * NT>(block, before * (D / 8), lane & 31, 32, was / now);
       if ((lane & 31) == 0) (lane < 32 ? key_scales : value_scales)[scale_at] = now;
@@ -548,9 +548,14 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
       load_keys(t0, 0);
       load_values(t0, 0);
     }
+    float x[8], own = 0.0f;
+    if (renews) {
+      unpack<T>(fresh, x);
+      own = scale_for(half_max(largest(x, 0.0f)));
+    }
     take_over(0);
     if (renews) {
-      renew();
+      renew(x, own);
       if (mine == 1) {
         load_keys(t0, 0);
         load_values(t0, 0);
