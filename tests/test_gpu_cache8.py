@@ -93,7 +93,7 @@ def new(g, dtype, *shape, size=1.0):
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("head_dim", [32, 64, 96, 128, 256])
-@pytest.mark.parametrize("page_size", [16, 32, 64])
+@pytest.mark.parametrize("page_size", [16, 32, 64, 256])
 def test_tokens_as_they_come(page_size, head_dim, dtype):
     """rooms of many sizes, one after the other, louder and quieter, so that blocks begin inside a call, end inside one and are raised by one; all codes and scales"""
     r, g = random.Random(head_dim + page_size), torch.Generator("cuda").manual_seed(head_dim)
@@ -118,7 +118,7 @@ def test_tokens_as_they_come(page_size, head_dim, dtype):
             k, v = cache.read(layer, 6 * page_size)
             want = ref.read(layer, 6 * page_size, range(slots), [0] * slots, dtype)
             assert torch.equal(bits(k), bits(want[0])) and torch.equal(bits(v), bits(want[1]))
-    assert int(cache.lengths.max()) > page_size + 16
+    assert int(cache.lengths.max()) > min(page_size, 64) + 16
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
@@ -197,7 +197,7 @@ def test_reading_back(head_dim, page_size, dtype, bits_):
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("head_dim", [32, 64, 96, 128, 256])
-@pytest.mark.parametrize("page_size", [16, 32, 64])
+@pytest.mark.parametrize("page_size", [16, 32, 64, 1024])
 def test_attention_over_lengths_and_head_sizes(head_dim, page_size, dtype):
     kv_heads, heads = 2, 6
     cache = filled(EDGES, 2, kv_heads, head_dim, page_size, dtype, seed=head_dim)
@@ -360,7 +360,8 @@ def test_a_pool_beyond_every_cache_gives_the_same(n, head_dim, heads):
 # ---- pages -----------------------------------------------------------------------------------------------------------------------------
 
 
-@pytest.mark.parametrize("page_size,kv_heads,head_dim,layers,dtype", [(16, 2, 64, 2, torch.bfloat16), (32, 1, 32, 1, torch.float16), (64, 3, 96, 1, torch.float16), (16, 1, 256, 3, torch.bfloat16)])
+@pytest.mark.parametrize("page_size,kv_heads,head_dim,layers,dtype", [(16, 2, 64, 2, torch.bfloat16), (32, 1, 32, 1, torch.float16), (64, 3, 96, 1, torch.float16), (16, 1, 256, 3, torch.bfloat16),
+                                                                      (512, 1, 32, 1, torch.bfloat16)])
 @pytest.mark.parametrize("seed", range(2))
 def test_random_histories(page_size, kv_heads, head_dim, layers, dtype, seed):
     """Every call in random order on a pool that runs out now and then; everything compared after each."""
