@@ -567,3 +567,54 @@ def test_refusals(what, native, monkeypatch):
         monkeypatch.setattr(pg.cache_binding, "_fast", None)
     with pytest.raises(pg.PgxGoError):
         dict(REFUSED)[what](*cache_and_more())
+
+
+def test_native_and_python_checks_make_the_same_calls(monkeypatch):
+    def history():
+        g = torch.Generator("cuda").manual_seed(1)
+        cache = filled([20, 5, 0, 33], 2, 2, 64, 16, torch.bfloat16, width=6, spare=20, junk=False)
+        out = []
+        cache.advance()
+        cache.write(0, new(g, torch.bfloat16, 4, 2, 64), new(g, torch.bfloat16, 4, 2, 64))
+        cache.advance(ints([3, -1, 1]), ints([2, 1, 9]))
+        many = new(g, torch.bfloat16, 3, 11, 2, 64)
+        cache.write(1, many, many.flip(1), ints([3, -1, 1]))
+        out += [*cache.attend(1, new(g, torch.bfloat16, 2, 6, 64), ints([3, 0]), lse=True), cache.attend(0, new(g, torch.bfloat16, 2, 4, 64), ints([1, 0]), k=many[:2, 0], v=many[:2, 1])]
+        out += [*cache.read(1, 7), *cache.read(0, 3, ints([2, 3, 3]), ints([0, 30, -1])), *cache.read(0, 9, first=4), *cache.read(1, 0)]
+        wide = torch.zeros(2, 4, 2, 6, 64, dtype=torch.bfloat16, device="cuda")
+        out += list(cache.read(1, 6, None, 2, wide[0].transpose(1, 2), wide[1].transpose(1, 2)))
+        cache.fork(ints([3, 0]), ints([2, 1]))
+        return out + [cache.kv.view(torch.uint8), cache.scales, cache.table, cache.lengths, cache.refs]
+
+    assert pg.cache_binding._fast is not None
+    native = history()
+    monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    for a, b in zip(native, history()):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_numbers_are_whole(native, monkeypatch):
+    cache, q, k = cache_and_more()
+    if not native:
+        monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    for call in (lambda: cache.read(0.5, 1), lambda: cache.read("0", 1), lambda: cache.read(0, None), lambda: cache.read(0, 2 ** 31), lambda: cache.read(0, 1, first=0.5), lambda: cache.read(0, 1, first=2 ** 31),
+                 lambda: cache.read(0, 1, first=[0, 0]), lambda: cache.read(0, 1, slots=[0]), lambda: cache.read(0, 1, k=3), lambda: cache.read(0, 1, v=q)):
+        with pytest.raises(pg.PgxGoError):
+            call()
+    one = torch.ones(1, dtype=torch.int64).numpy()[0]
+    assert torch.equal(cache.read(one, one, first=one)[0], cache.read(1, 1, first=1)[0])
+
+
+def test_lists_on_another_device_are_left_alone():
+    """A handle that says it is on another device stands for tensors on another device: neither the native checks nor Python's pass them on."""
+    cache, q, k = cache_and_more()
+    before = cache.kv.view(torch.uint8).clone()
+    one = ints([0])
+    cache._shape = cache._shape[:4] + (1,) + cache._shape[5:]
+    cache.device = torch.device("cuda:1")
+    out = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: cache.read(0, 1, one, k=out, v=out.clone()), lambda: cache.read(0, 1, None, ints([0, 0]), k=out, v=out.clone()), lambda: cache.write(0, k[:1], k[:1], one)):
+        with pytest.raises(pg.PgxGoError):
+            call()
+    assert torch.equal(cache.kv.view(torch.uint8), before)
