@@ -618,3 +618,27 @@ def test_lists_on_another_device_are_left_alone():
         with pytest.raises(pg.PgxGoError):
             call()
     assert torch.equal(cache.kv.view(torch.uint8), before)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,head_dim,most", [(150, 64, 5280), (150, 128, 4400), (100, 64, 9600), (520, 256, 2400), (150, 256, 4400)])
+def test_a_new_token_far_behind_the_first_tiles(n, head_dim, most, dtype):
+    """more than 32 tiles for a wavefront, four or two to a row, in one block or two: the last one's pages and scales are looked up after the token was written"""
+    lengths = [most - 1, most - 16, most - 17, most - 250, 4100 % most, 0, 1] + [0] * (n - 7)
+    g = torch.Generator("cuda").manual_seed(n)
+    a, b = (filled(lengths, 1, 2, head_dim, 16, dtype, seed=2, width=-(-most // 16), spare=2 * n) for _ in range(2))
+    ref = ref_of(a)
+    for step in range(2):
+        q = new(g, dtype, n, 4, head_dim)
+        k, v = ((torch.randn(n, 2, head_dim, generator=g, device="cuda") * (8.0 if step else 0.5)).to(dtype) for _ in range(2))
+        room = ints([1 if m + step < most else 0 for m in lengths])
+        for cache in (a, b):
+            cache.advance(counts=room)
+        ref.advance(range(n), room.tolist())
+        b.write(0, k, v)
+        got, want = a.attend(0, q, k=k, v=v, lse=True), b.attend(0, q, lse=True)
+        assert torch.equal(bits(got[0]), bits(want[0])) and torch.equal(bits(got[1]), bits(want[1]))
+        assert torch.equal(a.kv.view(torch.uint8), b.kv.view(torch.uint8)) and torch.equal(a.scales.view(torch.int32), b.scales.view(torch.int32))
+        ref.write_last(0, k, v, range(n))
+        assert torch.equal(codes_of(a), bytes_of(ref.kv))
+        check_attend(a, ref, got[0][:7], got[1][:7], 0, q[:7], range(7), head_dim ** -0.5)
