@@ -29,6 +29,7 @@
  *     code = to nearest, ties to even (x / s);  NaN where x is not finite
  * so a value is held to 2^-4 of itself, or of 2^-6 s where it is smaller.  A slot's tokens are written in their order: what a block holds behind the
  * tokens that a call writes is given up.  Scales in memory that the caller fills are finite and above 0; if one is no power of two, x / s may be rounded twice.
+ * A finite value near the type's end (float16: above 63488, bfloat16: above 2^127.95) may be held as a number beyond it; it is read back as the type's largest number.
  *
  * Lists of slots: slots_dev[n] int32, n <= slots, pairwise distinct; NULL: slots 0 .. n-1.  An entry of -1 is left out (as action
  * -1 in the environments), an entry outside [-1, slots) touches nothing.  status_dev (nullable, uint8 [n]): 0 done (or left out),
@@ -97,7 +98,7 @@ int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const in
 int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t tokens, const void* k_dev, int64_t k_entry_stride,
                    int64_t k_token_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride, int64_t v_token_stride, int64_t v_head_stride);
 
-/* Keys and values as they are held (a copy, or code * scale rounded to `type`): the tokens first_dev[i] (NULL: `first`), ... + tokens - 1 of each slot, in one layer, to
+/* Keys and values as they are held (a copy, or code * scale rounded to `type`, and no further than its largest number): the tokens first_dev[i] (NULL: `first`), ... + tokens - 1 of each slot, in one layer, to
  * element [i][t][head][.] at i * entry_stride + t * token_stride + head * head_stride; neither rows nor the two outputs may overlap.  Zeros where a slot has no such token, and
  * for an entry that is no slot.  Entries may repeat. */
 int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, const int32_t* first_dev, int32_t first, int32_t tokens, void* k_dev,
@@ -112,7 +113,9 @@ int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_d
  * ignored), so that a step takes one launch per layer; without them entries may repeat.  A slot without tokens, and an entry that is no slot, gives zeros and -infinity.
  * Scores, sums and the output before its rounding are held in 32 bits; probabilities are multiplied as two numbers of the
  * cache's type that add up to them within 2^-17 (float16: of the sum of 32 tokens' probabilities), however small they are.
- * With elements of 8 bits the probabilities, times the values' scales, are two bfloat16 numbers whatever `type` is.
+ * With elements of 8 bits the probabilities, times the values' scales, are two bfloat16 numbers whatever `type` is, and a float16 output between its largest number and
+ * 2^16 (1 + 2^-10) is that number: averages of held values may lie there.  Other outputs beyond the type's end are infinite.  Either way of holding sums up to 2^8 times a value for
+ * each token, in 32 bits: where bfloat16 values reach 2^119 over the number of tokens, the output may be infinite.
  * A key or value that is infinite or NaN makes what it counts for NaN; places behind a slot's last token may hold anything. */
 int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, int32_t heads, const void* q_dev, int64_t q_entry_stride,
                     int64_t q_head_stride, const void* k_dev, int64_t k_entry_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride,

@@ -103,6 +103,7 @@ typedef f32x4 f32x4_4 __attribute__((aligned(4)));
 struct F16 {
   typedef _Float16 elem;
   static constexpr bool kNarrow = true;
+  static constexpr float kLargest = 65504.0f;
   static constexpr float kRoom = 11.0f, kMost = 15.0f, kLeast = -3.0f, kDepth = 60.0f;
   typedef elem x8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -110,6 +111,7 @@ struct F16 {
 struct BF16 {
   typedef __bf16 elem;
   static constexpr bool kNarrow = false;
+  static constexpr float kLargest = 0x1.fep127f;
   static constexpr float kRoom = 0.0f, kMost = 8.0f, kLeast = 0.0f, kDepth = 0.0f;
   typedef elem x8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -143,9 +145,24 @@ struct Spot {
   bool alone;                        // the row's first wavefront has all of it
 };
 
+// Elements of the output before they are rounded.  Over 8 bits a float16 value above 63488 is held as 65536, so that averages of such values may lie beyond the type's end by what
+// held them and by the sums' errors, well below 2^-10; they become its largest number.  (One look for all of a wavefront's: two comparisons for each element take 0.2 us with 1024 rows.)
+template <class T, bool EIGHT, int N>
+__device__ __forceinline__ void within_type(float (&x)[N]) {
+  if constexpr (EIGHT && T::kNarrow) {
+    float most = 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) most = fmaxf(most, fabsf(x[e]));
+    if (__any(most > T::kLargest)) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = fabsf(x[e]) > T::kLargest && fabsf(x[e]) < 65536.0f * (1.0f + 0x1p-10f) ? copysignf(T::kLargest, x[e]) : x[e];
+    }
+  }
+}
+
 // The end of a row: the parts of W wavefronts, and of `active` blocks, are joined and written.  Lane 16 g + c has elements (4 g + r) D/16 + m of head c in
-// acc[m][r], relative to the exponent `top` (of powers of two), and the sum of its group's probabilities.
-template <class T, int NT, int W, bool SPLIT>
+// acc[m][r], relative to the exponent `top` (of powers of two), and the sum of its group's probabilities.  EIGHT: keys and values are held in 8 bits.
+template <class T, int NT, int W, bool SPLIT, bool EIGHT>
 __device__ __forceinline__ void finish_row(const AttendArgs& a, const Spot& at_spot, float top, float sum, f32x4 (&acc)[2 * NT]) {
   typedef typename T::x8 x8;
   constexpr int D = NT * 32, kOut = 8 * NT;   // elements of the output per lane
@@ -192,11 +209,15 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, const Spot& at_s
     if (col >= heads_here) return;
     const float inverse = 1.0f / sum;
     char* out = a.out + i * a.out_entry + (head0 + col) * a.out_head + g * kOut * 2;
+    float y[kOut];
+#pragma unroll
+    for (int e = 0; e < kOut; ++e) y[e] = acc[e % (2 * NT)][e / (2 * NT)] * inverse;
+    within_type<T, EIGHT>(y);
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       x8 x;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (typename T::elem)(acc[(u * 8 + e) % (2 * NT)][(u * 8 + e) / (2 * NT)] * inverse);
+      for (int e = 0; e < 8; ++e) x[e] = (typename T::elem)y[u * 8 + e];
       *(u32x4_2*)(out + u * 16) = __builtin_bit_cast(u32x4, x);
     }
     if (a.lse && g == 0) a.lse[(int64_t)i * a.heads + head0 + col] = (top + __log2f(sum)) * kLn2;
@@ -303,8 +324,10 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, const Spot& at_s
         fetch(e + kThreads, sharer);
       }
       typename T::elem* out = (typename T::elem*)(a.out + i * a.out_entry + (head0 + h) * a.out_head) + e * 4 % D;
+      float y[4] = {x[0], x[1], x[2], x[3]};
+      within_type<T, EIGHT>(y);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) out[k] = (typename T::elem)x[k];
+      for (int k = 0; k < 4; ++k) out[k] = (typename T::elem)y[k];
     }
   }
 }

@@ -772,7 +772,7 @@ __global__ void __launch_bounds__(64 * W, NT < 8 ? 2 : 1) attend_kernel(Cache c,
       compute(t0, number, outer);
     }
   }
-  finish_row<T, NT, W, (W >= 4)>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
+  finish_row<T, NT, W, (W >= 4), false>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
 }
 
 template <class T, int NT, int W>

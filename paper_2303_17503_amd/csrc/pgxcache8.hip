@@ -243,32 +243,47 @@ __global__ void __launch_bounds__(256) read_kernel(Cache c, int layer, int n, co
 #pragma unroll
   for (int j = 0; j < kTokensPerThread; ++j) {
     const int t = (int)(first + j0 + j);
-    data[j] = u32x4{0, 0, 0, 0};
     scale[j] = 0.0f;
+    if (EIGHT && c.is_page(page[j])) scale[j] = c.scales[scale_index(c, page[j], layer, (int)which) + (t >> kBlockShift & (c.page_blocks() - 1))];
+  }
+#pragma unroll
+  for (int j = 0; j < kTokensPerThread; ++j) {
+    const int t = (int)(first + j0 + j);
+    data[j] = u32x4{0, 0, 0, 0};
     if (!c.is_page(page[j])) continue;
     const char* source = from + page[j] * c.page_bytes(EIGHT ? 1 : 2) + (int64_t)(t & ((1 << c.page_shift) - 1)) * c.head_dim * (EIGHT ? 1 : 2);
     if (EIGHT) {
       const u32x2 w = *(const u32x2*)source;
       data[j][0] = w[0];
       data[j][1] = w[1];
-      scale[j] = c.scales[scale_index(c, page[j], layer, (int)which) + (t >> kBlockShift & (c.page_blocks() - 1))];
     } else {
       data[j] = *(const u32x4*)source;
     }
   }
+  // A code times its scale may lie beyond the type's end where the value that it stands for did not: then it is the largest number.  Scales are asked for first, so that one look at
+  // them chooses for the wavefront while the elements are on their way (1024 slots of 1 to 722 tokens 94.5 us; a look per token 98.5, comparing every element 102).
+  auto store = [&](auto within) __attribute__((always_inline)) {
 #pragma unroll
-  for (int j = 0; j < kTokensPerThread; ++j) {
-    if (j0 + j >= tokens) break;
-    if (EIGHT) {
-      float y[8];
-      decode(u32x2{data[j][0], data[j][1]}, y);
-      typename T::x8 h;
+    for (int j = 0; j < kTokensPerThread; ++j) {
+      if (j0 + j >= tokens) break;
+      u32x4 x = data[j];
+      if (EIGHT) {
+        float y[8];
+        decode(u32x2{data[j][0], data[j][1]}, y);
+        typename T::x8 h;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[e] = (typename T::elem)(y[e] * scale[j]);
-      data[j] = __builtin_bit_cast(u32x4, h);
+        for (int e = 0; e < 8; ++e) {
+          y[e] *= scale[j];
+          if (within.value) y[e] = y[e] > T::kLargest ? T::kLargest : y[e] < -T::kLargest ? -T::kLargest : y[e];   // (NaN stays)
+          h[e] = (typename T::elem)y[e];
+        }
+        x = __builtin_bit_cast(u32x4, h);
+      }
+      *(u32x4_2*)(p + (int64_t)(j0 + j) * to.token) = x;
     }
-    *(u32x4_2*)(p + (int64_t)(j0 + j) * to.token) = data[j];
-  }
+  };
+  if (EIGHT && __any(fmaxf(fmaxf(scale[0], scale[1]), fmaxf(scale[2], scale[3])) > T::kLargest / 448.0f)) store(std::true_type{});
+  else store(std::false_type{});
 }
 
 // ---- attention of one token per entry ----------------------------------------------------------------------------------------------------
@@ -582,7 +597,7 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
       }
     }
   }
-  finish_row<T, NT, W, SPLIT>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
+  finish_row<T, NT, W, SPLIT, true>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
 }
 
 template <class T, int NT, int W, int BUF, bool SPLIT>

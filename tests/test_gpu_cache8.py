@@ -642,3 +642,32 @@ def test_a_new_token_far_behind_the_first_tiles(n, head_dim, most, dtype):
         ref.write_last(0, k, v, range(n))
         assert torch.equal(codes_of(a), bytes_of(ref.kv))
         check_attend(a, ref, got[0][:7], got[1][:7], 0, q[:7], range(7), head_dim ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_finite_values_near_the_types_end_stay_finite(dtype):
+    """The code nearest to a value above 63488 (bfloat16: 2^127.95) at its scale is 256, beyond the type's largest number: what is read back is that number, 2^-4 of
+    the value away at most, and attention over float16's stays finite too, in the row of one wavefront, of several, and of several blocks.  Every block's scale s is the
+    one for the largest number, 448 s / 2 < most <= 448 s; values below 2^-6 s are held in steps of 2^-9 s, half a step 2^-10 s = 2^-4 2^-6 s."""
+    D, most, s = 64, torch.finfo(dtype).max, 2.0 ** (8 if dtype is torch.float16 else 120)
+    ends = [most, -most, most * 0.97, -most * 0.9698, most * 0.95, most / 2, 1.0]
+    x = torch.tensor(ends, dtype=torch.float64).repeat(-(-D * 5 // len(ends)))[: D * 5].reshape(5, 1, D).to(dtype).cuda()      # every end in every token
+    cache = pg.PagedCache.empty(5, 10, 32, 1, 1, D, dtype=dtype, bits=8)
+    x[1, 0, 3], x[2, 0, 5] = float("nan"), float("-inf")
+    odd = ~torch.isfinite(x)
+    cache.advance()
+    cache.write(0, x, x)
+    for held in cache.read(0, 1):
+        assert torch.equal(torch.isnan(held[:, 0]), odd)
+        held, want = held[:, 0][~odd].double(), x[~odd].double()
+        assert torch.isfinite(held).all() and ((held - want).abs() <= 2.0 ** -4 * want.abs().clamp(min=s / 64)).all()
+    if dtype is torch.float16:   # (sums of the largest bfloat16 numbers go beyond 32 bits)
+        for tokens, pages in ((1, 1), (16, 1), (300, 19), (2100, 132)):
+            cache = pg.PagedCache.empty(2, 2 * pages, pages * 16, 1, 1, D, dtype=dtype, bits=8)
+            cache.advance(counts=tokens)
+            loud = torch.full((2, tokens, 1, D), most, dtype=dtype, device="cuda")
+            loud[1, :, 0, 1::2], loud[1, :, 0, ::4] = -most, 63500.0
+            cache.write(0, torch.zeros_like(loud), loud)
+            out = cache.attend(0, torch.ones(2, 3, D, dtype=dtype, device="cuda")).double()
+            want = loud[:, 0].double()                                   # (all tokens are alike)
+            assert torch.isfinite(out).all() and ((out - want).abs() <= 2.0 ** -4 * want.abs()).all(), tokens
