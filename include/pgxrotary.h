@@ -16,7 +16,7 @@ extern "C" {
 #endif
 
 #define PGXROTARY_OK 0
-#define PGXROTARY_EINVAL (-1) /* null or misaligned pointer, size out of range, unknown type, output rows that overlap */
+#define PGXROTARY_EINVAL (-1) /* null or misaligned pointer, size out of range, unknown type, output rows that overlap each other or other tensors' rows */
 #define PGXROTARY_EHIP (-2)   /* a HIP runtime call failed; see pgxrotary_last_hip_error() */
 
 #define PGXROTARY_F32 0
@@ -27,7 +27,8 @@ extern "C" {
 #define PGXROTARY_MAX_PARTS 2
 
 /* One tensor, such as the queries or the keys: element [i][t][head][.] at i * entry_stride + t * token_stride + head * head_stride, in elements.
- * out_dev may be in_dev with the same strides; otherwise they do not overlap.  Rows of the output may not overlap each other. */
+ * out_dev may be in_dev with the same strides.  Otherwise no output shares memory with an input or an output of either tensor (rows that lie between each other's, as views of one
+ * product do, are apart), and rows of an output may not overlap each other: such calls are refused. */
 typedef struct {
   const void* in_dev;
   int64_t in_entry_stride, in_token_stride, in_head_stride;

@@ -231,12 +231,18 @@ int pgxrotary_turn(int32_t entries, int32_t tokens, int32_t head_dim, int32_t ro
     if (!p.in_dev || !p.out_dev || (either & (type == PGXROTARY_F32 ? 3u : 1u)) != 0 || !rows_apart(sizes, out, head_dim)) return PGXROTARY_EINVAL;
     const bool same = p.in_dev == p.out_dev && (entries == 1 || p.in_entry_stride == p.out_entry_stride) && (tokens == 1 || p.in_token_stride == p.out_token_stride) &&
                       (p.heads == 1 || p.in_head_stride == p.out_head_stride);
-    if (p.in_dev == p.out_dev && !same) return PGXROTARY_EINVAL;
     in_place = in_place && same;
     any_in_place = any_in_place || same;
+    // Wavefronts store rows while others have yet to load theirs: beside an output that is its own input, no output may share memory with an input or another output.
+    const int64_t bytes = type == PGXROTARY_F32 ? 4 : 2;
+    const Rows output = {p.out_dev, {entries, tokens, p.heads}, {out[0], out[1], out[2]}};
+    for (int j = 0; j < parts; ++j) {
+      const pgxrotary_part& o = part[j];
+      if (!(j == k && same) && rows_meet(Rows{o.in_dev, {entries, tokens, o.heads}, {o.in_entry_stride, o.in_token_stride, o.in_head_stride}}, output, head_dim, bytes)) return PGXROTARY_EINVAL;
+      if (j > k && rows_meet(Rows{o.out_dev, {entries, tokens, o.heads}, {o.out_entry_stride, o.out_token_stride, o.out_head_stride}}, output, head_dim, bytes)) return PGXROTARY_EINVAL;
+    }
   }
   if (total == 0 || a.heads == 0) return PGXROTARY_OK;
-  if (parts == 2 && part[0].heads > 0 && part[1].heads > 0 && part[0].out_dev == part[1].out_dev) return PGXROTARY_EINVAL;   // one tensor given twice
   if (!positions_dev || !frequencies_dev || ((uintptr_t)positions_dev & 3u) != 0 || ((uintptr_t)frequencies_dev & 7u) != 0) return PGXROTARY_EINVAL;
   a.positions = positions_dev; a.positions_entry = positions_entry_stride; a.positions_token = positions_token_stride;
   a.frequencies = frequencies_dev; a.magnitude = magnitude; a.inverse = inverse;

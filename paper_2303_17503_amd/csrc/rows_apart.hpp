@@ -1,4 +1,4 @@
-// rows_apart.hpp -- whether an output's rows overlap, looked at before a launch.
+// rows_apart.hpp -- whether the rows of outputs overlap, each other or those of another tensor, looked at before a launch.
 #ifndef ROWS_APART_HPP_
 #define ROWS_APART_HPP_
 
@@ -20,5 +20,66 @@ inline bool rows_apart(const int64_t (&sizes)[3], const int64_t (&strides)[3], i
   }
   return true;
 }
+
+struct Rows {   // of one tensor: row [i][t][h] at element i * strides[0] + t * strides[1] + h * strides[2]
+  const void* p;
+  int64_t sizes[3], strides[3];
+};
+
+// Whether a row of a and one of b, each of `row` elements of `bytes` bytes, share memory.  Two rows do if their distance, the bases' and a sum of whole multiples of the strides, is
+// below a row.  Equal strides of the two count as one, over the differences of their indexes; then the largest stride's multiples that the others can still
+// make up for are tried, in nested layouts one or two.  Layouts that need more than 2^14 trials (two sets of strides that do not nest, in the same memory) are taken to overlap.
+class RowsMeet {
+  struct Dim { __int128 stride, lo, hi; };   // multiples lo .. hi
+  Dim dims_[6];
+  __int128 least_[7], most_[7];              // what the dimensions from here on can add
+  int n_ = 0, trials_ = 0;
+  __int128 row_;
+
+  static __int128 floor_div(__int128 a, __int128 b) { return a / b - (a % b < 0); }   // b > 0
+  void add(int64_t stride, int64_t size, bool negative) {
+    if (size <= 1 || stride == 0) return;
+    if (stride < 0) negative = !negative;
+    const __int128 s = stride < 0 ? -(__int128)stride : (__int128)stride, most = size - 1;
+    int k = 0;
+    while (k < n_ && dims_[k].stride > s) ++k;
+    if (k == n_ || dims_[k].stride != s) {
+      for (int m = n_++; m > k; --m) dims_[m] = dims_[m - 1];
+      dims_[k] = Dim{s, 0, 0};
+    }
+    if (negative) dims_[k].lo -= most;
+    else dims_[k].hi += most;
+  }
+  bool reach(int k, __int128 at) {   // whether the dimensions from k on bring `at` to within a row of 0
+    if (k == n_) return at < row_ && -at < row_;
+    const Dim& d = dims_[k];
+    __int128 lo = -floor_div(row_ - 1 + most_[k + 1] + at, d.stride), hi = floor_div(row_ - 1 - least_[k + 1] - at, d.stride);
+    lo = lo < d.lo ? d.lo : lo;
+    hi = hi > d.hi ? d.hi : hi;
+    for (; lo <= hi; ++lo) {
+      if (k + 1 == n_ || ++trials_ > 1 << 14 || reach(k + 1, at + lo * d.stride)) return true;
+    }
+    return false;
+  }
+
+ public:
+  bool operator()(const Rows& a, const Rows& b, int64_t row, int64_t bytes) {
+    n_ = trials_ = 0;
+    row_ = (__int128)row * bytes;
+    for (int k = 0; k < 3; ++k) {
+      if (a.sizes[k] <= 0 || b.sizes[k] <= 0) return false;
+      add(a.strides[k], a.sizes[k], true);
+      add(b.strides[k], b.sizes[k], false);
+    }
+    least_[n_] = most_[n_] = 0;
+    for (int k = n_; k-- > 0;) {
+      dims_[k].stride *= bytes;
+      least_[k] = least_[k + 1] + dims_[k].lo * dims_[k].stride;
+      most_[k] = most_[k + 1] + dims_[k].hi * dims_[k].stride;
+    }
+    return reach(0, (__int128)(intptr_t)b.p - (__int128)(intptr_t)a.p);
+  }
+};
+inline bool rows_meet(const Rows& a, const Rows& b, int64_t row, int64_t bytes) { return RowsMeet()(a, b, row, bytes); }
 
 #endif  // ROWS_APART_HPP_

@@ -253,3 +253,62 @@ def test_native_and_python_checks_make_the_same_calls(monkeypatch):
     monkeypatch.setattr(pg.rotary_binding, "_fast", None)
     for a, b in zip(native, history()):
         assert torch.equal(a, b)
+
+
+SHARED = [
+    ("two tensors exchanged", lambda a, b: dict(x=(a, b), out=(b, a))), ("one output is the other's input", lambda a, b: dict(x=(a, b), out=(b, zeros(4, 2, 16)))),
+    ("an input that both read, in place", lambda a, b: dict(x=(a, a), out=(a, b))),
+    ("outputs that share a row", lambda a, b: (lambda t: dict(x=(a, b), out=(t[:, :2], t[:, 1:])))(zeros(4, 3, 16))),
+    ("an output that begins inside its input", lambda a, b: (lambda t: dict(x=t[:, :2], out=t[:, 1:]))(zeros(4, 3, 16))),
+    ("an element apart", lambda a, b: (lambda t: dict(x=t[..., :16], out=t[..., 1:]))(zeros(4, 2, 17))),
+    ("the same rows in another order", lambda a, b: dict(x=a, out=a.view(2, 4, 16).transpose(0, 1))),
+    ("an input whose rows repeat", lambda a, b: dict(x=a[:1].expand(4, 2, 16), out=a)),
+]
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("what", [n for n, _ in SHARED])
+def test_outputs_that_share_memory_with_other_tensors(what, native, monkeypatch):
+    call()
+    if not native:
+        monkeypatch.setattr(pg.rotary_binding, "_fast", None)
+    a, b = torch.randn(4, 2, 16, device="cuda"), torch.randn(4, 2, 16, device="cuda")
+    before = a.clone(), b.clone()
+    with pytest.raises(pg.PgxGoError):
+        call(**dict(SHARED)[what](a, b))
+    assert torch.equal(a, before[0]) and torch.equal(b, before[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_between_each_others(dtype):
+    """tensors of one allocation whose rows interleave: queries and keys turned into the place of other columns, heads in turn, tokens in turn, one of the pair in place"""
+    g = torch.Generator("cuda").manual_seed(5)
+    n, T, D = 3, 7, 24
+    positions, f = whole(g, 0, 5000, n, T), pg.rotary_frequencies(D)
+    q, k = (torch.randn(n, T, h, D, generator=g, device="cuda").to(dtype) for h in (4, 2))
+    want = pg.rotate((q, k), positions, f)
+    check(want[0], q, positions, f, False, 1.0, False)
+    check(want[1], k, positions, f, False, 1.0, False)
+
+    def same(x, out):
+        x[0].copy_(q)
+        x[1].copy_(k)
+        rest = [t for t in x if not any(t is o for o in out)]
+        kept = [t.clone() for t in rest]
+        got = pg.rotate(x, positions, f, out=out)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and all(torch.equal(t, c) for t, c in zip(rest, kept))
+
+    memory = torch.zeros(n, T, 12, D, dtype=dtype, device="cuda")
+    a, b, c, d = memory[:, :, :4], memory[:, :, 4:6], memory[:, :, 6:10], memory[:, :, 10:]
+    same((a, b), (c, d))
+    same((a, b), (a, d))
+    same((a, b), (c, b))
+    same((a, b), (a, b))
+    a, c, b = memory[:, :, 0:8:2], memory[:, :, 1:8:2], memory[:, :, 8:10]              # heads in turn
+    same((a, b), (c, b))
+    memory = torch.zeros(n, 4 * T, 4, D, dtype=dtype, device="cuda")
+    a, b, c, d = (memory[:, i::4] for i in range(4))                                    # tokens in turn
+    same((a, b[:, :, :2]), (c, d[:, :, 2:]))
+    memory = torch.zeros(12, T, n, D, dtype=dtype, device="cuda")                       # heads before tokens before entries
+    a, b, c, d = (memory[i:j].permute(2, 1, 0, 3) for i, j in ((0, 4), (4, 6), (6, 10), (10, 12)))
+    same((a, b), (c, d))

@@ -1,6 +1,8 @@
 """CPU-only checks of the rotary positions' boundary: exported symbols, refused arguments, frequencies, and the plain form's own gradient."""
 import ctypes as C
 import math
+import os
+import subprocess
 
 import pytest
 import torch
@@ -77,3 +79,86 @@ def test_the_plain_form_turns_back_and_is_its_own_gradient(interleaved):
     q, k = torch.randn(2, 1, 1, 10, generator=g, dtype=torch.float64)
     at = lambda v, n: turned(v, torch.tensor([n]), f, interleaved)  # noqa: E731
     assert torch.allclose((at(q, 50) * at(k, 43)).sum(), (at(q, 1007) * at(k, 1000)).sum())
+
+
+def test_outputs_that_share_memory_with_other_tensors():
+    """each refused before anything is launched"""
+    L, P, base = rotary_binding.lib(), rotary_binding._Part, 1 << 20
+    row, size = 64 * 4, 2 * 3 * 2 * 64 * 4            # bytes of a row and of a whole tensor [2][3][2][64]
+
+    def call(*parts):
+        array = (P * 2)(*[P(i, *a, o, *b, h) for i, a, o, b, h in parts])
+        return L.pgxrotary_turn(2, 3, 64, 64, 0, 4096, 3, 1, 4096, 1.0, 0, 0, len(parts), array, None)
+
+    dense, a, b, far, more = (384, 128, 64), base, base + size, base + 8 * size, base + 12 * size
+    wide = (3 * 2 * 128, 2 * 128, 128)                # rows with as much room behind each
+    for bad in ([(a, dense, b, dense, 2), (b, dense, a, dense, 2)],                        # two tensors exchanged
+                [(a, dense, b, dense, 2), (b, dense, far, dense, 2)],                      # one's output is the other's input
+                [(a, dense, far, dense, 2), (b, dense, a, dense, 2)],
+                [(a, dense, far, dense, 2), (b, dense, far, dense, 2)],                    # one output twice
+                [(a, dense, far, dense, 2), (b, dense, far + size - row, dense, 2)],       # outputs that share a row
+                [(a, dense, far, dense, 2), (b, dense, far + size - 4, dense, 2)],         # or an element
+                [(a, dense, far, dense, 2), (b, dense, a + row, dense, 1)],
+                [(a, dense, a + row, dense, 2)], [(a, dense, a + 4, dense, 2)], [(a, dense, a - size + 4, dense, 2)],      # an output that begins inside its own input
+                [(a, dense, a, (384, 64, 192), 2)],                                        # or is it in another order
+                [(a, wide, a + 32 * 4, wide, 2)],                                          # between the rows, but for half of them
+                [(a, (0, 0, 0), a, dense, 2)],                                             # over an input whose rows repeat
+                [(a, dense, far, dense, 2), (a, dense, a, dense, 2)]):                     # an input that both read, in place
+        assert call(*bad) == -1, bad
+    assert call((a, dense, far, dense, 0), (b, dense, far, dense, 0)) == 0                 # nothing in either
+
+
+PROGRAM = r"""
+#include <cstdio>
+#include <vector>
+#include "rows_apart.hpp"
+static uint32_t x = 1;
+static int below(int n) { x = x * 1664525u + 1013904223u; return (int)((x >> 8) % (uint32_t)n); }
+static void rows(const Rows& r, int64_t row, std::vector<char>& at, int bit, bool& meets) {
+  for (int64_t i = 0; i < r.sizes[0]; ++i)
+    for (int64_t t = 0; t < r.sizes[1]; ++t)
+      for (int64_t h = 0; h < r.sizes[2]; ++h)
+        for (int64_t e = 0; e < row; ++e) {
+          char& c = at[(size_t)(((intptr_t)r.p >> 1) + i * r.strides[0] + t * r.strides[1] + h * r.strides[2] + e)];
+          if (c & ~bit) meets = true;
+          c |= (char)bit;
+        }
+}
+int main() {
+  int wrong = 0, meeting = 0, looked = 400000;
+  std::vector<char> at(16384);
+  for (int k = 0; k < looked; ++k) {
+    const int row = 1 + below(5);
+    Rows r[2];
+    const bool alike = below(2);     // the same strides but for some
+    for (int j = 0; j < 2; ++j) {
+      r[j].p = (const void*)(intptr_t)(2 * (8000 + below(below(3) ? 40 : 300)));
+      for (int d = 0; d < 3; ++d) {
+        r[j].sizes[d] = below(20) ? 1 + below(4) : 0;
+        r[j].strides[d] = j && alike && below(8) ? r[0].strides[d] : below(4) ? below(41) - 10 : below(301) - 150;
+      }
+    }
+    std::fill(at.begin(), at.end(), 0);
+    bool before = false, meets = false;
+    rows(r[0], row, at, 1, before);
+    rows(r[1], row, at, 2, meets);
+    wrong += rows_meet(r[0], r[1], row, 2) != meets || rows_meet(r[1], r[0], row, 2) != meets;
+    meeting += meets;
+  }
+  // sizes that outgrow 64 bits as bytes, and layouts that do not nest
+  const int64_t big = (int64_t)1 << 62;
+  wrong += rows_meet(Rows{(void*)4096, {1 << 30, 1, 1}, {big, 1, 1}}, Rows{(void*)(4096 + 64), {1 << 30, 1, 1}, {big, 1, 1}}, 32, 2);
+  wrong += !rows_meet(Rows{(void*)4096, {1 << 30, 1, 1}, {big, 1, 1}}, Rows{(void*)(4096 + 62), {1 << 30, 1, 1}, {big, 1, 1}}, 32, 2);
+  wrong += !rows_meet(Rows{(void*)4096, {1 << 20, 1 << 20, 1}, {1000003, 1009, 1}}, Rows{(void*)5001, {1 << 20, 1 << 20, 1}, {1000033, 1013, 1}}, 1, 2);
+  printf("%d wrong of %d, %d meeting\n", wrong, looked, meeting);
+  return wrong != 0 || meeting < looked / 10 || meeting > looked - looked / 10;
+}
+"""
+
+
+def test_whether_rows_meet_against_every_element(tmp_path):
+    src, exe = tmp_path / "meet.cpp", tmp_path / "meet"
+    src.write_text(PROGRAM)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(os.path.dirname(rotary_binding.__file__), "csrc"), "-o", str(exe), str(src)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.startswith("0 wrong of "), r.stdout
