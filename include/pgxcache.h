@@ -99,7 +99,7 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
                    int64_t k_token_stride, int64_t k_head_stride, const void* v_dev, int64_t v_entry_stride, int64_t v_token_stride, int64_t v_head_stride);
 
 /* Keys and values as they are held (a copy, or code * scale rounded to `type`, and no further than its largest number): the tokens first_dev[i] (NULL: `first`), ... + tokens - 1 of each slot, in one layer, to
- * element [i][t][head][.] at i * entry_stride + t * token_stride + head * head_stride; neither rows nor the two outputs may overlap.  Zeros where a slot has no such token, and
+ * element [i][t][head][.] at i * entry_stride + t * token_stride + head * head_stride; neither rows nor the two outputs may overlap (rows of the one between those of the other are apart): such calls are refused.  Zeros where a slot has no such token, and
  * for an entry that is no slot.  Entries may repeat. */
 int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_dev, const int32_t* first_dev, int32_t first, int32_t tokens, void* k_dev,
                   int64_t k_entry_stride, int64_t k_token_stride, int64_t k_head_stride, void* v_dev, int64_t v_entry_stride, int64_t v_token_stride, int64_t v_head_stride);

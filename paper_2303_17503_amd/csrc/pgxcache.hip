@@ -985,7 +985,8 @@ int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_d
   if (n == 0 || tokens == 0) return PGXCACHE_OK;
   if (!k_dev || !v_dev || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 1u) != 0) return PGXCACHE_EINVAL;
   const int64_t sizes[3] = {n, tokens, h->o.kv_heads}, ks[3] = {k_entry_stride, k_token_stride, k_head_stride}, vs[3] = {v_entry_stride, v_token_stride, v_head_stride};
-  if (k_dev == v_dev || !rows_apart(sizes, ks, h->o.head_dim) || !rows_apart(sizes, vs, h->o.head_dim)) return PGXCACHE_EINVAL;
+  if (!rows_apart(sizes, ks, h->o.head_dim) || !rows_apart(sizes, vs, h->o.head_dim)) return PGXCACHE_EINVAL;
+  if (rows_meet(Rows{k_dev, {sizes[0], sizes[1], sizes[2]}, {ks[0], ks[1], ks[2]}}, Rows{v_dev, {sizes[0], sizes[1], sizes[2]}, {vs[0], vs[1], vs[2]}}, h->o.head_dim, 2)) return PGXCACHE_EINVAL;
   const Cache c = cache_of(h);
   if (read_blocks(c, n, tokens) > 0x7FFFFFFF) return PGXCACHE_EINVAL;
   const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};

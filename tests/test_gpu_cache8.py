@@ -671,3 +671,25 @@ def test_finite_values_near_the_types_end_stay_finite(dtype):
             out = cache.attend(0, torch.ones(2, 3, D, dtype=dtype, device="cuda")).double()
             want = loud[:, 0].double()                                   # (all tokens are alike)
             assert torch.isfinite(out).all() and ((out - want).abs() <= 2.0 ** -4 * want.abs()).all(), tokens
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("bits_", [8, 16])
+def test_keys_and_values_read_into_memory_that_they_share(bits_, native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(pg.cache_binding, "_fast", None)
+    cache = pg.PagedCache.empty(2, 6, 48, 1, 2, 64, bits=bits_)
+    g = torch.Generator("cuda").manual_seed(1)
+    k, v = new(g, torch.bfloat16, 2, 40, 2, 64), new(g, torch.bfloat16, 2, 40, 2, 64)
+    cache.advance(counts=40)
+    cache.write(0, k, v)
+    want = cache.read(0, 5, first=30)
+    memory = torch.zeros(2, 11, 5, 64, dtype=torch.bfloat16, device="cuda")
+    for a, b in ((memory[:, :5, :2], memory[:, 4:9, :2]), (memory[:, :5, :2], memory[:, :5, 1:3]), (memory[:, 0:10:2, :2], memory[:, 2:11:2, :2][:, :5]),
+                 (memory[:1].expand(2, 11, 5, 64)[:, :5, :2], memory[:, 6:, :2]), (memory.flatten()[:1280].view(2, 5, 2, 64), memory.flatten()[1279:2559].view(2, 5, 2, 64))):
+        with pytest.raises(pg.PgxGoError):
+            cache.read(0, 5, first=30, k=a, v=b)
+    assert (memory == 0).all()
+    for a, b in ((memory[:, :5, :2], memory[:, :5, 2:4]), (memory[:, 0:10:2, :2], memory[:, 1:11:2, :2]), (memory[:, :5, 0:4:2], memory[:, :5, 1:4:2])):   # rows between each other's
+        got = cache.read(0, 5, first=30, k=a, v=b)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
