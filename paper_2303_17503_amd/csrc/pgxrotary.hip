@@ -189,7 +189,7 @@ hipError_t launch(Args& a, int32_t entries, bool interleaved, hipStream_t stream
   tokens = tokens < room ? tokens : room;
   if (tokens < 1) tokens = 1;
   a.entry_blocks = (int32_t)((a.tokens + tokens - 1) / tokens);
-  a.block_tokens = (a.tokens + a.entry_blocks - 1) / a.entry_blocks;
+  a.block_tokens = (int32_t)(((int64_t)a.tokens + a.entry_blocks - 1) / a.entry_blocks);
   if ((int64_t)entries * a.entry_blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   const int threads = a.chunks <= 64 && a.block_tokens * per_token <= 128 ? 64 : 256;
   a.entries = entries;

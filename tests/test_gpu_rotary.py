@@ -312,3 +312,17 @@ def test_rows_between_each_others(dtype):
     memory = torch.zeros(12, T, n, D, dtype=dtype, device="cuda")                       # heads before tokens before entries
     a, b, c, d = (memory[i:j].permute(2, 1, 0, 3) for i, j in ((0, 4), (4, 6), (6, 10), (10, 12)))
     same((a, b), (c, d))
+
+
+def test_as_many_tokens_as_a_call_takes():
+    """2^31 - 1 tokens, counted in 32 bits, whose number and that of their blocks add up to more: every row of one position, and the last ones of others"""
+    n = 2 ** 31 - 1
+    x = torch.empty(n, 1, 2, dtype=torch.bfloat16, device="cuda")
+    x[..., 0], x[..., 1] = 1.0, -2.0
+    f = pg.rotary_frequencies(2)
+    want = pg.rotate(x[:5].clone(), torch.full((5,), 3, dtype=torch.int32, device="cuda"), f)
+    pg.rotate(x, torch.full((1,), 3, dtype=torch.int32, device="cuda").expand(n), f, out=x)
+    pair = want[0].view(torch.int32)
+    assert all((part == pair).all() for part in x.view(torch.int32).flatten().split(2 ** 28))
+    with pytest.raises(pg.PgxGoError):
+        pg.rotate(x[:1].expand(2 ** 31, 1, 2), torch.zeros(1, dtype=torch.int32, device="cuda").expand(2 ** 31), f, out=x)
