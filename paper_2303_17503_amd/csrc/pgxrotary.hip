@@ -11,6 +11,8 @@
 #include <stdint.h>
 #include <stdlib.h>
 
+#include <utility>
+
 #include "pgxrotary.h"
 #include "rows_apart.hpp"
 
@@ -190,8 +192,8 @@ hipError_t launch(Args& a, int32_t entries, bool interleaved, hipStream_t stream
   if (tokens < 1) tokens = 1;
   a.entry_blocks = (int32_t)((a.tokens + tokens - 1) / tokens);
   a.block_tokens = (int32_t)(((int64_t)a.tokens + a.entry_blocks - 1) / a.entry_blocks);
-  if ((int64_t)entries * a.entry_blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   const int threads = a.chunks <= 64 && a.block_tokens * per_token <= 128 ? 64 : 256;
+  if ((int64_t)entries * a.entry_blocks * threads >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;   // (a launch of so many threads runs what is left of them beyond 2^32, without an error)
   a.entries = entries;
   a.per_wave = a.chunks <= 64 ? 64 / a.chunks : 0;
   a.lanes = a.chunks <= 64 ? threads / 64 * a.per_wave : threads / a.chunks;
@@ -265,9 +267,17 @@ int pgxrotary_turn(int32_t entries, int32_t tokens, int32_t head_dim, int32_t ro
   if (follow) {
     a.tokens = (int32_t)total;
     entries = 1;
+  } else if (entries > tokens && entries >= 1 << 24) {   // more entries than a launch has blocks: tokens of one place are the entries then
+    std::swap(entries, a.tokens);
+    std::swap(a.positions_entry, a.positions_token);
+    for (pgxrotary_part& p : a.part) {
+      std::swap(p.in_entry_stride, p.in_token_stride);
+      std::swap(p.out_entry_stride, p.out_token_stride);
+    }
   }
   const hipStream_t s = (hipStream_t)stream;
   const hipError_t e = type == PGXROTARY_F32 ? launch<F32>(a, entries, interleaved != 0, s) : type == PGXROTARY_F16 ? launch<Half<_Float16>>(a, entries, interleaved != 0, s) : launch<Half<__bf16>>(a, entries, interleaved != 0, s);
+  if (e == hipErrorInvalidConfiguration) return PGXROTARY_EINVAL;
   if (e != hipSuccess) {
     g_last_hip = (int)e;
     return PGXROTARY_EHIP;

@@ -326,3 +326,17 @@ def test_as_many_tokens_as_a_call_takes():
     assert all((part == pair).all() for part in x.view(torch.int32).flatten().split(2 ** 28))
     with pytest.raises(pg.PgxGoError):
         pg.rotate(x[:1].expand(2 ** 31, 1, 2), torch.zeros(1, dtype=torch.int32, device="cuda").expand(2 ** 31), f, out=x)
+
+
+def test_more_entries_than_a_launch_has_blocks():
+    """2^26 + 5 entries of two tokens that lie tokens first, so that no entry follows another: 64 threads for each would be more than a launch takes"""
+    n = 2 ** 26 + 5
+    x = torch.zeros(2, n, 1, 2, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    x[:, 0, :, 0], x[:, 1, :, 1] = 1.0, 3.0
+    positions = torch.arange(n, dtype=torch.int32, device="cuda").remainder_(1000)[:, None].expand(n, 2) * torch.tensor([1, 7], dtype=torch.int32, device="cuda")
+    f = pg.rotary_frequencies(2)
+    got = pg.rotate(x, positions, f)
+    want = pg.rotate(x[:1000].contiguous(), positions[:1000].contiguous(), f)
+    check(want, x[:1000], positions[:1000], f, False, 1.0, False)
+    full = n // 1000 * 1000
+    assert (got[:full].view(-1, 1000, 2, 1, 2) == want).all() and torch.equal(got[full:], want[: n - full])
