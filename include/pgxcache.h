@@ -17,7 +17,8 @@
  * The calls read table, lengths and refs as they find them; a page number outside the pool is never followed.
  *
  * Conventions are those of pgxgo.h: asynchronous on the stream given at the beginning, no allocation, no synchronisation,
- * negative codes, nothing throws or aborts.  One handle's calls share work_dev and belong on one stream.
+ * negative codes, nothing throws or aborts.  One handle's calls share work_dev and belong on one stream.  A call that would need 2^32 threads (attend: 2^24 entries times key
+ * heads where slots can be long, read and write: a thread for 8 elements of 4 tokens or fewer, fork: 2^24 entries, free: 2^26) is refused and does nothing: it can be made in parts.
  *
  * Held in 8 bits (pgxcache_init_e4m3): kv_dev has elements of 8 bits in the same order, e4m3 codes (4 bits of exponent, 3 of fraction, up to
  * 448, no infinities).  An element is its code times the scale of its block: 16 tokens of a slot, from a multiple of 16 on, in one layer and head, keys or values.

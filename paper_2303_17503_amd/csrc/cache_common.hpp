@@ -133,6 +133,9 @@ __device__ __forceinline__ float across_groups_sum(float x) {
 constexpr int kAcrossDies = 16;             // cache policy of a buffer instruction: as an atomic access of the whole device (sc1)
 constexpr int kBufferFlags = 0x00027000;    // raw buffer of 32-bit words
 
+// A launch of 2^32 threads or more runs what is left of them beyond 2^32 and reports no error: calls that would need one are refused.
+inline bool launchable(int64_t blocks, int threads) { return blocks * threads < (int64_t)1 << 32; }
+
 template <bool STREAM, class V>
 __device__ __forceinline__ V read_once(const V* p) { return STREAM ? __builtin_nontemporal_load(p) : *p; }
 
@@ -336,6 +339,7 @@ __device__ __forceinline__ void finish_row(const AttendArgs& a, const Spot& at_s
 int64_t write8_blocks(const Cache& c, int n, int tokens);
 // last_only: the one token given is the slots' last, not the first of those that the last advance made room for
 hipError_t write8(const Cache& c, bool f16, int layer, int n, const int32_t* slots, int tokens, int last_only, const Tokens& k, const Tokens& v, hipStream_t stream);
+bool attend8_fits(const Cache& c, const AttendArgs& a);   // into a launch
 hipError_t attend8(const Cache& c, bool f16, const AttendArgs& a, hipStream_t stream);
 int64_t read_blocks(const Cache& c, int n, int tokens);
 hipError_t read_back(const Cache& c, bool f16, int layer, int n, const int32_t* slots, const int32_t* firsts, int first, int tokens, const Tokens& k, const Tokens& v,

@@ -783,6 +783,7 @@ hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t rows, h
   // streamed, and take 42 us instead of 34.
   const bool streamed = (int64_t)c.pages * c.page_bytes() > (int64_t)256 << 20;
   const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = a.splits > 1 ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
+  if (!launchable(rows * a.splits, 64 * W)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)(rows * a.splits)), block(64 * W);
   if (streamed) hipLaunchKernelGGL((attend_kernel<T, NT, W, true>), grid, block, join > weights ? join : weights, stream, c, a);
   else hipLaunchKernelGGL((attend_kernel<T, NT, W, false>), grid, block, join > weights ? join : weights, stream, c, a);
@@ -922,10 +923,10 @@ int pgxcache_advance(pgxcache_t h, int32_t n, const int32_t* slots_dev, const in
     HIPCHK(hipGetLastError());
     return PGXCACHE_OK;
   }
-  hipLaunchKernelGGL((advance_kernel<1, false>), dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
+  hipLaunchKernelGGL((advance_kernel<1, false>), dim3(((unsigned)n + kOneBlock - 1) / kOneBlock), dim3(kOneBlock), 0, stream, c, n, slots_dev, counts_dev, count, h->plan, status_dev);
   HIPCHK(hipGetLastError());
   const int words = (c.pages + 63) / 64, threads = n > words ? n : words;
-  hipLaunchKernelGGL(advance_apply_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, c, n, slots_dev, counts_dev, count, h->plan);
+  hipLaunchKernelGGL(advance_apply_kernel, dim3(((unsigned)threads + 255) / 256), dim3(256), 0, stream, c, n, slots_dev, counts_dev, count, h->plan);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
@@ -938,7 +939,7 @@ int pgxcache_write(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_
   const int64_t runs = ((int64_t)tokens + kTokensPerThread - 1) / kTokensPerThread;
   const Cache c = cache_of(h);
   const int64_t blocks = c.scales ? write8_blocks(c, n, tokens) : ((int64_t)n * runs * 2 * h->o.kv_heads * (h->o.head_dim / 8) + 255) / 256;
-  if (blocks > 0x7FFFFFFF) return PGXCACHE_EINVAL;
+  if (!launchable(blocks, 256)) return PGXCACHE_EINVAL;
   const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};
   if (c.scales) {
     HIPCHK(write8(c, h->o.type == PGXCACHE_F16, layer, n, slots_dev, tokens, 0, k, v, (hipStream_t)h->o.stream));
@@ -967,6 +968,7 @@ int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots
   if ((int64_t)n * h->o.kv_heads * a.head_tiles > 0x7FFFFFFF) return PGXCACHE_EINVAL;
   const Cache c = cache_of(h);
   if (c.scales) {
+    if (!attend8_fits(c, a)) return PGXCACHE_EINVAL;
     if (a.k && a.head_tiles > 1) {   // several blocks read the new token's block: it is written before, since rounding a block again is not the same twice
       const Tokens k = {a.k, a.k_entry, 0, a.k_head}, v = {a.v, a.v_entry, 0, a.v_head};
       HIPCHK(write8(c, h->o.type == PGXCACHE_F16, layer, n, slots_dev, 1, 1, k, v, (hipStream_t)h->o.stream));
@@ -975,7 +977,9 @@ int pgxcache_attend(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots
     HIPCHK(attend8(c, h->o.type == PGXCACHE_F16, a, (hipStream_t)h->o.stream));
     return PGXCACHE_OK;
   }
-  HIPCHK(h->o.type == PGXCACHE_F16 ? launch_attend_for<F16>(c, a, (hipStream_t)h->o.stream) : launch_attend_for<BF16>(c, a, (hipStream_t)h->o.stream));
+  const hipError_t e = h->o.type == PGXCACHE_F16 ? launch_attend_for<F16>(c, a, (hipStream_t)h->o.stream) : launch_attend_for<BF16>(c, a, (hipStream_t)h->o.stream);
+  if (e == hipErrorInvalidConfiguration) return PGXCACHE_EINVAL;
+  HIPCHK(e);
   return PGXCACHE_OK;
 }
 
@@ -988,7 +992,7 @@ int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_d
   if (!rows_apart(sizes, ks, h->o.head_dim) || !rows_apart(sizes, vs, h->o.head_dim)) return PGXCACHE_EINVAL;
   if (rows_meet(Rows{k_dev, {sizes[0], sizes[1], sizes[2]}, {ks[0], ks[1], ks[2]}}, Rows{v_dev, {sizes[0], sizes[1], sizes[2]}, {vs[0], vs[1], vs[2]}}, h->o.head_dim, 2)) return PGXCACHE_EINVAL;
   const Cache c = cache_of(h);
-  if (read_blocks(c, n, tokens) > 0x7FFFFFFF) return PGXCACHE_EINVAL;
+  if (!launchable(read_blocks(c, n, tokens), 256)) return PGXCACHE_EINVAL;
   const Tokens k = {(const char*)k_dev, k_entry_stride * 2, k_token_stride * 2, k_head_stride * 2}, v = {(const char*)v_dev, v_entry_stride * 2, v_token_stride * 2, v_head_stride * 2};
   HIPCHK(read_back(c, h->o.type == PGXCACHE_F16, layer, n, slots_dev, first_dev, first, tokens, k, v, (hipStream_t)h->o.stream));
   return PGXCACHE_OK;
@@ -998,11 +1002,13 @@ int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const i
   if (!list_ok(h, n)) return PGXCACHE_EINVAL;
   if (n == 0) return PGXCACHE_OK;
   if (!src_slots_dev || !dst_slots_dev) return PGXCACHE_EINVAL;
-  hipLaunchKernelGGL(fork_plan_kernel, dim3((unsigned)((n + kOneBlock - 1) / kOneBlock)), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->forks, status_dev);
-  HIPCHK(hipGetLastError());
   const size_t page = (size_t)cache_of(h).page_bytes();
   const int per = page <= 16384 ? 64 : page <= 32768 ? 128 : 256, entries = 256 / per, words = (h->o.pages + 63) / 64;
-  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)((n + entries - 1) / entries + (words + 255) / 256)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, h->forks, per);
+  const int64_t blocks = ((int64_t)n + entries - 1) / entries + (words + 255) / 256;
+  if (!launchable(blocks, 256)) return PGXCACHE_EINVAL;
+  hipLaunchKernelGGL(fork_plan_kernel, dim3(((unsigned)n + kOneBlock - 1) / kOneBlock), dim3(kOneBlock), 0, (hipStream_t)h->o.stream, cache_of(h), n, src_slots_dev, dst_slots_dev, h->forks, status_dev);
+  HIPCHK(hipGetLastError());
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, h->forks, per);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }
@@ -1010,7 +1016,9 @@ int pgxcache_fork(pgxcache_t h, int32_t n, const int32_t* src_slots_dev, const i
 int pgxcache_free(pgxcache_t h, int32_t n, const int32_t* slots_dev) {
   if (!list_ok(h, n)) return PGXCACHE_EINVAL;
   if (n == 0) return PGXCACHE_OK;
-  hipLaunchKernelGGL(free_kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, slots_dev);
+  const int64_t blocks = ((int64_t)n + 3) / 4;
+  if (!launchable(blocks, 256)) return PGXCACHE_EINVAL;
+  hipLaunchKernelGGL(free_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)h->o.stream, cache_of(h), n, slots_dev);
   HIPCHK(hipGetLastError());
   return PGXCACHE_OK;
 }

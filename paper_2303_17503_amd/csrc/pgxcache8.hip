@@ -600,18 +600,13 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
   finish_row<T, NT, W, SPLIT, true>(a, Spot{wave, lane, col, g, i, head0, heads_here, split, active, unit, alone}, top, sum, acc);
 }
 
-template <class T, int NT, int W, int BUF, bool SPLIT>
-hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, hipStream_t stream) {
-  const bool streamed = (int64_t)c.pages * c.page_bytes(1) > (int64_t)256 << 20;   // (as over 16 bits)
-  const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = SPLIT ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
-  const int64_t parts = (int64_t)a.n * a.splits, heads = (int64_t)c.kv_heads * a.head_tiles;
-  const dim3 grid((unsigned)(a.by_die ? (parts + 7) / 8 * 8 * heads : parts * heads)), block(64 * W);
-  if (streamed) hipLaunchKernelGGL((attend8_kernel<T, NT, W, BUF, SPLIT, true>), grid, block, join > weights ? join : weights, stream, c, a);
-  else hipLaunchKernelGGL((attend8_kernel<T, NT, W, BUF, SPLIT, false>), grid, block, join > weights ? join : weights, stream, c, a);
-  return hipGetLastError();
-}
-template <class T, int NT>
-hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
+// How an attend call is spread.
+struct Spread {
+  int waves, splits;   // wavefronts to a block, blocks to a row
+  bool by_die;
+  int64_t blocks;      // of the launch
+};
+Spread spread_of(const Cache& c, const AttendArgs& a) {
   // The lengths are known on the device only, so the choice goes by how long a slot can be and by the rows (2 key heads here, lengths from 1 up, us).
   //  * Up to 10 tiles of 32 tokens and from 1024 rows on a wavefront each (with 1, 2, 4 wavefronts: 1024 slots of up to 160 tokens, heads of 32 6.9 7.3 8.7, 64 7.4 8.1 10.2, 128 12.6 14.6
   //    22.1, 256 22 34 59; of up to 320, 64 11.8 12.5 13.4; 4096 of up to 320, 64 33.9 31.4 38.6, 128 75 77 100).
@@ -622,17 +617,40 @@ hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
   //  * Few rows that can be longer than 32 tiles are split over blocks, two for each compute unit at most (16 slots of 20000 tokens 20.8, with twice the blocks 27; 512
   //    slots of 2000 tokens in two blocks each 30.6, in one 23).
   const int64_t rows = (int64_t)a.n * c.kv_heads * a.head_tiles, most_tiles = (((int64_t)c.width << c.page_shift) + 31) / 32;
-  a.splits = 1;
+  Spread s{4, 1, false, 0};
   if (most_tiles > 32) {
     const int64_t spread = kSplitBlocks / rows, useful = (most_tiles + 7) / 8;
     const int64_t splits = spread < useful ? spread : useful;
-    a.splits = (int32_t)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
+    s.splits = (int)(splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits);
   }
-  a.by_die = a.head_tiles > 1 || (int64_t)a.n * a.splits >= 64;
-  if (a.splits > 1) return launch_attend_by<T, NT, 4, NT < 8 ? 2 : 1, true>(c, a, stream);   // (heads of 256: 201 slots of 2000 tokens 45.5 us, with the next tile beside the present 54)
-  if (rows >= 1024 && most_tiles <= 10) return launch_attend_by<T, NT, 1, 2, false>(c, a, stream);
-  if (NT == 8 ? rows >= 1024 || (rows >= 256 && most_tiles <= 32) : rows >= 4096 && most_tiles <= 32) return launch_attend_by<T, NT, 2, 2, false>(c, a, stream);
-  return launch_attend_by<T, NT, 4, 2, false>(c, a, stream);
+  if (s.splits == 1) {
+    if (rows >= 1024 && most_tiles <= 10) s.waves = 1;
+    else if (c.head_dim == 256 ? rows >= 1024 || (rows >= 256 && most_tiles <= 32) : rows >= 4096 && most_tiles <= 32) s.waves = 2;
+  }
+  const int64_t parts = (int64_t)a.n * s.splits, heads = (int64_t)c.kv_heads * a.head_tiles;
+  s.by_die = a.head_tiles > 1 || parts >= 64;
+  s.blocks = s.by_die ? (parts + 7) / 8 * 8 * heads : parts * heads;
+  return s;
+}
+
+template <class T, int NT, int W, int BUF, bool SPLIT>
+hipError_t launch_attend_by(const Cache& c, const AttendArgs& a, int64_t blocks, hipStream_t stream) {
+  const bool streamed = (int64_t)c.pages * c.page_bytes(1) > (int64_t)256 << 20;   // (as over 16 bits)
+  const size_t join = (size_t)(W - 1) * kHeads * NT * 32 * 4, weights = SPLIT ? (size_t)kMostSplits * kHeads * 4 + 64 * W * 16 : 0;
+  const dim3 grid((unsigned)blocks), block(64 * W);
+  if (streamed) hipLaunchKernelGGL((attend8_kernel<T, NT, W, BUF, SPLIT, true>), grid, block, join > weights ? join : weights, stream, c, a);
+  else hipLaunchKernelGGL((attend8_kernel<T, NT, W, BUF, SPLIT, false>), grid, block, join > weights ? join : weights, stream, c, a);
+  return hipGetLastError();
+}
+template <class T, int NT>
+hipError_t launch_attend(const Cache& c, AttendArgs a, hipStream_t stream) {
+  const Spread s = spread_of(c, a);
+  a.splits = s.splits;
+  a.by_die = s.by_die;
+  if (s.splits > 1) return launch_attend_by<T, NT, 4, NT < 8 ? 2 : 1, true>(c, a, s.blocks, stream);   // (heads of 256: 201 slots of 2000 tokens 45.5 us, with the next tile beside the present 54)
+  if (s.waves == 1) return launch_attend_by<T, NT, 1, 2, false>(c, a, s.blocks, stream);
+  if (s.waves == 2) return launch_attend_by<T, NT, 2, 2, false>(c, a, s.blocks, stream);
+  return launch_attend_by<T, NT, 4, 2, false>(c, a, s.blocks, stream);
 }
 
 template <class T>
@@ -675,6 +693,10 @@ hipError_t write8(const Cache& c, bool f16, int layer, int n, const int32_t* slo
   return f16 ? write8_for<F16>(c, layer, n, slots, tokens, last_only, k, v, stream) : write8_for<BF16>(c, layer, n, slots, tokens, last_only, k, v, stream);
 }
 
+bool attend8_fits(const Cache& c, const AttendArgs& a) {
+  const Spread s = spread_of(c, a);
+  return launchable(s.blocks, 64 * s.waves);
+}
 hipError_t attend8(const Cache& c, bool f16, const AttendArgs& a, hipStream_t stream) { return f16 ? attend8_for<F16>(c, a, stream) : attend8_for<BF16>(c, a, stream); }
 
 int64_t read_blocks(const Cache& c, int n, int tokens) {

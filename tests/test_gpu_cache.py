@@ -740,3 +740,62 @@ def test_numbers_of_tokens_and_layers_are_whole(native, monkeypatch):
     assert cache.lengths.tolist() == [20, 5]
     cache.advance(counts=torch.ones(1, dtype=torch.int64).numpy()[0])
     assert cache.lengths.tolist() == [21, 6]
+
+
+def sparse(slots, kv_heads, width, bits_):
+    """two pages and no tokens"""
+    return pg.PagedCache.empty(slots, 2, width * 16, 1, kv_heads, 32, bits=bits_)
+
+
+@pytest.mark.parametrize("bits_", [8, 16])
+def test_attention_of_more_rows_than_a_launch_takes(bits_):
+    n, kv_heads = 4104, 4096
+    cache = sparse(n, kv_heads, 65, bits_)                      # four wavefronts to a row: 2^32 threads
+    q = torch.zeros(1, kv_heads, 32, dtype=torch.bfloat16, device="cuda").expand(n, kv_heads, 32)
+    out = torch.full((n, kv_heads, 32), 7.0, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(pg.PgxGoError):
+        cache.attend(0, q, out=out)
+    assert (out == 7).all()
+    some = torch.arange(n - 16, dtype=torch.int32, device="cuda")
+    cache.attend(0, q[:-16], some, out=out[:-16])
+    assert (out[:-16] == 0).all() and (out[-16:] == 7).all()
+
+
+@pytest.mark.parametrize("bits_", [8, 16])
+def test_writing_and_reading_more_than_a_launch_takes(bits_):
+    n, kv_heads = 2 ** 17 + 8, 4096
+    cache = sparse(n, kv_heads, 1, bits_)
+    k = torch.zeros(1, 1, 1, 32, dtype=torch.bfloat16, device="cuda")
+    for tokens in (1, 2, 80):
+        with pytest.raises(pg.PgxGoError):
+            cache.write(0, *[k.expand(n, tokens, kv_heads, 32)] * 2)
+    some = torch.arange(n - 16, dtype=torch.int32, device="cuda")
+    cache.write(0, *[k.expand(n - 16, 1, kv_heads, 32)] * 2, some)
+    keys, values = (torch.empty(n, 1, kv_heads, 32, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    keys[-1], values[-1] = 7.0, 7.0
+    with pytest.raises(pg.PgxGoError):
+        cache.read(0, 1, k=keys, v=values)
+    cache.read(0, 1, some, k=keys[:-16], v=values[:-16])
+    assert all((part == 0).all() for t in (keys, values) for part in t[:-16].split(2 ** 14)) and (keys[-1] == 7).all() and (values[-1] == 7).all()
+    del keys, values
+    torch.cuda.empty_cache()
+
+
+def test_forking_and_freeing_more_than_a_launch_takes():
+    n = 2 ** 24
+    cache = sparse(n, 64, 1, 16)                                # pages of 131072 bytes: 256 threads to an entry
+    none, status = torch.full((n,), -1, dtype=torch.int32, device="cuda"), torch.full((n,), 99, dtype=torch.uint8, device="cuda")
+    with pytest.raises(pg.PgxGoError):
+        cache.fork(none, none, status)
+    assert (status == 99).all()
+    cache.fork(none[:-8], none[:-8], status[:-8])
+    assert (status[:-8] == 0).all()
+    n = 2 ** 26
+    cache = sparse(n, 1, 1, 16)
+    for refused in (None, torch.arange(n, dtype=torch.int32, device="cuda")):
+        cache.lengths.fill_(1)
+        with pytest.raises(pg.PgxGoError):
+            cache.free(refused)
+        assert (cache.lengths == 1).all()
+    cache.free(refused[8:])
+    assert (cache.lengths[8:] == 0).all() and (cache.lengths[:8] == 1).all()
