@@ -33,7 +33,7 @@ extern "C" {
 #endif
 
 #define PGXPOLICY_OK 0
-#define PGXPOLICY_EINVAL (-1) /* null pointer, size or pitch out of range, unknown type, repetition not above 0 */
+#define PGXPOLICY_EINVAL (-1) /* null pointer, size or pitch out of range (also rows of 2^32 threads: 16 to a row of up to 384 actions, 64 up to 2048, then 256), unknown type, repetition not above 0 */
 #define PGXPOLICY_EHIP (-2)   /* a HIP runtime call failed; see pgxpolicy_last_hip_error() */
 
 #define PGXPOLICY_F32 0

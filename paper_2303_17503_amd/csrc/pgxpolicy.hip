@@ -510,7 +510,8 @@ hipError_t launch(Args a, hipStream_t stream) {
   // a block of one wavefront while that leaves the machine's 256 compute units a block each at most; rows of a larger batch share blocks of four
   const int threads = G > 64 ? G : (int64_t)a.rows * G <= 64 * 1024 ? 64 : kThreads;
   const int rows_per_block = threads / G;
-  const unsigned blocks = (unsigned)((a.rows + rows_per_block - 1) / rows_per_block);
+  const unsigned blocks = ((unsigned)a.rows + (unsigned)rows_per_block - 1) / (unsigned)rows_per_block;
+  if ((int64_t)((blocks + 7) / 8 * 8) * threads >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;   // (a launch of so many threads runs what is left of them beyond 2^32, without an error)
   a.by_die = blocks >= 64;
   const dim3 grid(a.by_die ? (blocks + 7) / 8 * 8 : blocks), block((unsigned)threads);
   if (a.record) {
@@ -532,12 +533,16 @@ hipError_t launch_for_actions(const Args& a, hipStream_t stream) {
 template <int OP>
 int run(const Args& a, int32_t type, void* stream) {
   if (a.rows == 0) return PGXPOLICY_OK;
+  hipError_t e;
   switch (type) {
-    case PGXPOLICY_F32: HIPCHK((launch_for_actions<F32, OP>(a, (hipStream_t)stream))); return PGXPOLICY_OK;
-    case PGXPOLICY_F16: HIPCHK((launch_for_actions<F16, OP>(a, (hipStream_t)stream))); return PGXPOLICY_OK;
-    case PGXPOLICY_BF16: HIPCHK((launch_for_actions<BF16, OP>(a, (hipStream_t)stream))); return PGXPOLICY_OK;
+    case PGXPOLICY_F32: e = launch_for_actions<F32, OP>(a, (hipStream_t)stream); break;
+    case PGXPOLICY_F16: e = launch_for_actions<F16, OP>(a, (hipStream_t)stream); break;
+    case PGXPOLICY_BF16: e = launch_for_actions<BF16, OP>(a, (hipStream_t)stream); break;
     default: return PGXPOLICY_EINVAL;
   }
+  if (e == hipErrorInvalidConfiguration) return PGXPOLICY_EINVAL;
+  HIPCHK(e);
+  return PGXPOLICY_OK;
 }
 
 // rows of an output must not overlap; an input's may (pitch 0: one row for all games)

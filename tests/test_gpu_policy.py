@@ -509,3 +509,17 @@ def test_rows_beyond_32_bit_offsets(actions):
         assert torch.equal(a, b)
     for a, b in zip(pg.policy_loss(fx, fy, entropy=0.1, grad=far(x), **fhow), pg.policy_loss(x, y, entropy=0.1, **how)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("actions,threads", [(3, 16), (385, 64), (2049, 256)])
+def test_more_rows_than_a_launch_takes(actions, threads):
+    """a launch of 2^32 threads would run what is left of them beyond that: refused, just below it every row is sampled"""
+    n = 2 ** 32 // threads + 256
+    logits = torch.zeros(1, actions, dtype=torch.bfloat16, device="cuda")
+    logits[0, 1] = 40.0
+    out, logp = torch.full((n,), 7, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda")
+    with pytest.raises(pg.PgxGoError):
+        pg.sample_actions(logits.expand(n, actions), out=out, logp=logp)
+    assert (out == 7).all()
+    pg.sample_actions(logits.expand(n - 512, actions), out=out[:-512], logp=logp[:-512])
+    assert (out[:-512] == 1).all() and (out[-512:] == 7).all()
