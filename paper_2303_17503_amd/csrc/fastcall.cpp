@@ -6,6 +6,7 @@
 // anything is not as it has to be, and then the Python path runs and raises its error.  Nothing is kept between calls.
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/StreamGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -567,6 +568,7 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
           x.size(-2) > 65536 || !dense_rows(x) || !output(given[k], x.sizes(), type, first.device(), &outs[k]))
         return nullptr;
       const at::Tensor& o = outs[k];
+      if (c10::GradMode::is_enabled() && (x.requires_grad() || o.requires_grad())) return nullptr;
       parts[k] = pgxrotary_part{data_or_null(x), x.stride(0), dim == 4 ? x.stride(1) : 0, x.stride(-2), data_or_null(o), o.stride(0), dim == 4 ? o.stride(1) : 0, o.stride(-2),
                                 (int32_t)x.size(-2)};
     }
@@ -576,6 +578,8 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       return fn((int32_t)entries, (int32_t)tokens, (int32_t)D, (int32_t)(2 * f->size(0)), type == at::kFloat ? PGXROTARY_F32 : type == at::kHalf ? PGXROTARY_F16 : PGXROTARY_BF16,
                 (const int32_t*)p->data_ptr(), p->stride(0), dim == 4 ? p->stride(1) : 0, (const double*)f->data_ptr(), magnitude, interleaved, inverse, n, parts, stream);
     });
+    for (int k = 0; k < n && rc == 0; ++k)   // what autograd has kept of a given output is no longer what it was
+      if (given[k] != Py_None && !outs[k].is_inference()) outs[k].unsafeGetTensorImpl()->bump_version();
     if (n == 1) return outputs(rc, {{given[0], outs[0]}});
     return outputs(rc, {{given[0], outs[0]}, {given[1], outs[1]}});
   });

@@ -81,7 +81,9 @@ def rotate(x, positions, frequencies, interleaved=False, magnitude=1.0, inverse=
     (include/pgxrotary.h states the formula).  x: [n][heads][head_dim], or [n][tokens][heads][head_dim], of float32, float16 or bfloat16 with a dense last
     dimension, or a pair of them (queries and keys) that differ in their heads alone, for which one launch is enough; positions: int32 [n] or [n][tokens];
     frequencies: float64 [R / 2] (rotary_frequencies).  interleaved: pairs are neighbours, otherwise R / 2 apart.  inverse: turned back, times the
-    magnitude, which takes the result's gradient to x's.  out: as x, or x itself.  Returns a tensor, or a pair."""
+    magnitude, which takes the result's gradient to x's.  out: as x, or x itself.  Returns a tensor, or a pair.
+    The call makes no graph of its own: while one is being made, tensors that require gradients are refused (call it under torch.no_grad(), or in an autograd.Function
+    whose backward is the call with inverse=True)."""
     if not _ready: lib()
     if _fast is not None:
         got = _fast.rotate(_call, x, positions, frequencies, interleaved, magnitude, inverse, out)
@@ -114,6 +116,8 @@ def rotate(x, positions, frequencies, interleaved=False, magnitude=1.0, inverse=
         if len(outs) != len(xs) or any(not isinstance(o, torch.Tensor) or o.dtype is not t.dtype or o.device != dev or o.shape != t.shape or (o.numel() and D > 1 and o.stride(-1) != 1)
                                        for o, t in zip(outs, xs)):
             raise PgxGoError("out: expected tensors as x")
+    if torch.is_grad_enabled() and any(t.requires_grad for t in xs + outs):
+        raise PgxGoError("x: gradients would be lost, the call makes no graph; under torch.no_grad(), or in an autograd.Function whose backward is rotate(gradient, ..., inverse=True)")
     n, T = lead[0], lead[1] if len(lead) == 2 else 1
     if n * T >= 2 ** 31:
         raise PgxGoError(f"x: fewer than 2^31 tokens, got {n * T}")
@@ -122,4 +126,6 @@ def rotate(x, positions, frequencies, interleaved=False, magnitude=1.0, inverse=
     with _current(dev) as stream:
         _check(lib().pgxrotary_turn(n, T, D, R, TYPES[first.dtype], positions.data_ptr(), positions.stride(0), positions.stride(1) if len(lead) == 2 else 0,
                                     frequencies.data_ptr(), magnitude, int(bool(interleaved)), int(bool(inverse)), len(xs), parts, stream), "pgxrotary_turn")
+    if out is not None:   # what autograd has kept of them is no longer what it was
+        torch.autograd.graph.increment_version([o for o in outs if not o.is_inference()])
     return outs if pair else outs[0]

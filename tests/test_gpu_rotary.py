@@ -340,3 +340,44 @@ def test_more_entries_than_a_launch_has_blocks():
     check(want, x[:1000], positions[:1000], f, False, 1.0, False)
     full = n // 1000 * 1000
     assert (got[:full].view(-1, 1000, 2, 1, 2) == want).all() and torch.equal(got[full:], want[: n - full])
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_no_gradient_is_lost_unnoticed(native, monkeypatch):
+    """a call makes no graph: tensors that one is being made for are refused, and a tensor that is turned in place counts as changed"""
+    call()
+    if not native:
+        monkeypatch.setattr(pg.rotary_binding, "_fast", None)
+    leaf, plain = torch.randn(4, 2, 16, device="cuda", requires_grad=True), zeros(4, 2, 16)
+    for bad in (dict(x=leaf), dict(x=(plain, leaf)), dict(x=leaf * 2), dict(x=plain, out=leaf), dict(x=(plain, plain.clone()), out=(zeros(4, 2, 16), leaf)), dict(x=torch.nn.Parameter(plain.clone()))):
+        with pytest.raises(pg.PgxGoError, match="inverse"):
+            call(**bad)
+    want = call(x=leaf.detach())
+    with torch.no_grad():
+        got = call(x=leaf)
+    assert torch.equal(got, want) and not got.requires_grad and call(x=leaf.detach(), out=plain) is plain
+
+    class Turn(torch.autograd.Function):   # how a learner has both directions
+        @staticmethod
+        def forward(ctx, x, positions, f):
+            ctx.save_for_backward(positions, f)
+            return pg.rotate(x, positions, f)
+
+        @staticmethod
+        def backward(ctx, grad):
+            return pg.rotate(grad.contiguous(), *ctx.saved_tensors, inverse=True), None, None
+
+    positions, f, w = torch.tensor([3, 0, 700, 9], dtype=torch.int32, device="cuda"), pg.rotary_frequencies(16), torch.randn(4, 2, 16, device="cuda")
+    (Turn.apply(leaf, positions, f) * w).sum().backward()
+    check(leaf.grad, w, positions, f, False, 1.0, True)
+
+    for into in (lambda y: y, lambda y: (y, zeros(4, 2, 16))):
+        y = (leaf * 0.1).exp()                       # its backward needs y
+        with torch.no_grad():
+            call(x=into(y), out=into(y))
+        with pytest.raises(RuntimeError, match="modified by an inplace"):
+            y.sum().backward()
+    with torch.inference_mode():
+        t = zeros(4, 2, 16)
+        assert call(x=t, out=t) is t
+    assert call(x=t, out=t) is t
