@@ -40,8 +40,8 @@ typedef struct {
 /* For every entry i, token t and head, with p = positions[i][t], the first rotary_dim = R elements x of the head become
  *     a = p * frequencies_dev[j],  c = magnitude cos a,  s = magnitude sin a  (inverse != 0: s = -magnitude sin a),   0 <= j < R / 2
  *     x'[u] = x[u] c - x[w] s,   x'[w] = x[w] c + x[u] s,       u, w = j, j + R / 2,  or with interleaved != 0  2 j, 2 j + 1
- * and the others are copied.  inverse gives the gradient: d loss / d x from d loss / d x'.  The angle is formed and reduced in 64 bits (positions up to
- * 2^31 keep theirs to 2^-24), its cosine and sine and the products are in 32, rounded once to the type.
+ * and the others are copied.  inverse gives the gradient: d loss / d x from d loss / d x'.  The angle is formed and reduced as two 64-bit numbers (every
+ * position keeps its own to 2^-23 in 32 bits, while it turns less than 2^51 times), its cosine and sine and the products are in 32, rounded once to the type.
  * positions_dev: int32, element [i][t] at i * entry_stride + t * token_stride; they may repeat (stride 0).  frequencies_dev: float64 [R / 2], radians per position. */
 int pgxrotary_turn(int32_t entries, int32_t tokens, int32_t head_dim, int32_t rotary_dim, int32_t type, const int32_t* positions_dev, int64_t positions_entry_stride,
                    int64_t positions_token_stride, const double* frequencies_dev, float magnitude, int32_t interleaved, int32_t inverse, int32_t parts,

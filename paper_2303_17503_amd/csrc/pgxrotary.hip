@@ -128,7 +128,11 @@ __global__ void __launch_bounds__(256) turn_kernel(Args a) {
   for (int k = tid; k < here * A; k += threads) {
     const int t = A == 1 ? k : (int)__umulhi((uint32_t)k, a.pairs_inverse), j = k - t * A;
     const int32_t position = a.positions[entry * a.positions_entry + (int64_t)(token0 + t) * a.positions_token];
-    const double turn = (double)position * (a.frequencies[j] * 0.15915494309189533577), part = turn - rint(turn);   // of a whole circle, to -1/2 .. 1/2
+    // Of a whole circle, to -1/2 .. 1/2: the turns of a position as two numbers, and the whole turns taken off before their product with the position is rounded, so that 2^-52 of a turn
+    // is what is lost however far the position.
+    constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;   // 1 / (2 pi) is their sum
+    const double f = a.frequencies[j], far = (double)position, each = f * kTurn, each_rest = __builtin_fma(f, kTurnRest, __builtin_fma(f, kTurn, -each));
+    const double part = __builtin_fma(far, each_rest, __builtin_fma(far, each, -rint(far * each)));
     float s, c;
     sincospif(2.0f * (float)part, &s, &c);
     turns[k] = make_float2(a.magnitude * c, a.inverse ? -a.magnitude * s : a.magnitude * s);

@@ -4,6 +4,7 @@ Tolerance.  u = 2^-24.  The part of a circle is exact to |p| 2^-53 times the fre
 pi u + 2 pi 2^31 2^-53 < 4 u, cosine and sine (of sincospi, 2 units in the last place) by at most 4 u + 2 u and with the magnitude's product 7 u of the magnitude; a result x c - y s, of a
 rounded product and a fused one, by 9 u (|x| + |y|) times the magnitude, and the rounding to the type, half a step: eps / 2 of the result, and half of the smallest subnormal."""
 import random
+from fractions import Fraction
 
 import pytest
 import torch
@@ -381,3 +382,21 @@ def test_no_gradient_is_lost_unnoticed(native, monkeypatch):
         t = zeros(4, 2, 16)
         assert call(x=t, out=t) is t
     assert call(x=t, out=t) is t
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_of_the_farthest_positions(interleaved):
+    """cosines and sines themselves, against angles of whole numbers: position and frequency as fractions, over two pi to 100 digits.  The part of a circle is off by what 32 bits
+    leave of half of one, 2^-26 (pi / 2 u of an angle), and by 2^-52; sincospi by 2 units in the last place of a number up to 1, 2 u: less than 4 u together.
+    (An angle that is formed in one 64-bit product, or over a rounded two pi, is 2^31 2^-53 = 4 u off for each rounding, and for faster pairs more.)"""
+    two_pi = 2 * Fraction("3.1415926535897932384626433832795028841971693993751058209749445923078164062862089986280348253421170680")
+    r = random.Random(1)
+    positions = [0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 30 + 1] + [r.randrange(-2 ** 31, 2 ** 31) for _ in range(300)]
+    frequencies = [1.0, 0.1, 10000.0 ** (-2 / 48), 7.3, r.random(), 1e-4, 3.0, r.random() * 8]
+    x = torch.zeros(len(positions), 1, 16, device="cuda")
+    (x[..., 0::2] if interleaved else x[..., :8]).fill_(1.0)
+    got = pg.rotate(x, torch.tensor(positions, dtype=torch.int32, device="cuda"), torch.tensor(frequencies, dtype=torch.float64, device="cuda"), interleaved=interleaved)[:, 0].cpu().double()
+    c, s = (got[:, 0::2], got[:, 1::2]) if interleaved else (got[:, :8], got[:, 8:])
+    turns = [[Fraction(p) * Fraction(f) / two_pi for f in frequencies] for p in positions]
+    angle = torch.tensor([[float((t - round(t)) * two_pi) for t in row] for row in turns], dtype=torch.float64)
+    assert ((c - torch.cos(angle)).abs() <= 4 * U).all() and ((s - torch.sin(angle)).abs() <= 4 * U).all(), (float((c - torch.cos(angle)).abs().max() / U), float((s - torch.sin(angle)).abs().max() / U))
