@@ -28,8 +28,10 @@
  *     if tokens of the block were there before those that the call writes:  s = max(s, the block's scale), and where that makes the scale larger,
  *         their codes become  to nearest, ties to even (code * old scale / s)
  *     code = to nearest, ties to even (x / s);  NaN where x is not finite
- * so a value is held to 2^-4 of itself, or of 2^-6 s where it is smaller.  A slot's tokens are written in their order: what a block holds behind the
- * tokens that a call writes is given up.  Scales in memory that the caller fills are finite and above 0; if one is no power of two, x / s may be rounded twice.
+ * so a value is held to 2^-4 of itself, or where it is smaller than 2^-6 s to 2^-10 s, 2^-9 s if later tokens have raised the scale (each time it is rounded to half a step of the
+ * new scale, 2^-10 of that, and the scales before it add up to less than the last).  A slot's tokens are written in their order: what a block holds behind the
+ * tokens that a call writes is given up.  Scales in memory that the caller fills are finite, above 0 and at most 2^126; if one is no power of two, it is x times a reciprocal, off by 2^-22 of
+ * itself, that is rounded, and earlier codes times a quotient in 32 bits.
  * A finite value near the type's end (float16: above 63488, bfloat16: above 2^127.95) may be held as a number beyond it; it is read back as the type's largest number.
  *
  * Lists of slots: slots_dev[n] int32, n <= slots, pairwise distinct; NULL: slots 0 .. n-1.  An entry of -1 is left out (as action

@@ -66,3 +66,27 @@ def test_the_plain_model_keeps_its_own_rules(page):
     k, v = c.read(0, 5, [0, 3, -1], [88, 0, 0], torch.float64)
     n = int(c.lengths[0])
     assert torch.equal(k[0, : n - 88, 0], before[0, 0, 88:93][: 5]) and (k[1:] == 0).all() and (v[0, n - 88:] == 0).all()
+
+
+def test_what_is_held_after_the_scale_was_raised():
+    """Each raise rounds to half a step, 2^-10 of the new scale, what is below 2^-6 of it; the scales before it add up to less than the last: 2^-9 of that in all.
+    What is larger moves without rounding and stays within 2^-4 of itself."""
+    g = torch.Generator().manual_seed(3)
+
+    def after(x, scales):
+        s = scales[0]
+        code = e4m3(x / s)
+        for now in scales[1:]:
+            code, s = e4m3(code * s / now), now
+        return code * s
+
+    one = torch.tensor([0.65626], dtype=torch.float64)
+    assert float((after(one, [1.0, 64.0]) - one).abs()) > 2.0 ** -10 * 64      # 0.6875 at first, then 0.75
+    for _ in range(60):
+        raises = torch.randint(1, 5, (int(torch.randint(0, 7, (1,), generator=g)),), generator=g).cumsum(0)
+        scales = [2.0 ** -3] + [2.0 ** (-3 + int(e)) for e in raises]
+        x = (torch.rand(4000, generator=g, dtype=torch.float64) * 2 - 1) * 448 * scales[0] * torch.exp2(-torch.rand(4000, generator=g, dtype=torch.float64) * 20)
+        bound = torch.where(x.abs() >= scales[-1] * 2.0 ** -6, x.abs() * 2.0 ** -4, torch.tensor(scales[-1] * 2.0 ** -9))
+        assert ((after(x, scales) - x).abs() <= bound).all()
+        first = after(x, scales[:1])
+        assert ((first - x).abs() <= torch.where(x.abs() >= scales[0] * 2.0 ** -6, x.abs() * 2.0 ** -4, torch.tensor(scales[0] * 2.0 ** -10))).all()

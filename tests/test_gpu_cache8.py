@@ -11,7 +11,7 @@ import pytest
 import torch
 
 import paper_2303_17503_amd as pg
-from cache8_ref import RefCache8
+from cache8_ref import RefCache8, scale_for
 from test_gpu_cache import EDGES, ROUNDING, U, bits, ints, spread_of_lengths
 
 pytestmark = pytest.mark.gpu
@@ -693,3 +693,41 @@ def test_keys_and_values_read_into_memory_that_they_share(bits_, native, monkeyp
     for a, b in ((memory[:, :5, :2], memory[:, :5, 2:4]), (memory[:, 0:10:2, :2], memory[:, 1:11:2, :2]), (memory[:, :5, 0:4:2], memory[:, :5, 1:4:2])):   # rows between each other's
         got = cache.read(0, 5, first=30, k=a, v=b)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("how", ["one", "several", "attend", "attend by a launch of its own"])
+@pytest.mark.parametrize("head_dim", [32, 64, 96, 128, 256])
+def test_tokens_into_blocks_whose_scales_are_no_powers_of_two(head_dim, how):
+    """The product with a reciprocal is off by what the reciprocal (2^-23) and the product (2^-24) are, less than 2^-22 together; half a step of the code on top.  The step is that
+    of the exact quotient, 2^-3 of its power of two, or the next one's where 2^-22 takes it there."""
+    g = torch.Generator("cuda").manual_seed(head_dim)
+    filled_, new_ = 5, 3 if how == "several" else 1
+    scales = torch.tensor([1.25, 1.1, 0.7, 1 / 3, 3e-3, 0.0179, 2.0 ** -20 * 1.9, 3e3], device="cuda")
+    n, D = len(scales), head_dim
+    cache = filled([filled_] * n, 1, 2, D, 16, torch.bfloat16, seed=1, width=1, spare=0)
+    held = cache.table[:, 0].long()
+    cache.scales[held] = scales[:, None, None, None, None].expand(n, 1, 2, 2, 1).contiguous()
+    before = cache.kv.float()[held][:, 0, :, :, :filled_].double()
+    cache.advance(counts=new_)
+    k, v = new(g, torch.bfloat16, n, new_, 2, D), new(g, torch.bfloat16, n, new_, 2, D, size=0.3)
+    if how == "several": cache.write(0, k, v)
+    elif how == "one": cache.write(0, k[:, 0], v[:, 0])
+    else: cache.attend(0, torch.zeros(n, 2 if how == "attend" else 40, D, dtype=torch.bfloat16, device="cuda"), k=k[:, 0], v=v[:, 0])
+    now = cache.scales[held][:, 0, :, :, 0].double()                                               # [n][2][2]
+    x = torch.stack((k, v), 1).transpose(2, 3).double()                                            # [n][2][2][tokens][D]
+    own = torch.tensor([[[scale_for(m) for m in heads] for heads in which] for which in x.abs().amax((3, 4)).tolist()], dtype=torch.float64, device="cuda")
+    was = scales.double()[:, None, None].expand_as(own)
+    raised = own > was
+    assert torch.equal(now, torch.where(raised, own, was)) and raised.any() and not raised.all()
+    codes = cache.kv.float()[held][:, 0].double()
+
+    def near(code, exact):
+        _, e = torch.frexp(exact.abs() * (1 + 2.0 ** -22))
+        return ((code - exact).abs() <= torch.exp2((e.double() - 1).clamp(min=-6) - 4) + 2.0 ** -22 * exact.abs()).all()
+
+    now, was, raised = (t[..., None, None] for t in (now, was, raised))
+    assert near(codes[:, :, :, filled_: filled_ + new_], x / now) and near(codes[:, :, :, :filled_], before * was / now)
+    assert torch.equal(torch.where(raised, 0.0, codes[:, :, :, :filled_]), torch.where(raised, 0.0, before))
+    got = cache.read(0, new_, first=filled_)[0].transpose(1, 2).double()
+    want = codes[:, 0, :, filled_: filled_ + new_] * now[:, 0]
+    assert ((got - want).abs() <= 2.0 ** -8 * 1.01 * want.abs()).all()
