@@ -731,3 +731,58 @@ def test_tokens_into_blocks_whose_scales_are_no_powers_of_two(head_dim, how):
     got = cache.read(0, new_, first=filled_)[0].transpose(1, 2).double()
     want = codes[:, 0, :, filled_: filled_ + new_] * now[:, 0]
     assert ((got - want).abs() <= 2.0 ** -8 * 1.01 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("head_dim", [32, 64, 96, 128, 256])
+@pytest.mark.parametrize("tokens", [2, 17, 33, 40])
+def test_many_short_prompts(tokens, head_dim, dtype):
+    """thousands of entries of one to four blocks, which a wavefront writes one after the other: the same as in calls of fewer entries, a wavefront to each block, and some as in the
+    plain model; beginning anywhere in a block, with and without earlier tokens that are louder or quieter, entries without room, left out and no slots"""
+    n, kv_heads, layers = 2100, 2, 2
+    r, g = random.Random(tokens + head_dim), torch.Generator("cuda").manual_seed(head_dim)
+    lengths = [r.choice([0, 0, 1, 7, 15, 16, 17, 30, 31]) for _ in range(n)]
+    a, b = (filled(lengths, layers, kv_heads, head_dim, 16, dtype, seed=2, width=5, spare=4 * n, junk=False) for _ in range(2))
+    counts = [r.choice([0, 1, tokens // 2, tokens - 1, tokens, tokens, tokens + 3]) for _ in range(n)]
+    order = r.sample(range(n), n)
+    entries = [r.choice([-1, n, 2 ** 30]) if r.random() < 0.05 else s for s in order]
+    size = torch.exp2(torch.randint(-4, 5, (n, tokens, 1, 1), generator=g, device="cuda").float())
+    k, v = ((torch.randn(n, tokens, kv_heads, head_dim, generator=g, device="cuda") * size).to(dtype) for _ in range(2))
+    plain = [i for i in range(n) if 0 <= entries[i] < n][:12]
+    ref = ref_of(b)
+    for cache in (a, b):
+        cache.advance(ints(order), ints([counts[s] for s in order]))
+    ref.table, ref.lengths = b.table.cpu(), b.lengths.cpu()
+    ref.grown = [max(c, 0) for c in counts]
+    a.write(1, k, v, ints(entries))
+    assert n * 2 * kv_heads * ((tokens + 14) // 16 + 1) >= 16384
+    for i in range(0, n, 150):                 # (fewer than 16384 blocks in a call)
+        b.write(1, k[i: i + 150], v[i: i + 150], ints(entries[i: i + 150]))
+    assert torch.equal(a.kv.view(torch.uint8), b.kv.view(torch.uint8)) and torch.equal(a.scales.view(torch.int32), b.scales.view(torch.int32))
+    ref.write(1, k[plain].cpu(), v[plain].cpu(), [entries[i] for i in plain])
+    pages = [p for i in plain for p in ref.table[entries[i]].tolist() if p >= 0]
+    assert torch.equal(codes_of(a)[pages], bytes_of(ref.kv[pages])) and torch.equal(a.scales.cpu().double()[pages], ref.scales[pages])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("head_dim", [32, 64, 96, 128, 256])
+@pytest.mark.parametrize("n,width,kv_heads,heads", [(2050, 24, 2, 4), (2050, 64, 2, 2), (1030, 24, 4, 4)])
+def test_a_new_token_with_two_wavefronts_to_a_row(n, width, kv_heads, heads, head_dim, dtype):
+    """4096 rows and more of 11 to 32 tiles: what attention writes and gives is what write and attention give"""
+    r, g = random.Random(width), torch.Generator("cuda").manual_seed(head_dim)
+    most = width * 16
+    lengths = [r.choice([0, 1, 15, 16, 31, 32, 33, 63, 64, most // 2, most - 17, most - 3]) if i < 40 else r.choice([0, 5, 31, 33, 70]) for i in range(n)]
+    a, b = (filled(lengths, 1, kv_heads, head_dim, 16, dtype, seed=2, width=width, spare=3 * n) for _ in range(2))
+    assert n * kv_heads >= 4096 and 10 < (most + 31) // 32 <= 32
+    for step in range(3):
+        q = new(g, dtype, n, heads, head_dim)
+        size = torch.exp2(torch.randint(-3, 4, (n, 1, 1), generator=g, device="cuda").float())
+        k, v = ((torch.randn(n, kv_heads, head_dim, generator=g, device="cuda") * size).to(dtype) for _ in range(2))
+        for cache in (a, b):
+            cache.advance()
+        b.write(0, k, v)
+        got, want = a.attend(0, q, k=k, v=v, lse=True), b.attend(0, q, lse=True)
+        assert torch.equal(bits(got[0]), bits(want[0])) and torch.equal(bits(got[1]), bits(want[1]))
+        assert torch.equal(a.kv.view(torch.uint8), b.kv.view(torch.uint8)) and torch.equal(a.scales.view(torch.int32), b.scales.view(torch.int32))
+    few = list(range(12))
+    check_attend(a, ref_of(a), got[0][:12], got[1][:12], 0, q[:12], few, head_dim ** -0.5)
