@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
   const int32_t* row = c.row(is_slot ? slot : 0);
   // page of half-tile lane & 1 of the wavefront's tile number (a multiple of 32) + lane / 2; the first ones are asked for before the length is known
   int ids = 0;
-  if (!SPLIT || a.splits == 1) ids = row[min((((wave + (lane >> 1) * W) * 2 + (lane & 1)) << 4) >> c.page_shift, c.width - 1)];
+  if (!SPLIT) ids = row[min((((wave + (lane >> 1) * W) * 2 + (lane & 1)) << 4) >> c.page_shift, c.width - 1)];
   const int length = is_slot ? c.length(slot) : 0, grown = a.k && is_slot ? c.grown[slot] : 0;
 
   if (length == 0) {   // nothing to attend to
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(64 * W, BUF == 2 && NT == 8 ? 1 : 2) attend8_k
   auto lane_of = [](float x, int at) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), at)); };
   auto look_up = [&](int number) {   // pages and scales of the wavefront's tiles number to number + 31
     const int half = (begin + wave + (number + (lane >> 1)) * W) * 2 + (lane & 1);
-    if (number > 0 || (SPLIT && a.splits > 1)) take_pages(row[(min(half, last_half) << 4) >> c.page_shift]);
+    if (SPLIT || number > 0) take_pages(row[(min(half, last_half) << 4) >> c.page_shift]);
     const int64_t at = ids * page_scales + (half & in_blocks);
     asked_key_scale = key_scales[at];
     asked_value_scale = value_scales[at];
