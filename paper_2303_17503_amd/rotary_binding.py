@@ -53,7 +53,7 @@ def rotary_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, origi
       "parts"   pairs that turn at least `high` times within `original` positions stay, those that turn at most `low` times are slowed by factor, between them
                 the two are mixed by the number of turns (0.1 ln factor + 1 is then a usual `magnitude` for rotate)."""
     R = rotary_dim
-    if not isinstance(R, int) or not 2 <= R <= MAX_HEAD_DIM or R % 2:
+    if not isinstance(R, int) or isinstance(R, bool) or not 2 <= R <= MAX_HEAD_DIM or R % 2:
         raise PgxGoError(f"rotary_dim: an even number from 2 to {MAX_HEAD_DIM}, got {rotary_dim}")
     if not (0 < base < math.inf and 0 < factor < math.inf):
         raise PgxGoError(f"base and factor: above 0, got {base} and {factor}")
@@ -64,7 +64,12 @@ def rotary_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, origi
     if scaling == "base":
         if R == 2:
             raise PgxGoError("scaling 'base' needs a rotary_dim of 4 or more")
-        base = base * factor ** (R / (R - 2))
+        try:
+            base = base * factor ** (R / (R - 2))
+        except OverflowError:
+            base = math.inf
+        if not 0 < base < math.inf:
+            raise PgxGoError(f"scaling 'base': base and factor make a base of {base}")
     f = torch.tensor(base, dtype=torch.float64) ** (-torch.arange(0, R, 2, dtype=torch.float64) / R)
     if scaling == "linear":
         f = f / factor
@@ -73,6 +78,8 @@ def rotary_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, origi
             raise PgxGoError(f"scaling 'parts' needs original above 0 and low below high, got {original}, {low} and {high}")
         keep = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
         f = f * keep + f / factor * (1 - keep)
+    if not torch.isfinite(f).all():
+        raise PgxGoError("frequencies would not be finite")
     return f.to(device)
 
 

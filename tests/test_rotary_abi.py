@@ -162,3 +162,20 @@ def test_whether_rows_meet_against_every_element(tmp_path):
     subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(os.path.dirname(rotary_binding.__file__), "csrc"), "-o", str(exe), str(src)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.startswith("0 wrong of "), r.stdout
+
+
+@pytest.mark.parametrize("bad", [dict(scaling="parts", factor=2.0, original=8192, low=-math.inf),
+                                 dict(scaling="parts", factor=2.0, original=8192, low=-math.inf, high=math.inf),
+                                 dict(scaling="parts", factor=2.0, original=8192, high=math.nan), dict(scaling="parts", factor=2.0, original=math.nan),
+                                 dict(scaling="base", factor=1e200, rotary_dim=4), dict(scaling="base", factor=1e10, base=1e300), dict(base=math.nan), dict(scaling="linear", factor=math.nan),
+                                 dict(base=1e-300, scaling="linear", factor=1e-200), dict(rotary_dim=True)])
+def test_frequencies_that_would_not_be_finite(bad):
+    with pytest.raises(pg.PgxGoError):
+        pg.rotary_frequencies(**{**dict(rotary_dim=64, device="cpu"), **bad})
+
+
+def test_frequencies_at_the_ends():
+    """ends that leave every number finite are no reason to refuse"""
+    f = pg.rotary_frequencies(64, device="cpu")
+    assert torch.equal(pg.rotary_frequencies(64, scaling="parts", factor=2.0, original=8192, high=math.inf, device="cpu"), f / 2)
+    assert torch.equal(pg.rotary_frequencies(64, scaling="parts", factor=2.0, original=math.inf, device="cpu"), f)
