@@ -39,3 +39,12 @@ def test_no_kernel_keeps_vector_registers_in_memory(tmp_path):
     value = lambda block, key: int(re.search(rf"\.{key}: +(\d+)", block).group(1))  # noqa: E731
     spilled = {name: value(block, "vgpr_spill_count") for name, block in found if value(block, "vgpr_spill_count") or value(block, "private_segment_fixed_size")}
     assert not spilled, spilled
+
+
+@pytest.mark.skipif(not os.path.exists(READELF), reason="needs ROCm's llvm-readelf")
+def test_the_kernels_of_policies_and_their_cache_are_among_them(tmp_path):
+    """in every instance: types, head sizes, wavefronts to a row, ways of pairing"""
+    names = [name for name, _ in kernels(tmp_path)]
+    for part, instances in (("policy_kernel", 120), ("attend_kernel", 40), ("write_kernel", 1), ("fork_kernel", 1), ("compact_move_kernel", 1),
+                            ("attend8_kernel", 80), ("write8_kernel", 20), ("write8_one_kernel", 10), ("read_kernel", 3), ("turn_kernel", 6)):
+        assert sum(re.search(rf"\d{part}", name) is not None for name in names) >= instances, (part, [n for n in names if part in n])
