@@ -610,7 +610,10 @@ Spread spread_of(const Cache& c, const AttendArgs& a) {
   // The lengths are known on the device only, so the choice goes by how long a slot can be and by the rows (2 key heads here, lengths from 1 up, us).
   //  * Up to 10 tiles of 32 tokens and from 1024 rows on a wavefront each (with 1, 2, 4 wavefronts: 1024 slots of up to 160 tokens, heads of 32 6.9 7.3 8.7, 64 7.4 8.1 10.2, 128 12.6 14.6
   //    22.1, 256 22 34 59; of up to 320, 64 11.8 12.5 13.4; 4096 of up to 320, 64 33.9 31.4 38.6, 128 75 77 100).
-  //  * Up to 32 tiles and from 4096 rows on two (4096 of up to 722, 64 76.6 73.8 76.2; 1024 22.3 22.2 20.2).  Heads of 256, whose four have a compute unit to
+  //  * Up to 32 tiles and from 4096 rows on two (heads of 32, 64, 96, 128: 2048 slots of up to 400 17.7 22.9 31.3 38.2, with four 19.2 23.8 34.9 48.7, one 18.3 25.9 33.4 40.6; 4096 of up to 722 41.3
+  //    84.2 156.6 160.7, with four 44.3 84.0 159.9 175.9, one 44.2 86.6 160.6 160.8; 1024 of up to 722 16.9 22.9 31.0 36.5, with four 16.6 20.2 29.5 36.6), but for heads of 32 and 64 below 6144 rows
+  //    up to 16 tiles (2048 of up to 520 20.8 27.9 38.6 63.3, with four 22.2 27.4 40.5 71.1; of up to 722 25.7 38.1 76.7 81.9, with four 25.6 33.6 76.6 88.7; 3072 of up to 722 35.0 57.6 108.1 120.5, with
+  //    four 37.6 58.7 109.5 132.2).  Heads of 256, whose four have a compute unit to
   //    themselves: from 256 rows on (200 of up to 722 27.9 20.7 24.7, 1024 81 82 105), and from 1024 on however long (1024 of up to 1500 157 149 167).
   //  * Otherwise four (200 slots of up to 722, 64 13.7 11.4 8.2; 64, 128 16.4 10.9 8.4; 1024 of up to 1500, 64 41.9 41.1 36.0, of 4000 126 122 102); eight take as long with few rows and
   //    longer with many (one of 722 6.8 / 6.9, 256 9.3 / 8.3, 1024 26 / 21).
@@ -625,7 +628,7 @@ Spread spread_of(const Cache& c, const AttendArgs& a) {
   }
   if (s.splits == 1) {
     if (rows >= 1024 && most_tiles <= 10) s.waves = 1;
-    else if (c.head_dim == 256 ? rows >= 1024 || (rows >= 256 && most_tiles <= 32) : rows >= 4096 && most_tiles <= 32) s.waves = 2;
+    else if (c.head_dim == 256 ? rows >= 1024 || (rows >= 256 && most_tiles <= 32) : rows >= 4096 && most_tiles <= (c.head_dim <= 64 && rows < 6144 ? 16 : 32)) s.waves = 2;
   }
   const int64_t parts = (int64_t)a.n * s.splits, heads = (int64_t)c.kv_heads * a.head_tiles;
   s.by_die = a.head_tiles > 1 || parts >= 64;
