@@ -185,8 +185,9 @@ __global__ void __launch_bounds__(256) turn_kernel(Args a) {
 
 template <class T>
 hipError_t launch(Args& a, int32_t entries, bool interleaved, hipStream_t stream) {
-  // Tokens of a block: as many as give each of 256 threads three chunks, two of 32-bit elements (185000 tokens of 10 heads of 64 in bfloat16: 96.8 us, with two 96.6, four 98.3, eight 104; 192000 of 3
-  // heads of 256 126.5, 137.8, 130.4, 150; 40001 of 16 heads of 128 in float32 with one 134.6, two 137, three 139, four 143; 160000 of 10 of 130 389, 386, 398, 411), fewer where that would
+  // Tokens of a block: as many as give each of 256 threads three chunks, two of 32-bit elements (185000 tokens of 10 heads of 64 in bfloat16 with one 98.6 us, two 93.1, three 93.9, eight 104; 192000 of
+  // 3 heads of 256 146, 136, 126, 150; in float32 one and two are even: with one, two and three 65536 of 5 of 32 17.4, 16.4, -; 160000 of 10 of 130 336, 333.5, 345; 92000 of 16 of 128 270.5, 271.4, 280.9;
+  // 40001 of 16 of 128, half of each turned, 133.7, 134.8, 137.8; 185000 of 10 of 64 168.5, 175.9, 182; 64000 of 3 of 256 76.8, 82.9, 76.8), fewer where that would
   // leave the machine's 256 compute units without four blocks each (16384 tokens of one ply: 9.7 us, with half and twice the blocks 11.0 and 9.8); an entry's tokens in equal shares.
   constexpr int kChunks = sizeof(typename T::type) == 4 ? 2 : 3;
   const int64_t per_token = (int64_t)a.heads * a.chunks, spread = ((int64_t)entries * a.tokens + 1023) / 1024, room = 4096 / a.pairs;
