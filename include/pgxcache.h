@@ -113,7 +113,7 @@ int pgxcache_read(pgxcache_t h, int32_t layer, int32_t n, const int32_t* slots_d
  * overlap: strides below head_dim are refused); heads a multiple of kv_heads.  lse_dev
  * (nullable): float32 [n][heads], log sum_t exp(scale * q . K[t]).  k_dev and v_dev (both or neither): the key and value of each slot's
  * last token, [i][head][.], written to the cache by this call where the slot's last pgxcache_advance made room for it (and otherwise
- * ignored), so that a step takes one launch per layer; without them entries may repeat.  A slot without tokens, and an entry that is no slot, gives zeros and -infinity.
+ * ignored), so that a step takes one launch per layer (in 8 bits with more than 16 heads to a key head two); without them entries may repeat.  A slot without tokens, and an entry that is no slot, gives zeros and -infinity.
  * Scores, sums and the output before its rounding are held in 32 bits; probabilities are multiplied as two numbers of the
  * cache's type that add up to them within 2^-17 (float16: of the sum of 32 tokens' probabilities), however small they are.
  * With elements of 8 bits the probabilities, times the values' scales, are two bfloat16 numbers whatever `type` is, and a float16 output between its largest number and

@@ -3,9 +3,10 @@
 // An element is an e4m3 number times the scale of its block: 16 tokens of a slot (beginning with a multiple of 16) in one layer and head, keys or
 // values.  A head's block is one run of 16 head_dim bytes, half the rows of a matrix tile of attention, so that a wavefront knows its scale as one number.
 //
-// Bound by the bytes where there are many.  Measured, bfloat16, 2 heads of 64 unless said: attention of 4096 slots of 1 to 722 tokens 74 us, 5.2 TB/s in runs of 1 KB at random places (over 16 bits 134), of 3
-// sequences of 110000, 8 heads of 128 in float16, 110 to 120 us, 6 TB/s; of one slot of 722 6.2 us, a chain of round trips.  Writing 256 prompts of 60 to 500 tokens 17 us, 3.3 TB/s; one
-// token in each of 4096 slots 7.5 us (list, length, page, scale, block: a round trip each).  Reading 1024 slots of 1 to 722 tokens back 95.5 us, 5.0 TB/s.
+// Bound by the bytes where there are many.  Measured, bfloat16, 2 heads of 64 unless said: attention of 4096 slots of 1 to 722 tokens 74 to 77 us, 5.2 TB/s in runs of 1 KB at random places (over 16 bits 134), of 3
+// sequences of 110000, 8 heads of 128 in float16, 110 to 126 us, 5.4 to 6.2 TB/s; of one slot of 722 6.2 us, a chain of round trips.  Writing 256 prompts of 60 to 500 tokens 17 us, 3.3 TB/s (a chain of
+// round trips for 2 KB, and wavefronts for the longest prompt's blocks, of which 44 % find no token); one
+// token in each of 4096 slots 7.5 us (list, length, page, scale, block: a round trip each).  Reading 1024 slots of 1 to 722 tokens back 94 to 96 us, 5.0 TB/s.
 #include "cache_common.hpp"
 
 namespace pgxcache_parts {

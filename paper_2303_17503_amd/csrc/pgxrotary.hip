@@ -4,7 +4,7 @@
 // arithmetic and some 100 instructions, a pair of elements 4); then threads take the rows, 8 pairs each, so that neighbouring threads read neighbouring memory, with the next
 // row on its way while one is turned.
 //
-// Bound by the bytes: 185000 tokens of 10 heads of 64 in bfloat16 96.8 us, 4.9 TB/s (vector instructions keep half of the time busy); 40001 of 16 heads of 128 in float32, half of each turned, 137 us,
+// Bound by the bytes: 185000 tokens of 10 heads of 64 in bfloat16 94 to 97 us, 5.0 TB/s (vector instructions keep half of the time busy); 40001 of 16 heads of 128 in float32, half of each turned, 135 to 138 us,
 // 4.8 TB/s.  One ply of 256 games 3.3 us: a launch, one round trip to memory and an angle.
 #include <hip/hip_runtime.h>
 #include <math.h>
