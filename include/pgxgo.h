@@ -59,7 +59,7 @@ typedef struct {
 } pgxgo_opts;
 
 /* Bytes of device memory pgxgo_init needs for `batch` games of size board_size (9 or 19);
- * 0 if the arguments are invalid.  The caller allocates that many bytes, 256-byte aligned. */
+ * 0 if the arguments are invalid (also beyond 2^26 - 32 wavefronts, 201 million games of 19x19 or 402 million of 9x9).  The caller allocates that many bytes, 256-byte aligned. */
 size_t pgxgo_state_bytes(int32_t batch, int32_t board_size);
 
 /* Fig. 2 "init": creates `batch` games on the empty board, Black to move, and draws for each

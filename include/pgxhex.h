@@ -48,7 +48,7 @@ typedef struct {
   void* stream;       /* hipStream_t of the caller; NULL = default stream */
 } pgxhex_opts;
 
-/* Bytes of device memory pgxhex_init needs for `batch` games; 0 if batch <= 0.  The caller allocates that many
+/* Bytes of device memory pgxhex_init needs for `batch` games; 0 if batch <= 0 or beyond 2^26 - 32 wavefronts (335 million games).  The caller allocates that many
  * bytes, 256-byte aligned. */
 size_t pgxhex_state_bytes(int32_t batch);
 

@@ -2677,6 +2677,8 @@ int launch_reset(pgxgo_ctx* h, int first) {
   return PGXGO_OK;
 }
 
+// A launch of more than 2^32 threads runs what is left of them beyond that and reports no error: no more games than 2^26 wavefronts (less what blocks are rounded up by) hold.
+int most_games(int N) { return (N == 19 ? Geo<19>::W : Geo<9>::W) * ((1 << 26) - 32); }
 template <int N>
 unsigned waves_for(int B) { return (unsigned)((B + Geo<N>::W - 1) / Geo<N>::W); }
 template <int N>
@@ -3083,7 +3085,7 @@ int launch_superko_refresh(pgxgo_ctx* h, bool rebuild) {
 
 // validates the arguments of an init call and fills the handle; launches nothing
 int fill_ctx(pgxgo_ctx* h, int32_t batch, int32_t board_size, uint32_t seed, const pgxgo_opts* opts, void* state_dev, size_t state_bytes) {
-  if (batch <= 0 || (board_size != 9 && board_size != 19) || !state_dev) return PGXGO_EINVAL;
+  if (batch <= 0 || (board_size != 9 && board_size != 19) || batch > most_games(board_size) || !state_dev) return PGXGO_EINVAL;
   if (((uintptr_t)state_dev & 255u) != 0) return PGXGO_EINVAL;
   const int P = board_size * board_size;
   pgxgo_opts o;
@@ -3128,7 +3130,7 @@ static __device__ __align__(256) unsigned char scratch[PGXGO_STATIC_STATE_BYTES]
 extern "C" {
 
 size_t pgxgo_state_bytes(int32_t batch, int32_t board_size) {
-  if (batch <= 0) return 0;
+  if (batch <= 0 || batch > most_games(board_size)) return 0;
   if (board_size == 19) return state_bytes_for<19>(batch, nullptr, nullptr, nullptr);
   if (board_size == 9) return state_bytes_for<9>(batch, nullptr, nullptr, nullptr);
   return 0;
@@ -3400,7 +3402,7 @@ int pgxgo_fill_probe(void* dst_dev, size_t nbytes, uint32_t value, int32_t kind,
   if (!dst_dev || ((uintptr_t)dst_dev & 15u) != 0 || (nbytes & 15u) != 0 || kind < 0 || kind > 2) return PGXGO_EINVAL;
   if (nbytes == 0) return PGXGO_OK;
   const size_t n16 = nbytes / 16;
-  if ((n16 + 255) / 256 > 0x7FFFFFFFull) return PGXGO_EINVAL;
+  if ((n16 + 255) / 256 >= 1ull << 24) return PGXGO_EINVAL;   // 2^32 threads
   const dim3 grid((unsigned)((n16 + 255) / 256)), block(256);
   if (kind == 0) hipLaunchKernelGGL(fill_probe_kernel<kStorePlain>, grid, block, 0, (hipStream_t)stream, (uint4*)dst_dev, n16, value);
   else if (kind == 1) hipLaunchKernelGGL(fill_probe_kernel<kStoreStream>, grid, block, 0, (hipStream_t)stream, (uint4*)dst_dev, n16, value);

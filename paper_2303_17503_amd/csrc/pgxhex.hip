@@ -923,6 +923,9 @@ bool board_per_lane(const pgxhex_ctx* h, bool rollout = false) {
   return h->mapping == 2 || (h->mapping == 0 && h->B >= (rollout ? kLaneMappingFromRollout : kLaneMappingFromStep));
 }
 
+// A launch of more than 2^32 threads runs what is left of them beyond that and reports no error: no more games than 2^26 wavefronts (less what blocks are rounded up by) hold.
+constexpr int kMostGames = W * ((1 << 26) - 32);
+
 // grids of the board kernels: a multiple of 8 blocks (piece_of_block)
 unsigned blocks_for(int B) {
   const unsigned waves = (unsigned)((B + W - 1) / W);
@@ -979,14 +982,14 @@ int launch_step(pgxhex_ctx* h, const int32_t* actions, bool sample, uint32_t see
 
 extern "C" {
 
-size_t pgxhex_state_bytes(int32_t batch) { return batch > 0 ? state_layout(batch, nullptr, nullptr, nullptr) : 0; }
+size_t pgxhex_state_bytes(int32_t batch) { return batch > 0 && batch <= kMostGames ? state_layout(batch, nullptr, nullptr, nullptr) : 0; }
 
 int32_t pgxhex_boards_per_wavefront(void) { return W; }
 
 int pgxhex_init(pgxhex_t* out, int32_t batch, uint32_t seed, const pgxhex_opts* opts, void* state_dev, size_t state_bytes) {
   if (!out) return PGXHEX_EINVAL;
   *out = nullptr;
-  if (batch <= 0 || !state_dev || ((uintptr_t)state_dev & 255u) != 0) return PGXHEX_EINVAL;
+  if (batch <= 0 || batch > kMostGames || !state_dev || ((uintptr_t)state_dev & 255u) != 0) return PGXHEX_EINVAL;
   size_t off_meta, off_rew, off_term;
   if (state_bytes < state_layout(batch, &off_meta, &off_rew, &off_term)) return PGXHEX_EINVAL;
   pgxhex_ctx* h = (pgxhex_ctx*)calloc(1, sizeof(pgxhex_ctx));

@@ -103,3 +103,20 @@ def test_superko_entry_points_and_key_table():
 
     lows = [mix((0x9E3779B9 * (2 * p + c + 1)) & M) for p in range(361) for c in range(2)]
     assert len(set(lows)) == 722 and 0 not in lows
+
+
+def test_more_games_than_a_launch_takes():
+    """a launch of 2^32 threads would run what is left of them beyond that: 2^26 - 32 wavefronts at most"""
+    L, opts = pg.lib(), None
+    waves = 2 ** 26 - 32
+    for n in (9, 19):
+        most = L.pgxgo_boards_per_wavefront(n) * waves
+        assert L.pgxgo_state_bytes(most, n) > most and L.pgxgo_state_bytes(most + 1, n) == 0 and L.pgxgo_state_bytes(2 ** 31 - 1, n) == 0
+        h = C.c_void_p()
+        assert L.pgxgo_init(C.byref(h), most + 1, n, 0, opts, C.c_void_p(4096), 2 ** 62) == -1 and not h
+    H = pg.hex_binding.lib()
+    most = H.pgxhex_boards_per_wavefront() * waves
+    assert H.pgxhex_state_bytes(most) > most and H.pgxhex_state_bytes(most + 1) == 0
+    h = C.c_void_p()
+    assert H.pgxhex_init(C.byref(h), most + 1, 0, opts, C.c_void_p(4096), 2 ** 62) == -1 and not h
+    assert L.pgxgo_fill_probe(C.c_void_p(4096), 2 ** 36, 0, 0, None) == -1
